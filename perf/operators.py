@@ -176,13 +176,13 @@ def _normal(gen, *shape, dtype=torch.bfloat16, std=1.0):
 
 
 def _exponents(x):
-    """Smallest e with |x| 2^-e <= 448 over the last axis, not below -127; 448 = 1.75 * 2^8."""
+    """Smallest e with |x| 2^-e <= 448 over the last axis, not below -126; 448 = 1.75 * 2^8."""
     m, e = torch.frexp(x.abs().amax(-1))                    # amax = m 2^e, 0.5 <= m < 1
-    return torch.where(m > 0, e - 9 + (m > 0.875).int(), torch.full_like(e, -127)).clamp(min=-127)
+    return torch.where(m > 0, e - 9 + (m > 0.875).int(), torch.full_like(e, -126)).clamp(min=-126)
 
 
 def _power(e):
-    """2^e in 32 bits, exactly, for whole e from -126 to 127; 0 for -127."""
+    """2^e in 32 bits, exactly, for whole e from -126 to 127."""
     return ((e.int() + 127) << 23).view(torch.float32)
 
 
@@ -415,7 +415,7 @@ def _whole_power64(e):
 def _e4m3_64(x):
     """The values that rows of x are stored as: x 2^-e to the nearest e4m3, ties to even, times 2^e."""
     amax = x.abs().amax(-1, keepdim=True)
-    e = torch.ceil(torch.log2(torch.where(amax > 0, amax, torch.ones_like(amax)) / 448.0) - 1e-12).clamp(min=-127)
+    e = torch.ceil(torch.log2(torch.where(amax > 0, amax, torch.ones_like(amax)) / 448.0) - 1e-12).clamp(min=-126)
     y = x * _whole_power64(-e)
     step = _whole_power64(torch.frexp(y.abs().clamp(min=2.0 ** -6))[1] - 4)              # three bits behind the leading one
     return torch.where(amax > 0, torch.round(y / step) * step * _whole_power64(e), torch.zeros_like(x))
