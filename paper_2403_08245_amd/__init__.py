@@ -2,12 +2,13 @@
 
 Argument marshalling only: every function here checks tensor dtypes/contiguity, allocates
 outputs and scratch with torch, and calls the C entry point of the same name
-(smoe_<name>, declared in include/smoe.h) on torch's current HIP stream.  There is no
+(smoe_<name>, declared in include/smoe.h, or include/smoe_cache.h for positions and serving) on torch's current HIP stream.  There is no
 Python or PyTorch fallback: if libsmoe.so is missing, importing this package fails.
 """
 from __future__ import annotations
 
 import ctypes
+import math
 import os
 from dataclasses import dataclass
 
@@ -26,6 +27,11 @@ EXPORTS = [
     "smoe_plinear_act_fwd_workspace_bytes", "smoe_plinear_act_fwd", "smoe_mlp_fwd_workspace_bytes", "smoe_mlp_fwd", "smoe_mlp_saves_yhat", "smoe_mlp_bwd_workspace_bytes", "smoe_mlp_bwd",
     "smoe_group", "smoe_attention_fwd", "smoe_attention_bwd_workspace_bytes", "smoe_attention_bwd",
     "smoe_momha_fwd_workspace_bytes", "smoe_momha_fwd", "smoe_momha_bwd_workspace_bytes", "smoe_momha_bwd",
+]
+
+CACHE_EXPORTS = [
+    "smoe_rotary_frequencies", "smoe_rotary_fwd", "smoe_rotary_bwd", "smoe_cache_append", "smoe_cache_read",
+    "smoe_cached_attention_workspace_bytes", "smoe_cached_attention_fwd", "smoe_momha_decode_workspace_bytes", "smoe_momha_decode",
 ]
 
 
@@ -91,6 +97,32 @@ lib.smoe_mlp_bwd_workspace_bytes.restype = _sz
 lib.smoe_mlp_bwd.argtypes = [_vp, _vp, _i, _i, _vp, _vp, _i, _i, _i, _vp, _vp, _rp, _i, _vp, _vp, _vp, _vp,
                              _vp, _vp, _vp, _vp, _vp, _sz]
 lib.smoe_group.argtypes = [_vp, _vp, _i, _vp, _i, _rp, _i, _vp, _vp]
+
+
+class smoe_rotary(ctypes.Structure):
+    _fields_ = [("turns", _vp), ("rot", ctypes.c_int32), ("interleaved", ctypes.c_int32), ("amplitude", ctypes.c_float)]
+
+
+class smoe_cache(ctypes.Structure):
+    _fields_ = [("K", _vp), ("V", _vp), ("K_exp", _vp), ("V_exp", _vp), ("pages", ctypes.c_int32), ("page", ctypes.c_int32),
+                ("h", ctypes.c_int32), ("d_head", ctypes.c_int32), ("format", ctypes.c_int32)]
+
+
+class smoe_places(ctypes.Structure):
+    _fields_ = [("block_table", _vp), ("sequences", ctypes.c_int32), ("width", ctypes.c_int32), ("seqs", _vp), ("positions", _vp), ("lens", _vp)]
+
+
+_op, _cp, _pp, _d = ctypes.POINTER(smoe_rotary), ctypes.POINTER(smoe_cache), ctypes.POINTER(smoe_places), ctypes.c_double
+lib.smoe_rotary_frequencies.argtypes = [_i, _d, _i, _d, _d, _vp, _vp]
+lib.smoe_rotary_fwd.argtypes = lib.smoe_rotary_bwd.argtypes = [_vp, _vp, _i, _vp, _i, _vp, _i, _i, _i, _i, _vp, _op, _vp, _vp]
+lib.smoe_cache_append.argtypes = [_vp, _vp, _i, _cp, _pp, _vp, _vp, _i, _op, _vp, _i, _vp]
+lib.smoe_cache_read.argtypes = [_vp, _vp, _i, _cp, _pp, _i, _vp, _vp]
+lib.smoe_cached_attention_workspace_bytes.argtypes = [_i] * 5
+lib.smoe_cached_attention_workspace_bytes.restype = _sz
+lib.smoe_cached_attention_fwd.argtypes = [_vp, _vp, _i, _vp, _i, _i, _cp, _pp, _vp, _vp, _vp, _sz]
+lib.smoe_momha_decode_workspace_bytes.argtypes = [_i] * 6
+lib.smoe_momha_decode_workspace_bytes.restype = _sz
+lib.smoe_momha_decode.argtypes = [_vp, _vp, _i, _vp, _i, _i, _vp, _vp, _vp, _vp, _rp, _i, _vp, _cp, _pp, _op, _vp, _vp, _sz]
 
 
 class SmoeError(RuntimeError):
@@ -430,3 +462,213 @@ def mlp_bwd(dY, X, W1, W2, r: Routing, k: int, gates, act: int, buf: MLPBuffers)
                             _p(buf.dW1), _p(buf.dW2), _p(buf.dgates), _p(buf.ws_bwd), buf.ws_bwd.numel()),
            "smoe_mlp_bwd")
     return buf.dX, buf.dW1, buf.dW2, buf.dgates
+
+
+# ---- positions and serving (include/smoe_cache.h) ----------------------------------------------------------------------
+def _here(*tensors, dtype=None):
+    """_chk, and that the tensors live on the current device, on whose stream the launches go."""
+    dev = torch.cuda.current_device()
+    for t in tensors:
+        _chk(t, dtype)
+        if t.device.index != dev:
+            raise ValueError(f"tensor on {t.device}, but the current device is {dev}")
+
+
+ROTARY_SCALINGS = {"none": 0, "linear": 1, "base": 2, "blend": 3}
+
+
+class RotaryTable:
+    """Frequencies of the rotated pairs, on the device (made once; see smoe_rotary)."""
+
+    def __init__(self, turns: torch.Tensor, rot: int, interleaved: bool, amplitude: float):
+        self.turns, self.rot, self.interleaved, self.amplitude = turns, rot, interleaved, amplitude
+        self._c = ctypes.byref(smoe_rotary(turns.data_ptr(), rot, int(interleaved), amplitude))
+
+
+def rotary_table(rot: int, layout: str = "half", base: float = 10000.0, scaling: str = "none", factor: float = 1.0,
+                 trained_length: float = 4096.0, device=None) -> RotaryTable:
+    """Table of a rotation of the first `rot` elements of a row: pairs (i, i + rot/2) for layout "half", (2i, 2i+1) for "interleaved";
+    scaling "none", "linear", "base" or "blend" by `factor` (see smoe_rotary_scaling)."""
+    if layout not in ("half", "interleaved") or scaling not in ROTARY_SCALINGS:
+        raise ValueError(f"layout {layout!r}, scaling {scaling!r}")
+    turns = torch.zeros(max(rot, 2) // 2, dtype=torch.int64)
+    amplitude = ctypes.c_float(1.0)
+    _check(lib.smoe_rotary_frequencies(rot, base, ROTARY_SCALINGS[scaling], factor, trained_length, turns.data_ptr(), ctypes.byref(amplitude)),
+           "smoe_rotary_frequencies")
+    return RotaryTable(turns.to(torch.device("cuda", torch.cuda.current_device()) if device is None else device), rot, layout == "interleaved",
+                       amplitude.value)
+
+
+def _turn(entry, what, Q, K, table, positions, out):
+    _here(Q, table.turns)
+    if Q.dim() < 3:
+        raise ValueError("rows must be [B, T, heads..., d]")
+    B, T, d = Q.shape[0], Q.shape[1], Q.shape[-1]
+    hq, hk = math.prod(Q.shape[2:-1]), 0
+    if K is not None:
+        _here(K, dtype=Q.dtype)
+        if K.dim() < 3 or K.shape[:2] != Q.shape[:2] or K.shape[-1] != d:
+            raise ValueError("K must be [B, T, heads..., d] like Q")
+        hk = math.prod(K.shape[2:-1])
+    if positions is not None:
+        _here(positions, dtype=torch.int32)
+        if positions.numel() != B * T:
+            raise ValueError("positions must hold B*T entries")
+    Qr, Kr = (_like(Q), None if K is None else _like(K)) if out is None else out
+    if out is not None:
+        for t, like in ((Qr, Q), (Kr, K)):
+            if (t is None) != (like is None) or (t is not None and (t.shape != like.shape or t.dtype != like.dtype)):
+                raise ValueError("out must be a pair like (Q, K)")
+        _here(*(t for t in (Qr, Kr) if t is not None))
+    _check(entry(ctx(), _stream(), _dt(Q), _p(Q), hq, _p(K), hk, B * T, d, max(T, 1), _p(positions), table._c, _p(Qr), _p(Kr)), what)
+    return Qr, Kr
+
+
+def rotary_fwd(Q, K, table: RotaryTable, positions=None, out=None):
+    """Q [B, T, ..., d] and K [B, T, ..., d] (or None), F32 or BF16, turned by their positions: positions [B, T] int32, or 0..T-1 of every
+    sequence.  out = (Qr, Kr) may be (Q, K) themselves.  Returns (Qr, Kr)."""
+    return _turn(lib.smoe_rotary_fwd, "smoe_rotary_fwd", Q, K, table, positions, out)
+
+
+def rotary_bwd(dQ, dK, table: RotaryTable, positions=None, out=None):
+    """Gradient of rotary_fwd: (dQ, dK) of its inputs from those of its outputs."""
+    return _turn(lib.smoe_rotary_bwd, "smoe_rotary_bwd", dQ, dK, table, positions, out)
+
+
+class KVCache:
+    """A paged cache of keys and values: K and V [pages, h, page, d_head], bf16, or uint8 holding e4m3 with the rows' exponents
+    K_exp and V_exp [pages, h, page] uint8 (see smoe_cache).  The tensors stay the caller's and are written in place."""
+
+    def __init__(self, K: torch.Tensor, V: torch.Tensor, K_exp: torch.Tensor | None = None, V_exp: torch.Tensor | None = None):
+        quantised = K_exp is not None
+        for t in (K, V):
+            _chk(t, torch.uint8 if quantised else torch.bfloat16)
+        if K.dim() != 4 or V.shape != K.shape or (V_exp is not None) != quantised:
+            raise ValueError("K and V must be [pages, h, page, d_head], with exponents for both or neither")
+        for t in (K_exp, V_exp) if quantised else ():
+            _chk(t, torch.uint8)
+            if t.shape != K.shape[:3]:
+                raise ValueError("exponents must be [pages, h, page]")
+        if len({t.device for t in (K, V, K_exp, V_exp) if t is not None}) != 1:
+            raise ValueError("the cache's tensors must be on one device")
+        self.K, self.V, self.K_exp, self.V_exp = K, V, K_exp, V_exp
+        self.pages, self.h, self.page, self.d_head = K.shape
+        self.device = K.device.index
+        self._c = ctypes.byref(smoe_cache(_p(K), _p(V), _p(K_exp), _p(V_exp), self.pages, self.page, self.h, self.d_head, int(quantised)))
+
+
+def kv_cache(pages: int, page: int, h: int, d_head: int, quantised: bool = False, device=None) -> KVCache:
+    """An empty cache (contents unspecified: positions that were not written are never read)."""
+    device = torch.device("cuda", torch.cuda.current_device()) if device is None else device
+    K, V = (_new(pages, h, page, d_head, dtype=torch.uint8 if quantised else torch.bfloat16, device=device) for _ in "KV")
+    exps = [_new(pages, h, page, dtype=torch.uint8, device=device) for _ in "KV"] if quantised else [None, None]
+    return KVCache(K, V, *exps)
+
+
+def _places(cache: KVCache, block_table, lens=None, seqs=None, positions=None):
+    """The ctypes view of where rows live, and how many rows `seqs` names (None with lens)."""
+    if cache.device != torch.cuda.current_device():
+        raise ValueError(f"cache on device {cache.device}, but the current device is {torch.cuda.current_device()}")
+    _here(block_table, dtype=torch.int32)
+    if block_table.dim() != 2:
+        raise ValueError("block_table must be [sequences, width]")
+    B, width = block_table.shape
+    if lens is not None:
+        _here(lens, dtype=torch.int32)
+        if seqs is not None or positions is not None or lens.numel() != B:
+            raise ValueError("give lens [sequences], or seqs and positions")
+        return ctypes.byref(smoe_places(_p(block_table), B, width, None, None, _p(lens))), None
+    if seqs is None or positions is None or seqs.numel() != positions.numel():
+        raise ValueError("give lens [sequences], or seqs and positions of the same length")
+    _here(seqs, positions, dtype=torch.int32)
+    return ctypes.byref(smoe_places(_p(block_table), B, width, _p(seqs), _p(positions), None)), seqs.numel()
+
+
+def cache_append(cache: KVCache, K, V, block_table, lens=None, seqs=None, positions=None, rotary: RotaryTable | None = None, Q=None, out=None):
+    """Writes the rows K, V [rows, h, d_head] (bf16) to the last places of every sequence (lens), or to the listed ones; with `rotary` K is
+    turned first, and Q [rows, ..., d_head] into the returned tensor (`out`, which may be Q)."""
+    where, rows = _places(cache, block_table, lens, seqs, positions)
+    _here(K, V, dtype=torch.bfloat16)
+    M = K.numel() // (cache.h * cache.d_head)
+    if K.numel() != M * cache.h * cache.d_head or V.numel() != K.numel() or (M != rows if rows is not None else M % block_table.shape[0]):
+        raise ValueError("K and V must be [rows, h, d_head]")
+    hq, Qr = 0, None
+    if Q is not None:
+        _here(Q, dtype=torch.bfloat16)
+        hq = Q.numel() // max(1, M * cache.d_head)
+        if rotary is None or Q.numel() != M * hq * cache.d_head or Q.shape[-1] != cache.d_head:
+            raise ValueError("Q must be [rows, heads..., d_head], and goes with rotary")
+        Qr = _like(Q) if out is None else out
+        if out is not None:
+            _here(out, dtype=torch.bfloat16)
+            if out.shape != Q.shape:
+                raise ValueError("out must be like Q")
+        if M == 0:
+            Q = Qr = None       # nothing to turn
+    _check(lib.smoe_cache_append(ctx(), _stream(), BF16, cache._c, where, _p(K), _p(V), M, None if rotary is None else rotary._c, _p(Q), hq, _p(Qr)),
+           "smoe_cache_append")
+    return Qr
+
+
+def cache_read(cache: KVCache, block_table, lens=None, seqs=None, positions=None, N: int = 1, out=None):
+    """K, V [rows, h, d_head] (bf16) of the listed places, or of the last N of every sequence (lens)."""
+    where, rows = _places(cache, block_table, lens, seqs, positions)
+    rows = block_table.shape[0] * N if rows is None else rows
+    bf = dict(dtype=torch.bfloat16, device=cache.K.device)
+    K, V = (_new(rows, cache.h, cache.d_head, **bf) for _ in "KV") if out is None else out
+    if out is not None:
+        _here(K, V, dtype=torch.bfloat16)
+        if K.numel() != rows * cache.h * cache.d_head or V.numel() != K.numel():
+            raise ValueError("out must be two tensors [rows, h, d_head]")
+    _check(lib.smoe_cache_read(ctx(), _stream(), BF16, cache._c, where, rows, _p(K), _p(V)), "smoe_cache_read")
+    return K, V
+
+
+def cached_attention_fwd(Q, cache: KVCache, block_table, lens, out=None, ws=None):
+    """Q [B, N, G, h, d_head] (bf16), the last N positions of every sequence, over the cache -> O like Q, LSE [B, N, G, h] fp32.
+    out = (O, LSE) and ws reuse tensors; O may be Q."""
+    where, _ = _places(cache, block_table, lens)
+    _here(Q, dtype=torch.bfloat16)
+    B, N, G, h, d = Q.shape
+    if (h, d) != (cache.h, cache.d_head) or B != block_table.shape[0]:
+        raise ValueError("Q must be [sequences, N, G, h, d_head] with the cache's h and d_head")
+    O, LSE = (_like(Q), _new(B, N, G, h, dtype=torch.float32, device=Q.device)) if out is None else out
+    if out is not None:
+        _here(O, dtype=torch.bfloat16)
+        _here(LSE, dtype=torch.float32)
+        if O.shape != Q.shape or LSE.numel() != B * N * G * h:
+            raise ValueError("out must be a tensor like Q and one [B, N, G, h]")
+    nb = lib.smoe_cached_attention_workspace_bytes(B, N, G, h, d)
+    if ws is None:
+        ws = _ws(nb, Q.device)
+    _check(lib.smoe_cached_attention_fwd(ctx(), _stream(), BF16, _p(Q), N, G, cache._c, where, _p(O), _p(LSE), _p(ws), ws.numel()),
+           "smoe_cached_attention_fwd")
+    return O, LSE
+
+
+def momha_decode(X, W_K, W_V, W_Q, W_O, r: Routing, k: int, gates, cache: KVCache, block_table, lens, rotary: RotaryTable | None = None,
+                 out=None, ws=None):
+    """The SMoE attention layer on the last N positions of every sequence, X [B*N, d_model], over a cache that holds the earlier ones and
+    receives these.  Returns O [B*N, d_model]."""
+    where, _ = _places(cache, block_table, lens)
+    _here(X, W_K, W_V, W_Q, W_O, dtype=torch.bfloat16)
+    _here(gates, dtype=torch.float32)
+    M, d_model = X.shape
+    B, d_out = block_table.shape[0], cache.h * cache.d_head
+    if B == 0 or M == 0 or M % B or gates.numel() != M * k:
+        raise ValueError("X must be [sequences * N, d_model] and gates hold k for each row")
+    if W_K.numel() != d_model * d_out or W_V.numel() != W_K.numel() or W_Q.shape != (r.E, d_model, d_out) or W_O.shape != (r.E, d_out, d_model):
+        raise ValueError("weights do not fit d_model and the cache's h * d_head")
+    N = M // B
+    O = _like(X) if out is None else out
+    if out is not None:
+        _here(out, dtype=torch.bfloat16)
+        if out.shape != X.shape:
+            raise ValueError("out must be like X")
+    nb = lib.smoe_momha_decode_workspace_bytes(B, N, k, d_model, cache.h, cache.d_head)
+    if ws is None:
+        ws = _ws(nb, X.device)
+    rc = r.c()
+    _check(lib.smoe_momha_decode(ctx(), _stream(), BF16, _p(X), N, d_model, _p(W_K), _p(W_V), _p(W_Q), _p(W_O), ctypes.byref(rc), k, _p(gates),
+                                 cache._c, where, None if rotary is None else rotary._c, _p(O), _p(ws), ws.numel()), "smoe_momha_decode")
+    return O

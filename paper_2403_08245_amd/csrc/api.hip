@@ -1,12 +1,10 @@
 // C ABI of libsmoe: argument checks, workspace layout and the order of kernel launches for
 // ParallelLinear (Alg. 1, Alg. 2) and the SMoE MLP (Alg. 3).  No entry point allocates,
 // synchronises or touches the host copy of any tensor.
-#include "common.h"
+#include "cache.h"
 #include <new>
 
 namespace {
-inline bool aligned16(const void *p) { return ((uintptr_t)p & 15) == 0; }
-
 bool routing_ok(const smoe_routing *r) {
   if (!r || r->Tk < 0 || r->E < 1 || !r->expert_offsets) return false;
   return r->Tk == 0 || (r->sorted_expert_idxs && r->sorted_scattered_idxs);  // empty index arrays may be null
@@ -43,12 +41,6 @@ bool dw_reads_rows(const smoe_ctx *ctx, DWArgs a) {
   return ctx->kernel_mode == 0 && dw_stream_supported(a);
 }
 
-// Do two arrays share memory?  (An output over an input that only an earlier launch reads is fine while these are launches of their
-// own, and not where one launch does it all.)
-bool overlap(const void *a, size_t a_bytes, const void *b, size_t b_bytes) {
-  const uintptr_t p = (uintptr_t)a, q = (uintptr_t)b;
-  return a && b && p < q + b_bytes && q < p + a_bytes;
-}
 // The parts of an fp32 backward pass that wait for nothing but their inputs: in one launch, or (`apart`, or too many blocks for
 // one) in the order row dots, weight gradient, input gradient.
 int run_f32_backward(hipStream_t s, const S2SArgs &x, const DWArgs &w, const RowDots &d, bool apart) {
@@ -1013,6 +1005,56 @@ int smoe_momha_bwd(smoe_ctx *ctx, void *stream, smoe_dtype dtype, const void *dO
                    sub_bytes, in_sum ? dXk : nullptr, in_sum ? dXv : nullptr, inv);
   if (rc != SMOE_OK || in_sum) return rc;
   return launch_add3(s, dXq, dXk, dXv, dX, (size_t)N * d_model);
+}
+
+// ------------------------------------------------------------------------------ Alg. 4, decoding
+size_t smoe_momha_decode_workspace_bytes(int B, int N, int k, int d_model, int h_expert, int d_head) {
+  const size_t attention = smoe_cached_attention_workspace_bytes(B, N, k, h_expert, d_head);
+  if (!attention || d_model < 1) return 0;
+  MomhaSizes z = momha_sizes(B, N, k, d_model, h_expert, d_head);
+  return 256 + S2S_TAIL_WS_BYTES + 2 * z.kv + z.q + z.lse + z.yhat + attention;
+}
+
+int smoe_momha_decode(smoe_ctx *ctx, void *stream, smoe_dtype dtype, const void *X, int N, int d_model, const void *W_K, const void *W_V,
+                      const void *W_Q, const void *W_O, const smoe_routing *r, int k, const float *gates, const smoe_cache *cache,
+                      const smoe_places *places, const smoe_rotary *rotary, void *O, void *ws, size_t ws_bytes) {
+  if (!ctx || !routing_ok(r) || !X || !W_K || !W_V || !W_Q || !W_O || !gates || !O || N < 1 || k < 1 || d_model < 1) return SMOE_ERR_INVALID_ARG;
+  int rc = cache_args_ok(cache);
+  if (rc == SMOE_OK) rc = lengths_ok(cache, places);
+  if (rc == SMOE_OK && rotary) rc = rotary_args_ok(rotary, cache->d_head);
+  if (rc != SMOE_OK) return rc;
+  const int B = places->sequences, h = cache->h, d_head = cache->d_head;
+  if ((long long)B * N * k != r->Tk) return SMOE_ERR_INVALID_ARG;
+  const size_t need = smoe_momha_decode_workspace_bytes(B, N, k, d_model, h, d_head);
+  if (dtype != SMOE_BF16 || !width_ok(dtype, d_model) || !need || (long long)k * h > 65535) return SMOE_ERR_UNSUPPORTED;
+  if (!aligned16(X) || !aligned16(W_K) || !aligned16(W_V) || !aligned16(W_Q) || !aligned16(W_O) || !aligned16(O)) return SMOE_ERR_UNSUPPORTED;
+  if (!ws || ((uintptr_t)ws & 255) || ws_bytes < need) return SMOE_ERR_WORKSPACE;
+  const int M = B * N, d_out = h * d_head;
+  MomhaSizes z = momha_sizes(B, N, k, d_model, h, d_head);
+  char *p = (char *)ws;
+  int32_t *dense_off = (int32_t *)p;  p += 256;
+  float *tail_ws = (float *)p;  p += S2S_TAIL_WS_BYTES;
+  void *K = p;  p += z.kv;
+  void *V = p;  p += z.kv;
+  void *Q = p;  p += z.q;              // turned in place, then the attention's output in its place
+  float *LSE = (float *)p;  p += z.lse;
+  void *Yhat = p;  p += z.yhat;
+  hipStream_t s = (hipStream_t)stream;
+  auto product = [&](S2SArgs a) { a.tail_ws = tail_ws; return run_s2s(ctx, s, dtype, a); };
+  S2SArgs pv = dense_s2s(X, W_V, V, dense_off, M, d_model, d_out, false);
+  S2SArgs pk = dense_s2s(X, W_K, K, dense_off, M, d_model, d_out, false);
+  pv.tail_ws = pk.tail_ws = tail_ws;
+  rc = run_s2s_pair(ctx, s, pv, pk, dense_off);
+  if (rc != SMOE_OK) return rc;
+  rc = product(make_s2s(X, W_Q, Q, r, d_model, d_out, false, false, k, false));
+  if (rc != SMOE_OK) return rc;
+  rc = smoe_cache_append(ctx, stream, dtype, cache, places, K, V, M, rotary, rotary ? Q : nullptr, k * h, rotary ? Q : nullptr);
+  if (rc != SMOE_OK) return rc;
+  rc = smoe_cached_attention_fwd(ctx, stream, dtype, Q, N, k, cache, places, Q, LSE, p, need - (size_t)(p - (char *)ws));
+  if (rc != SMOE_OK) return rc;
+  rc = product(make_s2s(Q, W_O, Yhat, r, d_out, d_model, false, false, 1, false));
+  if (rc != SMOE_OK) return rc;
+  return launch_combine(s, dtype, Yhat, gates, O, M, k, d_model);
 }
 
 }  // extern "C"

@@ -25,6 +25,13 @@ struct smoe_ctx {
 
 static inline size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
 static inline size_t dtype_size(smoe_dtype d) { return d == SMOE_BF16 ? 2 : 4; }
+static inline bool aligned16(const void *p) { return ((uintptr_t)p & 15) == 0; }
+// Do two arrays share memory?  (An output over an input that only an earlier launch reads is fine while these are launches of their
+// own, and not where one launch does it all.)
+static inline bool overlap(const void *a, size_t a_bytes, const void *b, size_t b_bytes) {
+  const uintptr_t p = (uintptr_t)a, q = (uintptr_t)b;
+  return a && b && p < q + b_bytes && q < p + a_bytes;
+}
 static inline int ceil_div(int a, int b) { return (a + b - 1) / b; }
 
 template <typename T> __device__ __forceinline__ float to_f32(T v);
