@@ -1,114 +1,539 @@
-// Attention of the last N positions of every sequence over the paged cache.
+// Attention of the last N positions of every sequence over the paged cache: the decoding form of attention.hip.
+//
+// Bound by memory: every key and value is read once for the N * G query rows of its head, and 32 rows at most share a read, so a byte of
+// the cache meets 16 to 32 multiplications a row where the matrix cores could do 300.  What counts is that all compute units read from the
+// first microsecond to the last, whatever the lengths are: a sequence's keys are cut into pieces of about the same length over the
+// whole batch, one block a piece, and a second kernel joins the pieces of a sequence from their maxima and sums.
+//
+// Inside a block four wavefronts take steps of 32 keys in turn, from memory straight to registers.  Scores are worked out transposed,
+// S^T[key][query] = K Q^T on 16 x 16 x 32 matrix instructions, so a lane owns one query column: its running maximum and sum are scalars of
+// the lane, and its eight weights of a step already lie as the second product's operand, O^T[column][query] = V^T P^T, whose contraction
+// runs over the keys in the order the lanes hold them.  A lane reads its eight keys' values for D / 16 columns and turns them
+// into the operands of D / 16 instructions by byte permutations.  No LDS and no barrier until a piece ends.
 #include "cache.h"
+#include <algorithm>
+#include <type_traits>
 
 namespace {
 
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+
+constexpr int STEP = 32;         // keys of a step
+constexpr int WAVES = 4;
+constexpr int TARGET = 1024;     // pieces that the whole batch is cut into, about
+constexpr int MIN_STEPS = 16;    // steps of a piece, at least
+
 struct Dims {
-  int N, G, shift;
+  int N, G, R;                   // R = N * G query rows of a (sequence, head)
+  int tiles;                     // row tiles of each
+  int units;                     // tiles * h: what a sequence is worked on as
+  int shift;                     // page = 1 << shift
+  int cap;                       // positions the table can hold
+  int rows;                      // rows a piece leaves in the workspace
 };
 
-// 8 stored elements of a row, as fp32
-template <int FORMAT> __device__ __forceinline__ void stored8(const void *pages, const uint8_t *exps, size_t row, int d, int e0, float (&y)[8]) {
-  if constexpr (FORMAT == SMOE_CACHE_BF16) {
-    typedef bf16_t vec __attribute__((ext_vector_type(8)));
-    const vec v = *reinterpret_cast<const vec *>((const bf16_t *)pages + row * d + e0);
+// ------------------------------------------------------------------------------------------------ the cut
+// Steps of a sequence; one without keys has one, whose block writes its zeros.
+__device__ __forceinline__ int length_of(const int32_t *lens, int b, int cap) { return min(max(lens[b], 0), cap); }
+__device__ __forceinline__ int steps_of(int len) { return max((len + STEP - 1) / STEP, 1); }
+
+template <int CTRL, int ROWS> __device__ __forceinline__ int shifted(int v) { return __builtin_amdgcn_update_dpp(0, v, CTRL, ROWS, 0xf, false); }
+// inclusive sums over the lanes
+__device__ __forceinline__ int scan_add(int v) {
+  v += shifted<0x111, 0xf>(v);
+  v += shifted<0x112, 0xf>(v);
+  v += shifted<0x114, 0xf>(v);
+  v += shifted<0x118, 0xf>(v);
+  v += shifted<0x142, 0xa>(v);
+  v += shifted<0x143, 0xc>(v);
+  return v;
+}
+__device__ __forceinline__ float scan_add(float v) {
+  auto f = [](int x) { return __int_as_float(x); };
+  v += f(shifted<0x111, 0xf>(__float_as_int(v)));
+  v += f(shifted<0x112, 0xf>(__float_as_int(v)));
+  v += f(shifted<0x114, 0xf>(__float_as_int(v)));
+  v += f(shifted<0x118, 0xf>(__float_as_int(v)));
+  v += f(shifted<0x142, 0xa>(__float_as_int(v)));
+  v += f(shifted<0x143, 0xc>(__float_as_int(v)));
+  return v;
+}
+__device__ __forceinline__ int at_lane(int v, int lane) { return __builtin_amdgcn_readlane(v, lane); }
+
+struct Place {
+  int b, len, n;       // sequence, its length, the pieces each of its units is cut into
+  int local;           // number within what is counted of this sequence
+  int slot;            // pieces of cut sequences before this sequence's
+};
+// Which sequence does number `index` belong to, counting the pieces of all units (JOIN false), or the units that are cut (JOIN true), in the
+// order of the sequences?  Every wavefront finds its own: a lane takes ceil(B / 64) sequences in a row.  The length of a piece follows from
+// the batch's steps; their sum is a floating number (a few roundings longer or shorter pieces), the same in every wavefront of both kernels.
+// With the hundredth that it is longer there are fewer than TARGET cut units, and fewer than 2 TARGET pieces of cut units.
+template <bool JOIN> __device__ __forceinline__ bool find_piece(const int32_t *lens, int B, const Dims &d, int index, int lane, Place &p) {
+  const int each = (B + 63) >> 6, first = min(lane * each, B), end = min(first + each, B);
+  float sum = 0.f;
+  int mine = 0;                               // the only one's length, where each is one
+  for (int b = first; b < end; ++b) {
+    mine = length_of(lens, b, d.cap);
+    sum += (float)steps_of(mine);
+  }
+  const float total = __int_as_float(at_lane(__float_as_int(scan_add(sum)), 63)) * (float)d.units;
+  const int per = max((int)fminf(total * (1.01f / TARGET), 1e9f) + 1, MIN_STEPS);
+  int pieces = 0, cut_pieces = 0, cut_units = 0;
+  for (int b = first; b < end; ++b) {
+    const int n = (steps_of(each == 1 ? mine : length_of(lens, b, d.cap)) + per - 1) / per;
+    pieces += n * d.units;
+    cut_pieces += n > 1 ? n * d.units : 0;
+    cut_units += n > 1 ? d.units : 0;
+  }
+  const int counted = JOIN ? cut_units : pieces;
+  const int upto = scan_add(counted), slots_upto = scan_add(cut_pieces);
+  const unsigned long long past = __ballot(upto > index);
+  if (!past) return false;
+  const int owner = __ffsll((long long)past) - 1;
+  int before = at_lane(upto - counted, owner), slot = at_lane(slots_upto - cut_pieces, owner);
+  for (int c = 0; c < each; c += 64) {        // that lane's sequences, one a lane
+    const int b = owner * each + c + lane;
+    const bool have = c + lane < each && b < B;
+    const int len = have ? length_of(lens, b, d.cap) : 0, n = have ? (steps_of(len) + per - 1) / per : 0;
+    const int all = n * d.units, cut = n > 1 ? all : 0, here = JOIN ? (n > 1 ? d.units : 0) : all;
+    const int to = scan_add(here), slots_to = scan_add(cut);
+    const unsigned long long found = __ballot(before + to > index);
+    if (found) {
+      const int l = __ffsll((long long)found) - 1;
+      p.b = owner * each + c + l;
+      p.len = at_lane(len, l);
+      p.n = at_lane(n, l);
+      p.local = index - before - at_lane(to - here, l);
+      p.slot = slot + at_lane(slots_to - cut, l);
+      return true;
+    }
+    before += at_lane(to, 63);
+    slot += at_lane(slots_to, 63);
+  }
+  return false;
+}
+
+// What a piece leaves: its rows' sums of weighted values [rows][D], then their maxima and sums of weights [rows] each.
+__host__ __device__ inline size_t slot_floats(int rows, int D) { return (size_t)rows * (D + 2); }
+
+// ------------------------------------------------------------------------------------------------ a step's operands
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t window(const void *p, int bytes) { return __builtin_amdgcn_make_buffer_rsrc((void *)p, 0, bytes, 0x00020000); }
+__device__ __forceinline__ u32x4 load4(__amdgpu_buffer_rsrc_t w, int at) {
+  return __builtin_amdgcn_raw_buffer_load_b128(w, at, 0, 0);
+}
+__device__ __forceinline__ u32x2 load2(__amdgpu_buffer_rsrc_t w, int at) { return __builtin_amdgcn_raw_buffer_load_b64(w, at, 0, 0); }
+__device__ __forceinline__ uint32_t load1(__amdgpu_buffer_rsrc_t w, int at) { return __builtin_amdgcn_raw_buffer_load_b32(w, at, 0, 0); }
+
+// two bf16 of the lower or upper two of four e4m3 codes, scaled
+template <bool UPPER> __device__ __forceinline__ uint32_t widen(uint32_t codes, float scale) {
+  return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(codes, scale, UPPER));
+}
+
+// Keys: lane -> key (lane % 16) of each of the two groups of 16, D / 4 elements of its row.  Which elements go with which instruction is
+// free as long as the queries' fragments follow (query_offset).  A group of 16 keys lies on one page.
+template <int D, int FORMAT> struct Keys {
+  static constexpr int LOADS = FORMAT == SMOE_CACHE_BF16 ? D / 32 : D / 64;
+  u32x4 v[2][LOADS];
+  float scale[2];
+  __device__ __forceinline__ void load(int t, __amdgpu_buffer_rsrc_t rows, __amdgpu_buffer_rsrc_t exps, int lane) {
+    constexpr int BYTES = FORMAT == SMOE_CACHE_BF16 ? D * 2 : D;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) y[i] = (float)v[i];
-  } else {
-    typedef float f32x2 __attribute__((ext_vector_type(2)));
-    const uint2 q = *reinterpret_cast<const uint2 *>((const uint8_t *)pages + row * d + e0);
-    const float scale = e4m3_scale(exps[row]);
-    const f32x2 a = __builtin_amdgcn_cvt_pk_f32_fp8((int)q.x, false), b = __builtin_amdgcn_cvt_pk_f32_fp8((int)q.x, true);
-    const f32x2 c = __builtin_amdgcn_cvt_pk_f32_fp8((int)q.y, false), e = __builtin_amdgcn_cvt_pk_f32_fp8((int)q.y, true);
-    y[0] = a[0] * scale; y[1] = a[1] * scale; y[2] = b[0] * scale; y[3] = b[1] * scale;
-    y[4] = c[0] * scale; y[5] = c[1] * scale; y[6] = e[0] * scale; y[7] = e[1] * scale;
+    for (int i = 0; i < LOADS; ++i) v[t][i] = load4(rows, (lane & 15) * BYTES + i * 64 + (lane >> 4) * 16);
+    if constexpr (FORMAT == SMOE_CACHE_E4M3) scale[t] = e4m3_scale(__builtin_amdgcn_raw_buffer_load_b8(exps, lane & 15, 0, 0));
+  }
+  // first element of the lane's eight of instruction ks
+  static __device__ __forceinline__ int query_offset(int ks, int lane) {
+    return FORMAT == SMOE_CACHE_BF16 ? ks * 32 + (lane >> 4) * 8 : (ks >> 1) * 64 + (lane >> 4) * 16 + (ks & 1) * 8;
+  }
+  __device__ __forceinline__ bf16x8 frag(int t, int ks) const {
+    if constexpr (FORMAT == SMOE_CACHE_BF16) {
+      return __builtin_bit_cast(bf16x8, v[t][ks]);
+    } else {
+      const uint32_t a = v[t][ks >> 1][(ks & 1) * 2], b = v[t][ks >> 1][(ks & 1) * 2 + 1];
+      return __builtin_bit_cast(bf16x8, u32x4{widen<false>(a, scale[t]), widen<true>(a, scale[t]), widen<false>(b, scale[t]), widen<true>(b, scale[t])});
+    }
+  }
+};
+
+// Values: lane -> keys 4 (lane / 16) + 0..3 of both groups, columns D / 16 * (lane % 16) and on.  frag(j): column j of the lane's.
+template <int D, int FORMAT> struct Values {
+  static constexpr int COLS = D / 16, WORDS = COLS / 2;    // columns of a lane, 32-bit words of them as bf16
+  uint32_t v[8][WORDS];
+  // left: rows of the group within the length; the exponents behind them are masked, since a scale of what lies there could make a NaN of zero
+  __device__ __forceinline__ void load(int t, __amdgpu_buffer_rsrc_t rows, __amdgpu_buffer_rsrc_t exps, int lane, int left) {
+    const int g = lane >> 4;
+    if constexpr (FORMAT == SMOE_CACHE_BF16) {
+      const int at = g * 4 * D * 2 + (lane & 15) * COLS * 2;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        if constexpr (COLS == 8) {
+          const u32x4 x = load4(rows, at + i * D * 2);
+#pragma unroll
+          for (int w = 0; w < 4; ++w) v[4 * t + i][w] = x[w];
+        } else {
+          const u32x2 x = load2(rows, at + i * D * 2);
+          v[4 * t + i][0] = x[0];
+          v[4 * t + i][1] = x[1];
+        }
+      }
+    } else {
+      const int at = g * 4 * D + (lane & 15) * COLS;
+      const int mine = left - 4 * g;
+      const uint32_t e = load1(exps, g * 4) & (mine >= 4 ? ~0u : mine <= 0 ? 0u : (1u << (8 * mine)) - 1u);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const float scale = e4m3_scale((e >> (8 * i)) & 255u);
+        uint32_t codes[WORDS / 2];
+        if constexpr (COLS == 8) {
+          const u32x2 x = load2(rows, at + i * D);
+          codes[0] = x[0];
+          codes[1] = x[1];
+        } else {
+          codes[0] = load1(rows, at + i * D);
+        }
+#pragma unroll
+        for (int w = 0; w < WORDS / 2; ++w) {
+          v[4 * t + i][2 * w] = widen<false>(codes[w], scale);
+          v[4 * t + i][2 * w + 1] = widen<true>(codes[w], scale);
+        }
+      }
+    }
+  }
+  __device__ __forceinline__ bf16x8 frag(int j) const {
+    u32x4 r;
+#pragma unroll
+    for (int m = 0; m < 4; ++m) r[m] = __builtin_amdgcn_perm(v[2 * m + 1][j / 2], v[2 * m][j / 2], j % 2 ? 0x07060302u : 0x05040100u);
+    return __builtin_bit_cast(bf16x8, r);
+  }
+  // The same with zeros for the keys whose bit is not set.
+  __device__ __forceinline__ bf16x8 frag(int j, unsigned int keys) const {
+    u32x4 r = __builtin_bit_cast(u32x4, frag(j));
+#pragma unroll
+    for (int m = 0; m < 4; ++m) r[m] &= (keys >> (2 * m) & 1 ? 0xffffu : 0u) | (keys >> (2 * m + 1) & 1 ? 0xffff0000u : 0u);
+    return __builtin_bit_cast(bf16x8, r);
+  }
+  // is any of them infinite or NaN?
+  __device__ __forceinline__ bool odd() const {
+    bool found = false;
+#pragma unroll
+    for (int k = 0; k < 8; ++k)
+#pragma unroll
+      for (int w = 0; w < WORDS; ++w) found |= (v[k][w] & 0x7f80u) == 0x7f80u || (v[k][w] & 0x7f800000u) == 0x7f800000u;
+    return found;
+  }
+};
+
+// ------------------------------------------------------------------------------------------------ one piece
+template <int D, int FORMAT, int RT>
+__global__ void __launch_bounds__(64 * WAVES, RT == 1 ? 3 : 2)
+    cached_attention_kernel(const bf16_t *Q, smoe_cache c, smoe_places p, Dims d, bf16_t *O, float *LSE, float *ws) {
+  constexpr int KS = D / 32, COLS = D / 16, ROW = D + 4;     // padded: a wavefront's 16 rows start in 16 different banks
+  __shared__ __attribute__((aligned(16))) float s_acc[WAVES][RT * 16][ROW];
+  __shared__ float s_m[WAVES][RT * 16], s_l[WAVES][RT * 16];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+  const int col = lane & 15, g = lane >> 4;
+  Place at;
+  if (!find_piece<false>(p.lens, p.sequences, d, (int)blockIdx.x, lane, at)) return;   // the grid is an upper bound
+  const int unit = at.local / at.n, piece = at.local - unit * at.n;
+  const int tile = unit / c.h, hh = unit - tile * c.h, b = at.b, len = at.len;
+  const int all_steps = steps_of(len), long_ = (all_steps + at.n - 1) / at.n;
+  const int step0 = piece * long_, step1 = min(step0 + long_, all_steps);
+
+  // the lane's query of each 16, and the first position it does not see
+  const int row0 = tile * RT * 16, rows = min(RT * 16, d.R - row0);
+  int seen[RT], token[RT];
+  bf16x8 q[RT][KS];
+#pragma unroll
+  for (int t = 0; t < RT; ++t) {
+    const int r = row0 + min(t * 16 + col, rows - 1);
+    token[t] = r / d.G;
+    seen[t] = len - d.N + token[t] + 1;
+    const bf16_t *src = Q + (((size_t)b * d.R + r) * c.h + hh) * D;
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) q[t][ks] = *reinterpret_cast<const bf16x8 *>(src + Keys<D, FORMAT>::query_offset(ks, lane));
+  }
+  const int token0 = row0 / d.G, token1 = (row0 + rows - 1) / d.G;
+  const int all_see = len - d.N + token0 + 1;               // every query of the tile sees the keys before this one
+
+  constexpr float LOG2E = 1.4426950408889634f;
+  const float scale = LOG2E / sqrtf((float)D);
+  f32x4 acc[RT][COLS];
+  float m[RT], l[RT];
+#pragma unroll
+  for (int t = 0; t < RT; ++t) {
+    m[t] = -INFINITY;
+    l[t] = 0.f;
+#pragma unroll
+    for (int j = 0; j < COLS; ++j) acc[t][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+  }
+
+  constexpr int BYTES = FORMAT == SMOE_CACHE_BF16 ? D * 2 : D;
+  const int32_t *table = p.block_table + (size_t)b * p.width;
+  auto page_of = [&](int key) { return key < len ? __builtin_amdgcn_readfirstlane(table[key >> d.shift]) : -1; };
+  int next0 = -1, next1 = -1;
+  if (step0 + wave < step1) {
+    next0 = page_of((step0 + wave) * STEP);
+    next1 = page_of((step0 + wave) * STEP + 16);
+  }
+#pragma unroll 1
+  for (int s = step0 + wave; s < step1; s += WAVES) {
+    const int key0 = s * STEP;
+    Keys<D, FORMAT> k;
+    Values<D, FORMAT> v;
+    bool whole = key0 + STEP <= all_see;
+    unsigned int there = 0;
+    int left[2];
+    // Rows past the length and pages that do not exist lie outside the windows and read as zeros: no product of a weight of zero with
+    // whatever the cache holds there.
+    __amdgpu_buffer_rsrc_t kr[2], vr[2], ke[2], ve[2];
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      const int key = key0 + 16 * t, id = t ? next1 : next0;
+      const bool exists = (unsigned)id < (unsigned)c.pages;
+      there |= exists ? 1u << t : 0u;
+      whole = whole && exists;
+      const size_t row = ((size_t)(exists ? id : 0) * c.h + hh) * c.page + (key & (c.page - 1));
+      left[t] = exists ? min(max(len - key, 0), 16) : 0;
+      kr[t] = window((const char *)c.K + row * BYTES, left[t] * BYTES);
+      vr[t] = window((const char *)c.V + row * BYTES, left[t] * BYTES);
+      if constexpr (FORMAT == SMOE_CACHE_E4M3) {
+        ke[t] = window(c.K_exp + row, left[t]);
+        ve[t] = window(c.V_exp + row, left[t] ? 16 : 0);
+      }
+    }
+#pragma unroll
+    for (int t = 0; t < 2; ++t) k.load(t, kr[t], ke[t], lane);
+#pragma unroll
+    for (int t = 0; t < 2; ++t) v.load(t, vr[t], ve[t], lane, left[t]);
+    if (s + WAVES < step1) {
+      next0 = page_of((s + WAVES) * STEP);
+      next1 = page_of((s + WAVES) * STEP + 16);
+    }
+    bf16x8 pb[RT];
+#pragma unroll
+    for (int t = 0; t < RT; ++t) {
+      f32x4 sc[2];
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        sc[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) sc[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k.frag(i, ks), q[t][ks], sc[i], 0, 0, 0);
+      }
+      if (!whole) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            if (key0 + 16 * i + 4 * g + e >= seen[t] || !(there >> i & 1)) sc[i][e] = -INFINITY;
+      }
+      float mx = fmaxf(fmaxf(fmaxf(sc[0][0], sc[0][1]), fmaxf(sc[0][2], sc[0][3])), fmaxf(fmaxf(sc[1][0], sc[1][1]), fmaxf(sc[1][2], sc[1][3])));
+      mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
+      mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
+      const float m_new = fmaxf(m[t], mx), base = m_new == -INFINITY ? 0.f : m_new;   // no inf - inf while nothing was seen
+      const float alpha = __builtin_amdgcn_exp2f((m[t] - base) * scale);
+      m[t] = m_new;
+      float sum = 0.f;
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const float w = __builtin_amdgcn_exp2f((sc[i][e] - base) * scale);   // the difference first: huge scores cancel exactly
+          sum += w;
+          pb[t][4 * i + e] = (bf16_t)w;
+        }
+      l[t] = l[t] * alpha + sum;
+      if (__any(alpha != 1.f)) {
+#pragma unroll
+        for (int j = 0; j < COLS; ++j)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) acc[t][j][e] *= alpha;
+      }
+    }
+    if (!whole && d.N > 1 && __any(v.odd())) {
+      // Infinite or NaN values at positions that some queries see and others do not: a weight of zero would not keep them out, so each
+      // token's queries take their own product, over the values that the token sees.
+#pragma unroll 1
+      for (int n = token0; n <= token1; ++n) {
+        const int sees = len - d.N + n + 1;
+        unsigned int keys = 0;
+#pragma unroll
+        for (int kk = 0; kk < 8; ++kk) keys |= key0 + 16 * (kk >> 2) + 4 * g + (kk & 3) < sees ? 1u << kk : 0u;
+#pragma unroll
+        for (int j = 0; j < COLS; ++j)
+#pragma unroll
+          for (int t = 0; t < RT; ++t) {
+            const f32x4 with = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v.frag(j, keys), pb[t], acc[t][j], 0, 0, 0);
+            if (token[t] == n) acc[t][j] = with;
+          }
+      }
+    } else {
+#pragma unroll
+      for (int j = 0; j < COLS; ++j) {
+        const bf16x8 f = v.frag(j);
+#pragma unroll
+        for (int t = 0; t < RT; ++t) acc[t][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f, pb[t], acc[t][j], 0, 0, 0);
+      }
+    }
+  }
+
+  // The wavefronts' parts meet in LDS.  A lane holds columns 4 COLS g + COLS e + j of its query, j and e running.
+#pragma unroll
+  for (int t = 0; t < RT; ++t) {
+    float sum = l[t];
+    sum += __shfl_xor(sum, 16, 64);
+    sum += __shfl_xor(sum, 32, 64);
+    if (t * 16 + col < rows) {
+      float *dst = s_acc[wave][t * 16 + col] + 4 * COLS * g;
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+#pragma unroll
+        for (int j = 0; j < COLS; j += 4) *reinterpret_cast<f32x4 *>(dst + e * COLS + j) = f32x4{acc[t][j][e], acc[t][j + 1][e], acc[t][j + 2][e], acc[t][j + 3][e]};
+      if (g == 0) {
+        s_m[wave][t * 16 + col] = m[t];
+        s_l[wave][t * 16 + col] = sum;
+      }
+    }
+  }
+  __syncthreads();
+  float *out = ws + (size_t)(at.slot + at.local) * slot_floats(d.rows, D);
+  for (int i = threadIdx.x; i < rows * (D / 4); i += 64 * WAVES) {
+    const int r = i / (D / 4), x = (i - r * (D / 4)) * 4;
+    float top = s_m[0][r];
+#pragma unroll
+    for (int w = 1; w < WAVES; ++w) top = fmaxf(top, s_m[w][r]);
+    const float base = top == -INFINITY ? 0.f : top;
+    f32x4 sum = f32x4{0.f, 0.f, 0.f, 0.f};
+    float total = 0.f;
+#pragma unroll
+    for (int w = 0; w < WAVES; ++w) {
+      const float f = __builtin_amdgcn_exp2f((s_m[w][r] - base) * scale);
+      total = fmaf(s_l[w][r], f, total);
+      const f32x4 y = *reinterpret_cast<const f32x4 *>(&s_acc[w][r][x]);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) sum[e] = fmaf(y[e], f, sum[e]);
+    }
+    if (at.n == 1) {
+      const float inv = total == 0.f ? 0.f : 1.f / total;
+      typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+      bf16x4 o;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) o[e] = (bf16_t)(sum[e] * inv);
+      const size_t row = ((size_t)b * d.R + row0 + r) * c.h + hh;
+      *reinterpret_cast<bf16x4 *>(O + row * D + x) = o;
+      if (x == 0) LSE[row] = total == 0.f ? -INFINITY : fmaf(top, scale, __builtin_amdgcn_logf(total)) * 0.6931471805599453f;
+    } else {
+      *reinterpret_cast<f32x4 *>(out + (size_t)r * D + x) = sum;
+      if (x == 0) {
+        out[(size_t)d.rows * D + r] = top;
+        out[(size_t)d.rows * (D + 1) + r] = total;
+      }
+    }
   }
 }
 
-// One block of four wavefronts for each query row and head.  A wavefront takes every fourth 64 keys, one a lane; its lanes then
-// hold d / 64 elements of the output each.
-template <int D, int FORMAT>
-__global__ void __launch_bounds__(256) cached_attention_kernel(const bf16_t *Q, smoe_cache c, smoe_places p, Dims dim, bf16_t *O, float *LSE) {
-  __shared__ float q[D], part[4][D], top[4], sum[4];
-  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, R = dim.N * dim.G;
-  const size_t unit = blockIdx.x;              // ((b, n, g), head)
-  const int hh = (int)(unit % c.h);
-  const int b = (int)(unit / c.h / R), r = (int)(unit / c.h % R);
-  const long long cap = (long long)p.width * c.page;
-  const int len = (int)max(0ll, min((long long)p.lens[b], cap)), seen = len - dim.N + r / dim.G + 1;
-  for (int i = threadIdx.x; i < D; i += 256) q[i] = (float)Q[unit * D + i];
-  __syncthreads();
-  constexpr int PER = D / 64;
-  float m = -INFINITY, l = 0.f, acc[PER] = {};
-  for (int k0 = wave * 64; k0 < seen; k0 += 256) {
-    const int key = k0 + lane;
-    const int id = key < seen ? find_page(p, c.pages, dim.shift, b, key) : -1;
-    const size_t row = ((size_t)id * c.h + hh) * c.page + (key & (c.page - 1));
-    float s = -INFINITY;
-    if (id >= 0) {
-      s = 0.f;
-      for (int e = 0; e < D; e += 8) {
-        float y[8];
-        stored8<FORMAT>(c.K, c.K_exp, row, D, e, y);
+// ------------------------------------------------------------------------------------------------ the join
+// A block for each row of a cut unit: eight wavefronts' worth of lanes take its pieces in turn, D / 4 lanes a piece, and the groups' sums
+// meet in LDS in a fixed order.
+constexpr int JOIN_THREADS = 512;
+template <int D> __global__ void __launch_bounds__(JOIN_THREADS) cached_attention_join_kernel(smoe_places p, Dims d, int h, const float *ws, bf16_t *O, float *LSE) {
+  constexpr int LANES = D / 4, GROUPS = JOIN_THREADS / LANES;
+  __shared__ __attribute__((aligned(16))) float s_acc[GROUPS][D + 4];
+  __shared__ float s_m[GROUPS], s_l[GROUPS];
+  const int lane = threadIdx.x & 63;
+  Place at;
+  if (!find_piece<true>(p.lens, p.sequences, d, (int)blockIdx.x, lane, at)) return;
+  const int unit = at.local, tile = unit / h, hh = unit - tile * h, r = blockIdx.y;
+  if (tile * d.rows + r >= d.R) return;
+  const float scale = 1.4426950408889634f / sqrtf((float)D);
+  const size_t stride = slot_floats(d.rows, D);
+  const float *base = ws + (size_t)(at.slot + unit * at.n) * stride;
+  const int group = threadIdx.x / LANES, x = (threadIdx.x % LANES) * 4;
+  f32x4 acc = f32x4{0.f, 0.f, 0.f, 0.f};
+  float m = -INFINITY, l = 0.f;
+#pragma unroll 4
+  for (int i = group; i < at.n; i += GROUPS) {
+    const float *src = base + (size_t)i * stride;
+    const float pm = src[(size_t)d.rows * D + r], pl = src[(size_t)d.rows * (D + 1) + r];
+    const f32x4 y = *reinterpret_cast<const f32x4 *>(src + (size_t)r * D + x);
+    const float top = fmaxf(m, pm), safe = top == -INFINITY ? 0.f : top;
+    const float old = __builtin_amdgcn_exp2f((m - safe) * scale), now = __builtin_amdgcn_exp2f((pm - safe) * scale);
+    m = top;
+    l = fmaf(l, old, pl * now);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) s = fmaf(q[e + i], y[i], s);
-      }
-      s *= rsqrtf((float)D);
-    }
-    float mx = s;
-    for (int x = 32; x > 0; x >>= 1) mx = fmaxf(mx, __shfl_xor(mx, x, 64));
-    const float m_new = fmaxf(m, mx), base = m_new == -INFINITY ? 0.f : m_new;
-    const float w = expf(s - base), alpha = expf(m - base);
-    l = l * alpha + w;
-    m = m_new;
-#pragma unroll
-    for (int i = 0; i < PER; ++i) acc[i] *= alpha;
-    for (int kk = 0; kk < 64; ++kk) {
-      const int idk = __shfl(id, kk, 64);
-      const float wk = __shfl(w, kk, 64);
-      if (idk < 0) continue;
-      const size_t rk = ((size_t)idk * c.h + hh) * c.page + ((k0 + kk) & (c.page - 1));
-      float y[8];
-      stored8<FORMAT>(c.V, c.V_exp, rk, D, lane * PER & ~7, y);
-#pragma unroll
-      for (int i = 0; i < PER; ++i) {
-        float v = 0.f;
-#pragma unroll
-        for (int t = 0; t < 8; ++t) v = ((lane * PER + i) & 7) == t ? y[t] : v;
-        acc[i] = fmaf(wk, v, acc[i]);
-      }
-    }
+    for (int e = 0; e < 4; ++e) acc[e] = fmaf(acc[e], old, y[e] * now);
   }
-  for (int x = 32; x > 0; x >>= 1) l += __shfl_xor(l, x, 64);
-  if (lane == 0) { top[wave] = m; sum[wave] = l; }
-#pragma unroll
-  for (int i = 0; i < PER; ++i) part[wave][lane * PER + i] = acc[i];
-  __syncthreads();
-  const float M = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])), base = M == -INFINITY ? 0.f : M;
-  float total = 0.f, scale[4];
-  for (int i = 0; i < 4; ++i) { scale[i] = expf(top[i] - base); total += sum[i] * scale[i]; }
-  for (int i = threadIdx.x; i < D; i += 256) {
-    float o = 0.f;
-    for (int k = 0; k < 4; ++k) o += part[k][i] * scale[k];
-    O[unit * D + i] = (bf16_t)(total == 0.f ? 0.f : o / total);
+  *reinterpret_cast<f32x4 *>(&s_acc[group][x]) = acc;
+  if (x == 0) {
+    s_m[group] = m;
+    s_l[group] = l;
   }
-  if (threadIdx.x == 0) LSE[unit] = total == 0.f ? -INFINITY : M + logf(total);
+  __syncthreads();
+  if (threadIdx.x >= LANES) return;
+  float top = s_m[0];
+#pragma unroll
+  for (int w = 1; w < GROUPS; ++w) top = fmaxf(top, s_m[w]);
+  const float safe = top == -INFINITY ? 0.f : top;
+  f32x4 sum = f32x4{0.f, 0.f, 0.f, 0.f};
+  float total = 0.f;
+#pragma unroll
+  for (int w = 0; w < GROUPS; ++w) {
+    const float f = __builtin_amdgcn_exp2f((s_m[w] - safe) * scale);
+    total = fmaf(s_l[w], f, total);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) sum[e] = fmaf(s_acc[w][x + e], f, sum[e]);
+  }
+  const float inv = total == 0.f ? 0.f : 1.f / total;
+  typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+  bf16x4 o;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) o[e] = (bf16_t)(sum[e] * inv);
+  const size_t row = ((size_t)at.b * d.R + tile * d.rows + r) * h + hh;
+  *reinterpret_cast<bf16x4 *>(O + row * D + x) = o;
+  if (x == 0) LSE[row] = total == 0.f ? -INFINITY : fmaf(top, scale, __builtin_amdgcn_logf(total)) * 0.6931471805599453f;
 }
+
+// Query rows that share a read of the cache: 16, or 32 where there are more.
+int row_tiles(int R) { return R > 16 ? 2 : 1; }
 
 }  // namespace
 
+constexpr size_t MAX_SLOTS = 2 * TARGET;
 size_t cached_attention_workspace_bytes(int N, int G, int d_head) {
-  (void)N; (void)G; (void)d_head;
-  return 256;
+  const long long R = (long long)N * G;
+  return MAX_SLOTS * slot_floats((int)std::min<long long>(R, 16 * row_tiles((int)std::min<long long>(R, 1 << 20))), d_head) * sizeof(float);
 }
 
 int launch_cached_attention(hipStream_t s, const void *Q, int N, int G, const smoe_cache &c, const smoe_places &p, void *O, float *LSE, void *ws) {
-  (void)ws;
-  const Dims dim{N, G, __builtin_ctz((unsigned int)c.page)};
-  const unsigned int blocks = (unsigned int)((size_t)p.sequences * N * G * c.h);
-  auto go = [&](auto kernel) { kernel<<<blocks, 256, 0, s>>>((const bf16_t *)Q, c, p, dim, (bf16_t *)O, LSE); };
-  if (c.d_head == 128) c.format == SMOE_CACHE_BF16 ? go(cached_attention_kernel<128, SMOE_CACHE_BF16>) : go(cached_attention_kernel<128, SMOE_CACHE_E4M3>);
-  else c.format == SMOE_CACHE_BF16 ? go(cached_attention_kernel<64, SMOE_CACHE_BF16>) : go(cached_attention_kernel<64, SMOE_CACHE_E4M3>);
-  SMOE_LAUNCH_CHECK();
-  return SMOE_OK;
+  Dims d;
+  d.N = N;
+  d.G = G;
+  d.R = N * G;
+  const int rt = row_tiles(d.R);
+  d.tiles = ceil_div(d.R, 16 * rt);
+  d.rows = std::min(d.R, 16 * rt);
+  d.shift = __builtin_ctz((unsigned int)c.page);
+  d.cap = p.width * c.page;
+  const long long units = (long long)d.tiles * c.h, all = units * p.sequences;
+  if (all > 0x7fffffffLL / 256 - 2 * TARGET) return SMOE_ERR_UNSUPPORTED;    // one-dimensional grids
+  d.units = (int)units;
+  auto go = [&](auto kernel, auto join) {
+    kernel<<<(unsigned int)all + TARGET, 64 * WAVES, 0, s>>>((const bf16_t *)Q, c, p, d, (bf16_t *)O, LSE, (float *)ws);
+    if (hipGetLastError() != hipSuccess) return SMOE_ERR_HIP;
+    if (d.cap <= MIN_STEPS * STEP) return SMOE_OK;                           // no sequence can be cut
+    join<<<dim3((unsigned int)std::min<long long>(all, TARGET), d.rows), JOIN_THREADS, 0, s>>>(p, d, c.h, (const float *)ws, (bf16_t *)O, LSE);
+    return hipGetLastError() == hipSuccess ? SMOE_OK : SMOE_ERR_HIP;
+  };
+  auto by_rows = [&](auto d_c, auto f_c) {
+    constexpr int D = decltype(d_c)::value, F = decltype(f_c)::value;
+    return rt == 1 ? go(cached_attention_kernel<D, F, 1>, cached_attention_join_kernel<D>) : go(cached_attention_kernel<D, F, 2>, cached_attention_join_kernel<D>);
+  };
+  auto by_format = [&](auto d_c) {
+    return c.format == SMOE_CACHE_BF16 ? by_rows(d_c, std::integral_constant<int, SMOE_CACHE_BF16>{}) : by_rows(d_c, std::integral_constant<int, SMOE_CACHE_E4M3>{});
+  };
+  return c.d_head == 128 ? by_format(std::integral_constant<int, 128>{}) : by_format(std::integral_constant<int, 64>{});
 }

@@ -328,7 +328,7 @@ def _case(smoe, lens, page, h, d, quantised, seed, width=None, behind=10 ** 6, s
         t.fill_(0x7F if quantised else float("nan"))
     for t in (cache.K_exp, cache.V_exp):
         if t is not None:
-            t.fill_(254)
+            t.fill_(255)
     seqs = torch.tensor([b for b, n in enumerate(lens) for _ in range(n)], dtype=torch.int32)
     pos = torch.tensor([p for n in lens for p in range(n)], dtype=torch.int32)
     K, V = _normal((len(seqs), h, d), seed + 1, std=std), _normal((len(seqs), h, d), seed + 2)
