@@ -41,6 +41,7 @@ struct Dims {
 __device__ __forceinline__ int length_of(const int32_t *lens, int b, int cap) { return min(max(lens[b], 0), cap); }
 __device__ __forceinline__ int steps_of(int len) { return max((len + STEP - 1) / STEP, 1); }
 
+__device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
 template <int CTRL, int ROWS> __device__ __forceinline__ int shifted(int v) { return __builtin_amdgcn_update_dpp(0, v, CTRL, ROWS, 0xf, false); }
 // inclusive sums over the lanes
 __device__ __forceinline__ int scan_add(int v) {
@@ -134,17 +135,45 @@ template <bool UPPER> __device__ __forceinline__ uint32_t widen(uint32_t codes, 
   return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(codes, scale, UPPER));
 }
 
-// Keys: lane -> key (lane % 16) of each of the two groups of 16, D / 4 elements of its row.  Which elements go with which instruction is
-// free as long as the queries' fragments follow (query_offset).  A group of 16 keys lies on one page.
+// The same offset, but what is added to it stays an immediate of the loads: hoisted out of the loop, every sum would take a register.
+__device__ __forceinline__ int here(int at) {
+  __asm__ volatile("" : "+v"(at));
+  return at;
+}
+// the largest over the lanes of a query (lane % 16)
+__device__ __forceinline__ float max_of_query(float x) {
+  unsigned int b = __float_as_uint(x);
+  u32x2 r = __builtin_amdgcn_permlane16_swap(b, b, false, false);
+  unsigned int r0 = r[0], r1 = r[1];
+  x = fmaxf(__uint_as_float(r0), __uint_as_float(r1));
+  b = __float_as_uint(x);
+  r = __builtin_amdgcn_permlane32_swap(b, b, false, false);
+  r0 = r[0], r1 = r[1];
+  return fmaxf(__uint_as_float(r0), __uint_as_float(r1));
+}
+
+// A group of 16 keys, which lies on one page: windows over its rows and exponents (wave-uniform).  Rows past the length and pages that do not
+// exist lie outside and read as zeros: no product of a weight of zero with whatever the cache holds there.
+struct Group {
+  const char *K, *V;
+  const uint8_t *K_exp, *V_exp;
+  int left;              // rows within the length
+  bool exists;
+};
+
+// Keys: lane -> key (lane % 16) of each of the two groups, D / 4 elements of its row.  Which elements go with which instruction is
+// free as long as the queries' fragments follow (query_offset).
 template <int D, int FORMAT> struct Keys {
-  static constexpr int LOADS = FORMAT == SMOE_CACHE_BF16 ? D / 32 : D / 64;
+  static constexpr int BYTES = FORMAT == SMOE_CACHE_BF16 ? D * 2 : D, LOADS = BYTES / 64;
   u32x4 v[2][LOADS];
-  float scale[2];
-  __device__ __forceinline__ void load(int t, __amdgpu_buffer_rsrc_t rows, __amdgpu_buffer_rsrc_t exps, int lane) {
-    constexpr int BYTES = FORMAT == SMOE_CACHE_BF16 ? D * 2 : D;
+  uint32_t e[2];
+  static __device__ __forceinline__ int lane_offset(int lane) { return (lane & 15) * BYTES + (lane >> 4) * 16; }
+  __device__ __forceinline__ void load(int t, const Group &p, int at, int lane) {
+    const __amdgpu_buffer_rsrc_t rows = window(p.K, p.left * BYTES);
+    at = here(at);
 #pragma unroll
-    for (int i = 0; i < LOADS; ++i) v[t][i] = load4(rows, (lane & 15) * BYTES + i * 64 + (lane >> 4) * 16);
-    if constexpr (FORMAT == SMOE_CACHE_E4M3) scale[t] = e4m3_scale(__builtin_amdgcn_raw_buffer_load_b8(exps, lane & 15, 0, 0));
+    for (int i = 0; i < LOADS; ++i) v[t][i] = load4(rows, at + i * 64);
+    if constexpr (FORMAT == SMOE_CACHE_E4M3) e[t] = __builtin_amdgcn_raw_buffer_load_b8(window(p.K_exp, p.left), lane & 15, 0, 0);
   }
   // first element of the lane's eight of instruction ks
   static __device__ __forceinline__ int query_offset(int ks, int lane) {
@@ -155,66 +184,77 @@ template <int D, int FORMAT> struct Keys {
       return __builtin_bit_cast(bf16x8, v[t][ks]);
     } else {
       const uint32_t a = v[t][ks >> 1][(ks & 1) * 2], b = v[t][ks >> 1][(ks & 1) * 2 + 1];
-      return __builtin_bit_cast(bf16x8, u32x4{widen<false>(a, scale[t]), widen<true>(a, scale[t]), widen<false>(b, scale[t]), widen<true>(b, scale[t])});
+      const float scale = e4m3_scale(e[t]);
+      return __builtin_bit_cast(bf16x8, u32x4{widen<false>(a, scale), widen<true>(a, scale), widen<false>(b, scale), widen<true>(b, scale)});
     }
   }
 };
 
-// Values: lane -> keys 4 (lane / 16) + 0..3 of both groups, columns D / 16 * (lane % 16) and on.  frag(j): column j of the lane's.
+// Values: lane -> keys 4 (lane / 16) + 0..3 of both groups, columns D / 16 * (lane % 16) and on.
 template <int D, int FORMAT> struct Values {
   static constexpr int COLS = D / 16, WORDS = COLS / 2;    // columns of a lane, 32-bit words of them as bf16
-  uint32_t v[8][WORDS];
-  // left: rows of the group within the length; the exponents behind them are masked, since a scale of what lies there could make a NaN of zero
-  __device__ __forceinline__ void load(int t, __amdgpu_buffer_rsrc_t rows, __amdgpu_buffer_rsrc_t exps, int lane, int left) {
-    const int g = lane >> 4;
-    if constexpr (FORMAT == SMOE_CACHE_BF16) {
-      const int at = g * 4 * D * 2 + (lane & 15) * COLS * 2;
+  static constexpr int HELD = FORMAT == SMOE_CACHE_BF16 ? WORDS : WORDS / 2;
+  static constexpr int BYTES = FORMAT == SMOE_CACHE_BF16 ? D * 2 : D;
+  uint32_t v[8][HELD];
+  uint32_t e[2];
+  static __device__ __forceinline__ int lane_offset(int lane) { return (lane >> 4) * 4 * BYTES + (lane & 15) * HELD * 4; }
+  __device__ __forceinline__ void load(int t, const Group &p, int at, int lane) {
+    const __amdgpu_buffer_rsrc_t rows = window(p.V, p.left * BYTES);
+    at = here(at);
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        if constexpr (COLS == 8) {
-          const u32x4 x = load4(rows, at + i * D * 2);
+    for (int i = 0; i < 4; ++i) {
+      if constexpr (HELD == 4) {
+        const u32x4 x = load4(rows, at + i * BYTES);
 #pragma unroll
-          for (int w = 0; w < 4; ++w) v[4 * t + i][w] = x[w];
-        } else {
-          const u32x2 x = load2(rows, at + i * D * 2);
-          v[4 * t + i][0] = x[0];
-          v[4 * t + i][1] = x[1];
-        }
+        for (int w = 0; w < 4; ++w) v[4 * t + i][w] = x[w];
+      } else if constexpr (HELD == 2) {
+        const u32x2 x = load2(rows, at + i * BYTES);
+        v[4 * t + i][0] = x[0];
+        v[4 * t + i][1] = x[1];
+      } else {
+        v[4 * t + i][0] = load1(rows, at + i * BYTES);
       }
-    } else {
-      const int at = g * 4 * D + (lane & 15) * COLS;
-      const int mine = left - 4 * g;
-      const uint32_t e = load1(exps, g * 4) & (mine >= 4 ? ~0u : mine <= 0 ? 0u : (1u << (8 * mine)) - 1u);
+    }
+    if constexpr (FORMAT == SMOE_CACHE_E4M3) e[t] = load1(window(p.V_exp, p.left ? 16 : 0), (lane >> 4) * 4);
+  }
+};
+// The same as bf16.
+template <int D> struct Columns {
+  static constexpr int WORDS = D / 32;
+  uint32_t v[8][WORDS];
+  template <int FORMAT> __device__ __forceinline__ Columns(const Values<D, FORMAT> &x, const int (&left)[2], int g) {
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const float scale = e4m3_scale((e >> (8 * i)) & 255u);
-        uint32_t codes[WORDS / 2];
-        if constexpr (COLS == 8) {
-          const u32x2 x = load2(rows, at + i * D);
-          codes[0] = x[0];
-          codes[1] = x[1];
-        } else {
-          codes[0] = load1(rows, at + i * D);
-        }
+    for (int k = 0; k < 8; ++k) {
+      if constexpr (FORMAT == SMOE_CACHE_BF16) {
+#pragma unroll
+        for (int w = 0; w < WORDS; ++w) v[k][w] = x.v[k][w];
+      } else {
+        // the exponents behind the length are masked: a scale of what lies there could make a NaN of zero
+        const float scale = 4 * g + (k & 3) < left[k >> 2] ? e4m3_scale((x.e[k >> 2] >> (8 * (k & 3))) & 255u) : 0.f;
 #pragma unroll
         for (int w = 0; w < WORDS / 2; ++w) {
-          v[4 * t + i][2 * w] = widen<false>(codes[w], scale);
-          v[4 * t + i][2 * w + 1] = widen<true>(codes[w], scale);
+          v[k][2 * w] = widen<false>(x.v[k][w], scale);
+          v[k][2 * w + 1] = widen<true>(x.v[k][w], scale);
         }
       }
     }
   }
+  // column j of the lane's, its eight keys
   __device__ __forceinline__ bf16x8 frag(int j) const {
     u32x4 r;
 #pragma unroll
     for (int m = 0; m < 4; ++m) r[m] = __builtin_amdgcn_perm(v[2 * m + 1][j / 2], v[2 * m][j / 2], j % 2 ? 0x07060302u : 0x05040100u);
     return __builtin_bit_cast(bf16x8, r);
   }
-  // The same with zeros for the keys whose bit is not set.
-  __device__ __forceinline__ bf16x8 frag(int j, unsigned int keys) const {
-    u32x4 r = __builtin_bit_cast(u32x4, frag(j));
+  // The same with zeros for the keys whose bit is not set.  (`pick` is the permutation of even columns: an opaque value, so that a loop
+  // around this does not hold every column's operand in registers.)
+  __device__ __forceinline__ bf16x8 frag(int j, unsigned int keys, unsigned int pick) const {
+    u32x4 r;
 #pragma unroll
-    for (int m = 0; m < 4; ++m) r[m] &= (keys >> (2 * m) & 1 ? 0xffffu : 0u) | (keys >> (2 * m + 1) & 1 ? 0xffff0000u : 0u);
+    for (int m = 0; m < 4; ++m) {
+      r[m] = __builtin_amdgcn_perm(v[2 * m + 1][j / 2], v[2 * m][j / 2], j % 2 ? pick + 0x02020202u : pick);
+      r[m] &= (keys >> (2 * m) & 1 ? 0xffffu : 0u) | (keys >> (2 * m + 1) & 1 ? 0xffff0000u : 0u);
+    }
     return __builtin_bit_cast(bf16x8, r);
   }
   // is any of them infinite or NaN?
@@ -229,8 +269,9 @@ template <int D, int FORMAT> struct Values {
 };
 
 // ------------------------------------------------------------------------------------------------ one piece
-template <int D, int FORMAT, int RT>
-__global__ void __launch_bounds__(64 * WAVES, RT == 1 ? 3 : 2)
+// ONE: a single new token a sequence, so that every position within the length is seen by every query.
+template <int D, int FORMAT, int RT, bool ONE>
+__global__ void __launch_bounds__(64 * WAVES, RT == 1 && ONE ? 3 : 2)
     cached_attention_kernel(const bf16_t *Q, smoe_cache c, smoe_places p, Dims d, bf16_t *O, float *LSE, float *ws) {
   constexpr int KS = D / 32, COLS = D / 16, ROW = D + 4;     // padded: a wavefront's 16 rows start in 16 different banks
   __shared__ __attribute__((aligned(16))) float s_acc[WAVES][RT * 16][ROW];
@@ -239,14 +280,19 @@ __global__ void __launch_bounds__(64 * WAVES, RT == 1 ? 3 : 2)
   const int col = lane & 15, g = lane >> 4;
   Place at;
   if (!find_piece<false>(p.lens, p.sequences, d, (int)blockIdx.x, lane, at)) return;   // the grid is an upper bound
-  const int unit = at.local / at.n, piece = at.local - unit * at.n;
-  const int tile = unit / c.h, hh = unit - tile * c.h, b = at.b, len = at.len;
-  const int all_steps = steps_of(len), long_ = (all_steps + at.n - 1) / at.n;
+  // everything of the piece is wave-uniform, and is told so: the windows below live in scalar registers
+  const int pieces = uniform(at.n), len = uniform(at.len), b = uniform(at.b);
+  const int unit = uniform(at.local / pieces), piece = uniform(at.local) - unit * pieces;
+  const int tile = uniform(unit / c.h), hh = unit - tile * c.h;
+  const int all_steps = steps_of(len), long_ = uniform((all_steps + pieces - 1) / pieces);
   const int step0 = piece * long_, step1 = min(step0 + long_, all_steps);
 
   // the lane's query of each 16, and the first position it does not see
   const int row0 = tile * RT * 16, rows = min(RT * 16, d.R - row0);
   int seen[RT], token[RT];
+  // The queries' fragments: in registers, or, two tiles of them, in LDS (held in registers they spilled, and a reload in the loop waits
+  // for every request under way: two sequences of 90001 and 131072 positions in e4m3 133 us).
+  __shared__ __attribute__((aligned(16))) bf16x8 s_q[RT > 1 ? RT * KS : 1][64];
   bf16x8 q[RT][KS];
 #pragma unroll
   for (int t = 0; t < RT; ++t) {
@@ -255,8 +301,12 @@ __global__ void __launch_bounds__(64 * WAVES, RT == 1 ? 3 : 2)
     seen[t] = len - d.N + token[t] + 1;
     const bf16_t *src = Q + (((size_t)b * d.R + r) * c.h + hh) * D;
 #pragma unroll
-    for (int ks = 0; ks < KS; ++ks) q[t][ks] = *reinterpret_cast<const bf16x8 *>(src + Keys<D, FORMAT>::query_offset(ks, lane));
+    for (int ks = 0; ks < KS; ++ks) {
+      if (RT == 1) q[t][ks] = *reinterpret_cast<const bf16x8 *>(src + Keys<D, FORMAT>::query_offset(ks, lane));
+      else if ((t * KS + ks) % WAVES == wave) s_q[t * KS + ks][lane] = *reinterpret_cast<const bf16x8 *>(src + Keys<D, FORMAT>::query_offset(ks, lane));
+    }
   }
+  if (RT > 1) __syncthreads();
   const int token0 = row0 / d.G, token1 = (row0 + rows - 1) / d.G;
   const int all_see = len - d.N + token0 + 1;               // every query of the tile sees the keys before this one
 
@@ -274,66 +324,70 @@ __global__ void __launch_bounds__(64 * WAVES, RT == 1 ? 3 : 2)
 
   constexpr int BYTES = FORMAT == SMOE_CACHE_BF16 ? D * 2 : D;
   const int32_t *table = p.block_table + (size_t)b * p.width;
-  auto page_of = [&](int key) { return key < len ? __builtin_amdgcn_readfirstlane(table[key >> d.shift]) : -1; };
-  int next0 = -1, next1 = -1;
-  if (step0 + wave < step1) {
-    next0 = page_of((step0 + wave) * STEP);
-    next1 = page_of((step0 + wave) * STEP + 16);
-  }
-#pragma unroll 1
-  for (int s = step0 + wave; s < step1; s += WAVES) {
-    const int key0 = s * STEP;
-    Keys<D, FORMAT> k;
-    Values<D, FORMAT> v;
-    bool whole = key0 + STEP <= all_see;
-    unsigned int there = 0;
-    int left[2];
-    // Rows past the length and pages that do not exist lie outside the windows and read as zeros: no product of a weight of zero with
-    // whatever the cache holds there.
-    __amdgpu_buffer_rsrc_t kr[2], vr[2], ke[2], ve[2];
+  // The wavefront's next 64 page numbers, one a lane: two for each of its steps from the `from`-th on.
+  int ids = -1;
+  auto fetch_pages = [&](int from) {
+    const int step = step0 + wave + (from + (lane >> 1)) * WAVES, key = step * STEP + 16 * (lane & 1);
+    ids = step < step1 && key < len ? table[key >> d.shift] : -1;
+    ids = here(ids);      // waited for at this place, not where a number is used in the loop
+  };
+  auto group_of = [&](int step, int t, int id) {
+    const int key = step * STEP + 16 * t;
+    Group x;
+    x.exists = (unsigned)id < (unsigned)c.pages;
+    const size_t row = ((size_t)(x.exists ? id : 0) * c.h + hh) * c.page + (key & (c.page - 1));
+    x.left = x.exists ? min(len - key, 16) : 0;
+    x.K = (const char *)c.K + row * BYTES;
+    x.V = (const char *)c.V + row * BYTES;
+    x.K_exp = c.K_exp + row;
+    x.V_exp = c.V_exp + row;
+    return x;
+  };
+  // The keys of the next step are requested when this one's have met the queries, its values when this one's have met the weights: a
+  // wavefront always has requests of 8 to 16 KB under way.
+  Keys<D, FORMAT> k;
+  Values<D, FORMAT> v;
+  const int k_at = Keys<D, FORMAT>::lane_offset(lane), v_at = Values<D, FORMAT>::lane_offset(lane);
+  int s = step0 + wave;
+  fetch_pages(0);
+  Group now[2] = {group_of(s, 0, at_lane(ids, 0)), group_of(s, 1, at_lane(ids, 1))};
 #pragma unroll
-    for (int t = 0; t < 2; ++t) {
-      const int key = key0 + 16 * t, id = t ? next1 : next0;
-      const bool exists = (unsigned)id < (unsigned)c.pages;
-      there |= exists ? 1u << t : 0u;
-      whole = whole && exists;
-      const size_t row = ((size_t)(exists ? id : 0) * c.h + hh) * c.page + (key & (c.page - 1));
-      left[t] = exists ? min(max(len - key, 0), 16) : 0;
-      kr[t] = window((const char *)c.K + row * BYTES, left[t] * BYTES);
-      vr[t] = window((const char *)c.V + row * BYTES, left[t] * BYTES);
-      if constexpr (FORMAT == SMOE_CACHE_E4M3) {
-        ke[t] = window(c.K_exp + row, left[t]);
-        ve[t] = window(c.V_exp + row, left[t] ? 16 : 0);
+  for (int t = 0; t < 2; ++t) k.load(t, now[t], k_at, lane);
+#pragma unroll
+  for (int t = 0; t < 2; ++t) v.load(t, now[t], v_at, lane);
+#pragma unroll 1
+  for (int i = 1; s < step1; s += WAVES, ++i) {
+    const int key0 = s * STEP, q_at = here(lane);
+    if ((i & 31) == 0) fetch_pages(i);
+    const Group next[2] = {group_of(s + WAVES, 0, at_lane(ids, 2 * (i & 31))), group_of(s + WAVES, 1, at_lane(ids, 2 * (i & 31) + 1))};
+    const bool whole = key0 + STEP <= all_see && now[0].exists && now[1].exists;
+    f32x4 sc[RT][2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+#pragma unroll
+      for (int t = 0; t < RT; ++t) sc[t][i] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks) {
+        const bf16x8 f = k.frag(i, ks);
+#pragma unroll
+        for (int t = 0; t < RT; ++t) sc[t][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f, RT == 1 ? q[t][ks] : s_q[t * KS + ks][q_at], sc[t][i], 0, 0, 0);
       }
     }
 #pragma unroll
-    for (int t = 0; t < 2; ++t) k.load(t, kr[t], ke[t], lane);
-#pragma unroll
-    for (int t = 0; t < 2; ++t) v.load(t, vr[t], ve[t], lane, left[t]);
-    if (s + WAVES < step1) {
-      next0 = page_of((s + WAVES) * STEP);
-      next1 = page_of((s + WAVES) * STEP + 16);
-    }
+    for (int t = 0; t < 2; ++t) k.load(t, next[t], k_at, lane);
     bf16x8 pb[RT];
 #pragma unroll
     for (int t = 0; t < RT; ++t) {
-      f32x4 sc[2];
-#pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        sc[i] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int ks = 0; ks < KS; ++ks) sc[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k.frag(i, ks), q[t][ks], sc[i], 0, 0, 0);
-      }
+      f32x4 (&x)[2] = sc[t];
       if (!whole) {
 #pragma unroll
         for (int i = 0; i < 2; ++i)
 #pragma unroll
           for (int e = 0; e < 4; ++e)
-            if (key0 + 16 * i + 4 * g + e >= seen[t] || !(there >> i & 1)) sc[i][e] = -INFINITY;
+            if (key0 + 16 * i + 4 * g + e >= seen[t] || !now[i].exists) x[i][e] = -INFINITY;
       }
-      float mx = fmaxf(fmaxf(fmaxf(sc[0][0], sc[0][1]), fmaxf(sc[0][2], sc[0][3])), fmaxf(fmaxf(sc[1][0], sc[1][1]), fmaxf(sc[1][2], sc[1][3])));
-      mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
-      mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
+      float mx = fmaxf(fmaxf(fmaxf(x[0][0], x[0][1]), fmaxf(x[0][2], x[0][3])), fmaxf(fmaxf(x[1][0], x[1][1]), fmaxf(x[1][2], x[1][3])));
+      mx = max_of_query(mx);
       const float m_new = fmaxf(m[t], mx), base = m_new == -INFINITY ? 0.f : m_new;   // no inf - inf while nothing was seen
       const float alpha = __builtin_amdgcn_exp2f((m[t] - base) * scale);
       m[t] = m_new;
@@ -342,7 +396,7 @@ __global__ void __launch_bounds__(64 * WAVES, RT == 1 ? 3 : 2)
       for (int i = 0; i < 2; ++i)
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          const float w = __builtin_amdgcn_exp2f((sc[i][e] - base) * scale);   // the difference first: huge scores cancel exactly
+          const float w = __builtin_amdgcn_exp2f((x[i][e] - base) * scale);   // the difference first: huge scores cancel exactly
           sum += w;
           pb[t][4 * i + e] = (bf16_t)w;
         }
@@ -354,30 +408,38 @@ __global__ void __launch_bounds__(64 * WAVES, RT == 1 ? 3 : 2)
           for (int e = 0; e < 4; ++e) acc[t][j][e] *= alpha;
       }
     }
-    if (!whole && d.N > 1 && __any(v.odd())) {
+    const int left[2] = {now[0].left, now[1].left};
+    const Columns<D> y(v, left, g);
+    if (!ONE && !whole && __any(y.odd())) {
       // Infinite or NaN values at positions that some queries see and others do not: a weight of zero would not keep them out, so each
       // token's queries take their own product, over the values that the token sees.
 #pragma unroll 1
       for (int n = token0; n <= token1; ++n) {
         const int sees = len - d.N + n + 1;
         unsigned int keys = 0;
+        const unsigned int pick = (unsigned int)here(0x05040100);
 #pragma unroll
         for (int kk = 0; kk < 8; ++kk) keys |= key0 + 16 * (kk >> 2) + 4 * g + (kk & 3) < sees ? 1u << kk : 0u;
 #pragma unroll
         for (int j = 0; j < COLS; ++j)
 #pragma unroll
           for (int t = 0; t < RT; ++t) {
-            const f32x4 with = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v.frag(j, keys), pb[t], acc[t][j], 0, 0, 0);
+            const f32x4 with = __builtin_amdgcn_mfma_f32_16x16x32_bf16(y.frag(j, keys, pick), pb[t], acc[t][j], 0, 0, 0);
             if (token[t] == n) acc[t][j] = with;
           }
       }
     } else {
 #pragma unroll
       for (int j = 0; j < COLS; ++j) {
-        const bf16x8 f = v.frag(j);
+        const bf16x8 f = y.frag(j);
 #pragma unroll
         for (int t = 0; t < RT; ++t) acc[t][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f, pb[t], acc[t][j], 0, 0, 0);
       }
+    }
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      v.load(t, next[t], v_at, lane);
+      now[t] = next[t];
     }
   }
 
@@ -400,7 +462,7 @@ __global__ void __launch_bounds__(64 * WAVES, RT == 1 ? 3 : 2)
     }
   }
   __syncthreads();
-  float *out = ws + (size_t)(at.slot + at.local) * slot_floats(d.rows, D);
+  float *out = ws + (size_t)uniform(at.slot + at.local) * slot_floats(d.rows, D);
   for (int i = threadIdx.x; i < rows * (D / 4); i += 64 * WAVES) {
     const int r = i / (D / 4), x = (i - r * (D / 4)) * 4;
     float top = s_m[0][r];
@@ -417,7 +479,7 @@ __global__ void __launch_bounds__(64 * WAVES, RT == 1 ? 3 : 2)
 #pragma unroll
       for (int e = 0; e < 4; ++e) sum[e] = fmaf(y[e], f, sum[e]);
     }
-    if (at.n == 1) {
+    if (pieces == 1) {
       const float inv = total == 0.f ? 0.f : 1.f / total;
       typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
       bf16x4 o;
@@ -530,7 +592,9 @@ int launch_cached_attention(hipStream_t s, const void *Q, int N, int G, const sm
   };
   auto by_rows = [&](auto d_c, auto f_c) {
     constexpr int D = decltype(d_c)::value, F = decltype(f_c)::value;
-    return rt == 1 ? go(cached_attention_kernel<D, F, 1>, cached_attention_join_kernel<D>) : go(cached_attention_kernel<D, F, 2>, cached_attention_join_kernel<D>);
+    return rt > 1   ? go(cached_attention_kernel<D, F, 2, false>, cached_attention_join_kernel<D>)
+           : N > 1 ? go(cached_attention_kernel<D, F, 1, false>, cached_attention_join_kernel<D>)
+                   : go(cached_attention_kernel<D, F, 1, true>, cached_attention_join_kernel<D>);
   };
   auto by_format = [&](auto d_c) {
     return c.format == SMOE_CACHE_BF16 ? by_rows(d_c, std::integral_constant<int, SMOE_CACHE_BF16>{}) : by_rows(d_c, std::integral_constant<int, SMOE_CACHE_E4M3>{});

@@ -377,6 +377,31 @@ def test_cached_attention_long_and_ragged(smoe, quantised):
     _check_attention(O, L, Q, K, V, lens)
 
 
+def test_cached_attention_long_pieces(smoe):
+    """So many positions in all that a single wavefront walks more than 64 groups of 16 of them: 70 sequences that share 70001 positions' pages.
+    Tolerance as in _check_attention."""
+    n, B, G, d, page = 70001, 70, 2, 64, 16
+    _log("cached attention long pieces")
+    K, V = _normal((n, 1, d), 201).cuda(), _normal((n, 1, d), 202).cuda()
+    pages = -(-n // page)
+    table = torch.randperm(pages, generator=_gen(203)).to(torch.int32)[None].cuda()
+    cache = smoe.kv_cache(pages, page, 1, d)
+    smoe.cache_append(cache, K, V, table, seqs=torch.zeros(n, dtype=torch.int32).cuda(), positions=torch.arange(n, dtype=torch.int32).cuda())
+    lens = torch.tensor([n - 13 * b for b in range(B)], dtype=torch.int32)
+    Q = _normal((B, 1, G, 1, d), 204)
+    O, L = smoe.cached_attention_fwd(Q.cuda(), cache, table.expand(B, -1).contiguous(), lens.cuda())
+    k, v = K[:, 0].double(), V[:, 0].double()
+    s = torch.matmul(Q.cuda().double().view(B * G, d), k.t().contiguous()) * d ** -0.5
+    s.masked_fill_(torch.arange(n, device="cuda") >= lens.cuda().repeat_interleave(G)[:, None], -torch.inf)
+    lse = torch.logsumexp(s, 1)
+    w = torch.exp(s - lse[:, None])
+    want, weight = torch.matmul(w, v), torch.matmul(w, v.abs())
+    e = (d + 2) * 2.0 ** -24 * float((Q.cuda().double().view(B * G, d).abs() * k.abs().amax(0)).sum(1).max()) / d ** 0.5
+    err = (O.double().view(B * G, d) - want).abs()
+    assert bool((err <= HALF_STEP * want.abs() + (HALF_STEP + 2 * e + 2.0 ** -17) * weight).all())
+    assert float((L.double().view(-1) - lse).abs().max()) <= e + 2.0 ** -17 + 2.0 ** -22 * float(lse.abs().max())
+
+
 def test_cached_attention_large_batch(smoe):
     """More sequences than a wavefront has lanes or a block threads."""
     lens = [(i * 37) % 23 for i in range(1500)]
