@@ -465,13 +465,28 @@ def mlp_bwd(dY, X, W1, W2, r: Routing, k: int, gates, act: int, buf: MLPBuffers)
 
 
 # ---- positions and serving (include/smoe_cache.h) ----------------------------------------------------------------------
-def _here(*tensors, dtype=None):
-    """_chk, and that the tensors live on the current device, on whose stream the launches go."""
-    dev = torch.cuda.current_device()
+# These calls are a few microseconds of work each, so their checks are written to cost little: the device is asked for once a call.
+def _device(first: torch.Tensor) -> int:
+    """The current device, on whose stream the launches go."""
+    if not first.is_cuda:
+        raise ValueError("tensors must be contiguous device tensors")
+    return torch._C._cuda_getDevice()
+
+
+def _here(dev: int, dtype, *tensors):
+    """_chk, and that the tensors live on the current device."""
     for t in tensors:
-        _chk(t, dtype)
-        if t.device.index != dev:
+        if not t.is_cuda or not t.is_contiguous():
+            raise ValueError("tensors must be contiguous device tensors")
+        if t.dtype != dtype:
+            raise TypeError(f"expected {dtype}, got {t.dtype}")
+        if t.get_device() != dev:
             raise ValueError(f"tensor on {t.device}, but the current device is {dev}")
+
+
+def _where(dev: int):
+    """Context and stream of a launch."""
+    return _ctx_by_device.get(dev) or ctx(dev), torch._C._cuda_getCurrentRawStream(dev)
 
 
 ROTARY_SCALINGS = {"none": 0, "linear": 1, "base": 2, "blend": 3}
@@ -500,27 +515,36 @@ def rotary_table(rot: int, layout: str = "half", base: float = 10000.0, scaling:
 
 
 def _turn(entry, what, Q, K, table, positions, out):
-    _here(Q, table.turns)
-    if Q.dim() < 3:
+    dev, dtype = _device(Q), Q.dtype
+    _here(dev, dtype, Q)
+    shape = Q.shape
+    if len(shape) < 3:
         raise ValueError("rows must be [B, T, heads..., d]")
-    B, T, d = Q.shape[0], Q.shape[1], Q.shape[-1]
-    hq, hk = math.prod(Q.shape[2:-1]), 0
+    B, T, d = shape[0], shape[1], shape[-1]
+    hq, hk = math.prod(shape[2:-1]), 0
+    if table.turns.get_device() != dev:
+        raise ValueError(f"table on {table.turns.device}, but the current device is {dev}")
     if K is not None:
-        _here(K, dtype=Q.dtype)
-        if K.dim() < 3 or K.shape[:2] != Q.shape[:2] or K.shape[-1] != d:
+        _here(dev, dtype, K)
+        like = K.shape
+        if len(like) < 3 or like[0] != B or like[1] != T or like[-1] != d:
             raise ValueError("K must be [B, T, heads..., d] like Q")
-        hk = math.prod(K.shape[2:-1])
+        hk = math.prod(like[2:-1])
     if positions is not None:
-        _here(positions, dtype=torch.int32)
+        _here(dev, torch.int32, positions)
         if positions.numel() != B * T:
             raise ValueError("positions must hold B*T entries")
-    Qr, Kr = (_like(Q), None if K is None else _like(K)) if out is None else out
-    if out is not None:
-        for t, like in ((Qr, Q), (Kr, K)):
-            if (t is None) != (like is None) or (t is not None and (t.shape != like.shape or t.dtype != like.dtype)):
+    if out is None:
+        Qr, Kr = _like(Q), None if K is None else _like(K)
+    else:
+        Qr, Kr = out
+        for t, x in ((Qr, Q), (Kr, K)):
+            if (t is None) != (x is None) or (t is not None and t.shape != x.shape):
                 raise ValueError("out must be a pair like (Q, K)")
-        _here(*(t for t in (Qr, Kr) if t is not None))
-    _check(entry(ctx(), _stream(), _dt(Q), _p(Q), hq, _p(K), hk, B * T, d, max(T, 1), _p(positions), table._c, _p(Qr), _p(Kr)), what)
+            if t is not None:
+                _here(dev, dtype, t)
+    c, stream = _where(dev)
+    _check(entry(c, stream, _dt(Q), Q.data_ptr(), hq, _p(K), hk, B * T, d, T or 1, _p(positions), table._c, Qr.data_ptr(), _p(Kr)), what)
     return Qr, Kr
 
 
@@ -553,7 +577,7 @@ class KVCache:
             raise ValueError("the cache's tensors must be on one device")
         self.K, self.V, self.K_exp, self.V_exp = K, V, K_exp, V_exp
         self.pages, self.h, self.page, self.d_head = K.shape
-        self.device = K.device.index
+        self.device = K.get_device()
         self._c = ctypes.byref(smoe_cache(_p(K), _p(V), _p(K_exp), _p(V_exp), self.pages, self.page, self.h, self.d_head, int(quantised)))
 
 
@@ -565,83 +589,99 @@ def kv_cache(pages: int, page: int, h: int, d_head: int, quantised: bool = False
     return KVCache(K, V, *exps)
 
 
-def _places(cache: KVCache, block_table, lens=None, seqs=None, positions=None):
+def _places(dev: int, cache: KVCache, block_table, lens=None, seqs=None, positions=None):
     """The ctypes view of where rows live, and how many rows `seqs` names (None with lens)."""
-    if cache.device != torch.cuda.current_device():
-        raise ValueError(f"cache on device {cache.device}, but the current device is {torch.cuda.current_device()}")
-    _here(block_table, dtype=torch.int32)
+    if cache.device != dev:
+        raise ValueError(f"cache on device {cache.device}, but the current device is {dev}")
+    _here(dev, torch.int32, block_table)
     if block_table.dim() != 2:
         raise ValueError("block_table must be [sequences, width]")
     B, width = block_table.shape
     if lens is not None:
-        _here(lens, dtype=torch.int32)
+        _here(dev, torch.int32, lens)
         if seqs is not None or positions is not None or lens.numel() != B:
             raise ValueError("give lens [sequences], or seqs and positions")
-        return ctypes.byref(smoe_places(_p(block_table), B, width, None, None, _p(lens))), None
+        return ctypes.byref(smoe_places(block_table.data_ptr(), B, width, None, None, lens.data_ptr())), None
     if seqs is None or positions is None or seqs.numel() != positions.numel():
         raise ValueError("give lens [sequences], or seqs and positions of the same length")
-    _here(seqs, positions, dtype=torch.int32)
-    return ctypes.byref(smoe_places(_p(block_table), B, width, _p(seqs), _p(positions), None)), seqs.numel()
+    _here(dev, torch.int32, seqs, positions)
+    return ctypes.byref(smoe_places(block_table.data_ptr(), B, width, seqs.data_ptr(), positions.data_ptr(), None)), seqs.numel()
 
 
 def cache_append(cache: KVCache, K, V, block_table, lens=None, seqs=None, positions=None, rotary: RotaryTable | None = None, Q=None, out=None):
     """Writes the rows K, V [rows, h, d_head] (bf16) to the last places of every sequence (lens), or to the listed ones; with `rotary` K is
     turned first, and Q [rows, ..., d_head] into the returned tensor (`out`, which may be Q)."""
-    where, rows = _places(cache, block_table, lens, seqs, positions)
-    _here(K, V, dtype=torch.bfloat16)
-    M = K.numel() // (cache.h * cache.d_head)
-    if K.numel() != M * cache.h * cache.d_head or V.numel() != K.numel() or (M != rows if rows is not None else M % block_table.shape[0]):
+    dev = _device(K)
+    where, rows = _places(dev, cache, block_table, lens, seqs, positions)
+    _here(dev, torch.bfloat16, K, V)
+    row, n = cache.h * cache.d_head, K.numel()
+    M = n // row
+    if n != M * row or V.numel() != n or (M != rows if rows is not None else M % block_table.shape[0]):
         raise ValueError("K and V must be [rows, h, d_head]")
+    if rotary is not None and rotary.turns.get_device() != dev:
+        raise ValueError(f"table on {rotary.turns.device}, but the current device is {dev}")
     hq, Qr = 0, None
     if Q is not None:
-        _here(Q, dtype=torch.bfloat16)
+        _here(dev, torch.bfloat16, Q)
         hq = Q.numel() // max(1, M * cache.d_head)
         if rotary is None or Q.numel() != M * hq * cache.d_head or Q.shape[-1] != cache.d_head:
             raise ValueError("Q must be [rows, heads..., d_head], and goes with rotary")
-        Qr = _like(Q) if out is None else out
-        if out is not None:
-            _here(out, dtype=torch.bfloat16)
+        if out is None:
+            Qr = _like(Q)
+        else:
+            Qr = out
+            _here(dev, torch.bfloat16, out)
             if out.shape != Q.shape:
                 raise ValueError("out must be like Q")
-        if M == 0:
-            Q = Qr = None       # nothing to turn
-    _check(lib.smoe_cache_append(ctx(), _stream(), BF16, cache._c, where, _p(K), _p(V), M, None if rotary is None else rotary._c, _p(Q), hq, _p(Qr)),
-           "smoe_cache_append")
+    ask_q = Q is not None and M > 0       # without rows there is nothing to turn
+    c, stream = _where(dev)
+    _check(lib.smoe_cache_append(c, stream, BF16, cache._c, where, K.data_ptr(), V.data_ptr(), M, None if rotary is None else rotary._c,
+                                 Q.data_ptr() if ask_q else None, hq, Qr.data_ptr() if ask_q else None), "smoe_cache_append")
     return Qr
 
 
 def cache_read(cache: KVCache, block_table, lens=None, seqs=None, positions=None, N: int = 1, out=None):
     """K, V [rows, h, d_head] (bf16) of the listed places, or of the last N of every sequence (lens)."""
-    where, rows = _places(cache, block_table, lens, seqs, positions)
+    dev = _device(cache.K)
+    where, rows = _places(dev, cache, block_table, lens, seqs, positions)
     rows = block_table.shape[0] * N if rows is None else rows
-    bf = dict(dtype=torch.bfloat16, device=cache.K.device)
-    K, V = (_new(rows, cache.h, cache.d_head, **bf) for _ in "KV") if out is None else out
-    if out is not None:
-        _here(K, V, dtype=torch.bfloat16)
+    if out is None:
+        K, V = (_new(rows, cache.h, cache.d_head, dtype=torch.bfloat16, device=cache.K.device) for _ in "KV")
+    else:
+        K, V = out
+        _here(dev, torch.bfloat16, K, V)
         if K.numel() != rows * cache.h * cache.d_head or V.numel() != K.numel():
             raise ValueError("out must be two tensors [rows, h, d_head]")
-    _check(lib.smoe_cache_read(ctx(), _stream(), BF16, cache._c, where, rows, _p(K), _p(V)), "smoe_cache_read")
+    c, stream = _where(dev)
+    _check(lib.smoe_cache_read(c, stream, BF16, cache._c, where, rows, K.data_ptr(), V.data_ptr()), "smoe_cache_read")
     return K, V
 
 
 def cached_attention_fwd(Q, cache: KVCache, block_table, lens, out=None, ws=None):
     """Q [B, N, G, h, d_head] (bf16), the last N positions of every sequence, over the cache -> O like Q, LSE [B, N, G, h] fp32.
     out = (O, LSE) and ws reuse tensors; O may be Q."""
-    where, _ = _places(cache, block_table, lens)
-    _here(Q, dtype=torch.bfloat16)
+    dev = _device(Q)
+    where, _ = _places(dev, cache, block_table, lens)
+    _here(dev, torch.bfloat16, Q)
+    if Q.dim() != 5:
+        raise ValueError("Q must be [sequences, N, G, h, d_head]")
     B, N, G, h, d = Q.shape
-    if (h, d) != (cache.h, cache.d_head) or B != block_table.shape[0]:
+    if h != cache.h or d != cache.d_head or B != block_table.shape[0]:
         raise ValueError("Q must be [sequences, N, G, h, d_head] with the cache's h and d_head")
-    O, LSE = (_like(Q), _new(B, N, G, h, dtype=torch.float32, device=Q.device)) if out is None else out
-    if out is not None:
-        _here(O, dtype=torch.bfloat16)
-        _here(LSE, dtype=torch.float32)
+    if out is None:
+        O, LSE = _new(B, N, G, h, d, dtype=torch.bfloat16, device=Q.device), _new(B, N, G, h, dtype=torch.float32, device=Q.device)
+    else:
+        O, LSE = out
+        _here(dev, torch.bfloat16, O)
+        _here(dev, torch.float32, LSE)
         if O.shape != Q.shape or LSE.numel() != B * N * G * h:
             raise ValueError("out must be a tensor like Q and one [B, N, G, h]")
-    nb = lib.smoe_cached_attention_workspace_bytes(B, N, G, h, d)
     if ws is None:
-        ws = _ws(nb, Q.device)
-    _check(lib.smoe_cached_attention_fwd(ctx(), _stream(), BF16, _p(Q), N, G, cache._c, where, _p(O), _p(LSE), _p(ws), ws.numel()),
+        ws = _ws(lib.smoe_cached_attention_workspace_bytes(B, N, G, h, d), Q.device)
+    else:
+        _here(dev, torch.uint8, ws)
+    c, stream = _where(dev)
+    _check(lib.smoe_cached_attention_fwd(c, stream, BF16, Q.data_ptr(), N, G, cache._c, where, O.data_ptr(), LSE.data_ptr(), ws.data_ptr(), ws.numel()),
            "smoe_cached_attention_fwd")
     return O, LSE
 
@@ -650,9 +690,12 @@ def momha_decode(X, W_K, W_V, W_Q, W_O, r: Routing, k: int, gates, cache: KVCach
                  out=None, ws=None):
     """The SMoE attention layer on the last N positions of every sequence, X [B*N, d_model], over a cache that holds the earlier ones and
     receives these.  Returns O [B*N, d_model]."""
-    where, _ = _places(cache, block_table, lens)
-    _here(X, W_K, W_V, W_Q, W_O, dtype=torch.bfloat16)
-    _here(gates, dtype=torch.float32)
+    dev = _device(X)
+    where, _ = _places(dev, cache, block_table, lens)
+    _here(dev, torch.bfloat16, X, W_K, W_V, W_Q, W_O)
+    _here(dev, torch.float32, gates)
+    if rotary is not None and rotary.turns.get_device() != dev:
+        raise ValueError(f"table on {rotary.turns.device}, but the current device is {dev}")
     M, d_model = X.shape
     B, d_out = block_table.shape[0], cache.h * cache.d_head
     if B == 0 or M == 0 or M % B or gates.numel() != M * k:
@@ -662,13 +705,15 @@ def momha_decode(X, W_K, W_V, W_Q, W_O, r: Routing, k: int, gates, cache: KVCach
     N = M // B
     O = _like(X) if out is None else out
     if out is not None:
-        _here(out, dtype=torch.bfloat16)
+        _here(dev, torch.bfloat16, out)
         if out.shape != X.shape:
             raise ValueError("out must be like X")
-    nb = lib.smoe_momha_decode_workspace_bytes(B, N, k, d_model, cache.h, cache.d_head)
     if ws is None:
-        ws = _ws(nb, X.device)
+        ws = _ws(lib.smoe_momha_decode_workspace_bytes(B, N, k, d_model, cache.h, cache.d_head), X.device)
+    else:
+        _here(dev, torch.uint8, ws)
     rc = r.c()
-    _check(lib.smoe_momha_decode(ctx(), _stream(), BF16, _p(X), N, d_model, _p(W_K), _p(W_V), _p(W_Q), _p(W_O), ctypes.byref(rc), k, _p(gates),
+    c, stream = _where(dev)
+    _check(lib.smoe_momha_decode(c, stream, BF16, _p(X), N, d_model, _p(W_K), _p(W_V), _p(W_Q), _p(W_O), ctypes.byref(rc), k, _p(gates),
                                  cache._c, where, None if rotary is None else rotary._c, _p(O), _p(ws), ws.numel()), "smoe_momha_decode")
     return O
