@@ -24,8 +24,13 @@ typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 
 constexpr int STEP = 32;         // keys of a step
 constexpr int WAVES = 4;
-constexpr int TARGET = 1024;     // pieces that the whole batch is cut into, about
-constexpr int MIN_STEPS = 16;    // steps of a piece, at least
+constexpr int MAX_TARGET = 768;  // pieces that the whole batch is cut into, about (Dims::target), at most
+// As many pieces as blocks are resident, three a compute unit (one new token) or two: a few more would run by themselves at the end (64
+// sequences of up to 8192 positions: 768 pieces 31.1 us, 1024 33.0; two long ones of three tokens: 512 82.8, 1024 94.4).
+constexpr int T_ONE = 768, T_MULTI = 512, T_TWO = 512;
+constexpr int WHOLE_STEPS = 16;  // sequences of no more steps are not cut
+constexpr int MIN_STEPS = 8;     // steps of a piece, at least
+constexpr int MOST_PIECES = 256; // of a unit
 
 struct Dims {
   int N, G, R;                   // R = N * G query rows of a (sequence, head)
@@ -34,6 +39,8 @@ struct Dims {
   int shift;                     // page = 1 << shift
   int cap;                       // positions the table can hold
   int rows;                      // rows a piece leaves in the workspace
+  int target;                    // pieces that the whole batch is cut into, about
+  bool whole;                    // the table holds too few positions for a sequence to be cut
 };
 
 // ------------------------------------------------------------------------------------------------ the cut
@@ -73,34 +80,76 @@ struct Place {
 // Which sequence does number `index` belong to, counting the pieces of all units (JOIN false), or the units that are cut (JOIN true), in the
 // order of the sequences?  Every wavefront finds its own: a lane takes ceil(B / 64) sequences in a row.  The length of a piece follows from
 // the batch's steps; their sum is a floating number (a few roundings longer or shorter pieces), the same in every wavefront of both kernels.
-// With the hundredth that it is longer there are fewer than TARGET cut units, and fewer than 2 TARGET pieces of cut units.
+// With the hundredth that it is longer there are fewer than `target` cut units, and fewer than twice as many pieces of cut units.
+constexpr int HELD = 4;   // lengths a lane keeps in registers, requested together
 template <bool JOIN> __device__ __forceinline__ bool find_piece(const int32_t *lens, int B, const Dims &d, int index, int lane, Place &p) {
-  const int each = (B + 63) >> 6, first = min(lane * each, B), end = min(first + each, B);
+  const int each = (B + 63) >> 6, first = lane * each, end = min(first + each, B);
+  int held[HELD];
   float sum = 0.f;
-  int mine = 0;                               // the only one's length, where each is one
-  for (int b = first; b < end; ++b) {
-    mine = length_of(lens, b, d.cap);
-    sum += (float)steps_of(mine);
+  auto batch = [&](int from) {
+    if (each == 1) {
+      held[0] = from < end ? lens[from] : -1;
+      held[0] = from < end ? min(max(held[0], 0), d.cap) : -1;
+#pragma unroll
+      for (int i = 1; i < HELD; ++i) held[i] = -1;
+      return;
+    }
+#pragma unroll
+    for (int i = 0; i < HELD; ++i) held[i] = from + i < end ? lens[from + i] : -1;
+#pragma unroll
+    for (int i = 0; i < HELD; ++i) held[i] = from + i < end ? min(max(held[i], 0), d.cap) : -1;
+  };
+#pragma unroll 1
+  for (int c = 0; c < each; c += HELD) {
+    batch(first + c);
+#pragma unroll
+    for (int i = 0; i < HELD; ++i) sum += held[i] >= 0 ? (float)steps_of(held[i]) : 0.f;
   }
   const float total = __int_as_float(at_lane(__float_as_int(scan_add(sum)), 63)) * (float)d.units;
-  const int per = max((int)fminf(total * (1.01f / TARGET), 1e9f) + 1, MIN_STEPS);
+  const int per = max((int)fminf(total * (1.01f / (float)d.target), 1e9f) + 1, MIN_STEPS);
+  // ceil(steps / per) by a reciprocal: steps and per are whole numbers under 2^26, so the quotient is off by less than one
+  const float inv = 1.0f / (float)per;
+  auto pieces_of = [&](int len) {
+    const int steps = steps_of(len);
+    if (steps <= WHOLE_STEPS) return 1;
+    int n = (int)((float)steps * inv);
+    n += n * per < steps ? 1 : 0;
+    n += n * per < steps ? 1 : 0;
+    n -= (n - 1) * per >= steps ? 1 : 0;
+    return min(n, MOST_PIECES);
+  };
   int pieces = 0, cut_pieces = 0, cut_units = 0;
-  for (int b = first; b < end; ++b) {
-    const int n = (steps_of(each == 1 ? mine : length_of(lens, b, d.cap)) + per - 1) / per;
-    pieces += n * d.units;
-    cut_pieces += n > 1 ? n * d.units : 0;
-    cut_units += n > 1 ? d.units : 0;
+#pragma unroll 1
+  for (int c = 0; c < each; c += HELD) {
+    if (each > HELD) batch(first + c);
+#pragma unroll
+    for (int i = 0; i < HELD; ++i) {
+      const int n = held[i] >= 0 ? pieces_of(held[i]) : 0;
+      pieces += n;
+      cut_pieces += n > 1 ? n : 0;
+      cut_units += n > 1 ? 1 : 0;
+    }
   }
-  const int counted = JOIN ? cut_units : pieces;
+  const int counted = (JOIN ? cut_units : pieces) * d.units;
+  cut_pieces *= d.units;
   const int upto = scan_add(counted), slots_upto = scan_add(cut_pieces);
   const unsigned long long past = __ballot(upto > index);
   if (!past) return false;
   const int owner = __ffsll((long long)past) - 1;
   int before = at_lane(upto - counted, owner), slot = at_lane(slots_upto - cut_pieces, owner);
+  if (each == 1) {                            // that lane's only one
+    p.b = owner;
+    p.len = at_lane(held[0], owner);
+    p.n = at_lane(pieces, owner);
+    p.local = index - before;
+    p.slot = slot;
+    return true;
+  }
+#pragma unroll 1
   for (int c = 0; c < each; c += 64) {        // that lane's sequences, one a lane
     const int b = owner * each + c + lane;
     const bool have = c + lane < each && b < B;
-    const int len = have ? length_of(lens, b, d.cap) : 0, n = have ? (steps_of(len) + per - 1) / per : 0;
+    const int len = have ? length_of(lens, b, d.cap) : 0, n = have ? pieces_of(len) : 0;
     const int all = n * d.units, cut = n > 1 ? all : 0, here = JOIN ? (n > 1 ? d.units : 0) : all;
     const int to = scan_add(here), slots_to = scan_add(cut);
     const unsigned long long found = __ballot(before + to > index);
@@ -124,11 +173,10 @@ __host__ __device__ inline size_t slot_floats(int rows, int D) { return (size_t)
 
 // ------------------------------------------------------------------------------------------------ a step's operands
 __device__ __forceinline__ __amdgpu_buffer_rsrc_t window(const void *p, int bytes) { return __builtin_amdgcn_make_buffer_rsrc((void *)p, 0, bytes, 0x00020000); }
-__device__ __forceinline__ u32x4 load4(__amdgpu_buffer_rsrc_t w, int at) {
-  return __builtin_amdgcn_raw_buffer_load_b128(w, at, 0, 0);
-}
-__device__ __forceinline__ u32x2 load2(__amdgpu_buffer_rsrc_t w, int at) { return __builtin_amdgcn_raw_buffer_load_b64(w, at, 0, 0); }
-__device__ __forceinline__ uint32_t load1(__amdgpu_buffer_rsrc_t w, int at) { return __builtin_amdgcn_raw_buffer_load_b32(w, at, 0, 0); }
+// ONCE: bytes that nothing will read again are kept by no cache.
+template <bool ONCE> __device__ __forceinline__ u32x4 load4(__amdgpu_buffer_rsrc_t w, int at) { return __builtin_amdgcn_raw_buffer_load_b128(w, at, 0, ONCE ? 2 : 0); }
+template <bool ONCE> __device__ __forceinline__ u32x2 load2(__amdgpu_buffer_rsrc_t w, int at) { return __builtin_amdgcn_raw_buffer_load_b64(w, at, 0, ONCE ? 2 : 0); }
+template <bool ONCE> __device__ __forceinline__ uint32_t load1(__amdgpu_buffer_rsrc_t w, int at) { return __builtin_amdgcn_raw_buffer_load_b32(w, at, 0, ONCE ? 2 : 0); }
 
 // two bf16 of the lower or upper two of four e4m3 codes, scaled
 template <bool UPPER> __device__ __forceinline__ uint32_t widen(uint32_t codes, float scale) {
@@ -168,11 +216,11 @@ template <int D, int FORMAT> struct Keys {
   u32x4 v[2][LOADS];
   uint32_t e[2];
   static __device__ __forceinline__ int lane_offset(int lane) { return (lane & 15) * BYTES + (lane >> 4) * 16; }
-  __device__ __forceinline__ void load(int t, const Group &p, int at, int lane) {
+  template <bool ONCE> __device__ __forceinline__ void load(int t, const Group &p, int at, int lane) {
     const __amdgpu_buffer_rsrc_t rows = window(p.K, p.left * BYTES);
     at = here(at);
 #pragma unroll
-    for (int i = 0; i < LOADS; ++i) v[t][i] = load4(rows, at + i * 64);
+    for (int i = 0; i < LOADS; ++i) v[t][i] = load4<ONCE>(rows, at + i * 64);
     if constexpr (FORMAT == SMOE_CACHE_E4M3) e[t] = __builtin_amdgcn_raw_buffer_load_b8(window(p.K_exp, p.left), lane & 15, 0, 0);
   }
   // first element of the lane's eight of instruction ks
@@ -193,29 +241,29 @@ template <int D, int FORMAT> struct Keys {
 // Values: lane -> keys 4 (lane / 16) + 0..3 of both groups, columns D / 16 * (lane % 16) and on.
 template <int D, int FORMAT> struct Values {
   static constexpr int COLS = D / 16, WORDS = COLS / 2;    // columns of a lane, 32-bit words of them as bf16
-  static constexpr int HELD = FORMAT == SMOE_CACHE_BF16 ? WORDS : WORDS / 2;
+  static constexpr int KEPT = FORMAT == SMOE_CACHE_BF16 ? WORDS : WORDS / 2;
   static constexpr int BYTES = FORMAT == SMOE_CACHE_BF16 ? D * 2 : D;
-  uint32_t v[8][HELD];
+  uint32_t v[8][KEPT];
   uint32_t e[2];
-  static __device__ __forceinline__ int lane_offset(int lane) { return (lane >> 4) * 4 * BYTES + (lane & 15) * HELD * 4; }
-  __device__ __forceinline__ void load(int t, const Group &p, int at, int lane) {
+  static __device__ __forceinline__ int lane_offset(int lane) { return (lane >> 4) * 4 * BYTES + (lane & 15) * KEPT * 4; }
+  template <bool ONCE> __device__ __forceinline__ void load(int t, const Group &p, int at, int lane) {
     const __amdgpu_buffer_rsrc_t rows = window(p.V, p.left * BYTES);
     at = here(at);
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      if constexpr (HELD == 4) {
-        const u32x4 x = load4(rows, at + i * BYTES);
+      if constexpr (KEPT == 4) {
+        const u32x4 x = load4<ONCE>(rows, at + i * BYTES);
 #pragma unroll
         for (int w = 0; w < 4; ++w) v[4 * t + i][w] = x[w];
-      } else if constexpr (HELD == 2) {
-        const u32x2 x = load2(rows, at + i * BYTES);
+      } else if constexpr (KEPT == 2) {
+        const u32x2 x = load2<ONCE>(rows, at + i * BYTES);
         v[4 * t + i][0] = x[0];
         v[4 * t + i][1] = x[1];
       } else {
-        v[4 * t + i][0] = load1(rows, at + i * BYTES);
+        v[4 * t + i][0] = load1<ONCE>(rows, at + i * BYTES);
       }
     }
-    if constexpr (FORMAT == SMOE_CACHE_E4M3) e[t] = load1(window(p.V_exp, p.left ? 16 : 0), (lane >> 4) * 4);
+    if constexpr (FORMAT == SMOE_CACHE_E4M3) e[t] = load1<false>(window(p.V_exp, p.left ? 16 : 0), (lane >> 4) * 4);
   }
 };
 // The same as bf16.
@@ -270,7 +318,7 @@ template <int D> struct Columns {
 
 // ------------------------------------------------------------------------------------------------ one piece
 // ONE: a single new token a sequence, so that every position within the length is seen by every query.
-template <int D, int FORMAT, int RT, bool ONE>
+template <int D, int FORMAT, int RT, bool ONE, bool ONCE>
 __global__ void __launch_bounds__(64 * WAVES, RT == 1 && ONE ? 3 : 2)
     cached_attention_kernel(const bf16_t *Q, smoe_cache c, smoe_places p, Dims d, bf16_t *O, float *LSE, float *ws) {
   constexpr int KS = D / 32, COLS = D / 16, ROW = D + 4;     // padded: a wavefront's 16 rows start in 16 different banks
@@ -279,7 +327,15 @@ __global__ void __launch_bounds__(64 * WAVES, RT == 1 && ONE ? 3 : 2)
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
   const int col = lane & 15, g = lane >> 4;
   Place at;
-  if (!find_piece<false>(p.lens, p.sequences, d, (int)blockIdx.x, lane, at)) return;   // the grid is an upper bound
+  if (d.whole) {              // no sequence can be long enough to be cut: a block for each unit
+    at.b = (int)blockIdx.x / d.units;
+    at.len = length_of(p.lens, at.b, d.cap);
+    at.n = 1;
+    at.local = (int)blockIdx.x - at.b * d.units;
+    at.slot = 0;
+  } else if (!find_piece<false>(p.lens, p.sequences, d, (int)blockIdx.x, lane, at)) {
+    return;                   // the grid is an upper bound
+  }
   // everything of the piece is wave-uniform, and is told so: the windows below live in scalar registers
   const int pieces = uniform(at.n), len = uniform(at.len), b = uniform(at.b);
   const int unit = uniform(at.local / pieces), piece = uniform(at.local) - unit * pieces;
@@ -301,12 +357,9 @@ __global__ void __launch_bounds__(64 * WAVES, RT == 1 && ONE ? 3 : 2)
     seen[t] = len - d.N + token[t] + 1;
     const bf16_t *src = Q + (((size_t)b * d.R + r) * c.h + hh) * D;
 #pragma unroll
-    for (int ks = 0; ks < KS; ++ks) {
-      if (RT == 1) q[t][ks] = *reinterpret_cast<const bf16x8 *>(src + Keys<D, FORMAT>::query_offset(ks, lane));
-      else if ((t * KS + ks) % WAVES == wave) s_q[t * KS + ks][lane] = *reinterpret_cast<const bf16x8 *>(src + Keys<D, FORMAT>::query_offset(ks, lane));
-    }
+    for (int ks = 0; ks < KS; ++ks)
+      if (RT == 1 || (t * KS + ks) % WAVES == wave) q[t][ks] = *reinterpret_cast<const bf16x8 *>(src + Keys<D, FORMAT>::query_offset(ks, lane));
   }
-  if (RT > 1) __syncthreads();
   const int token0 = row0 / d.G, token1 = (row0 + rows - 1) / d.G;
   const int all_see = len - d.N + token0 + 1;               // every query of the tile sees the keys before this one
 
@@ -327,14 +380,14 @@ __global__ void __launch_bounds__(64 * WAVES, RT == 1 && ONE ? 3 : 2)
   // The wavefront's next 64 page numbers, one a lane: two for each of its steps from the `from`-th on.
   int ids = -1;
   auto fetch_pages = [&](int from) {
-    const int step = step0 + wave + (from + (lane >> 1)) * WAVES, key = step * STEP + 16 * (lane & 1);
-    ids = step < step1 && key < len ? table[key >> d.shift] : -1;
+    const int key = (step0 + wave + (from + (lane >> 1)) * WAVES) * STEP + 16 * (lane & 1);
+    ids = (unsigned)key < (unsigned)d.cap ? table[key >> d.shift] : -1;    // whatever the length: it may still be on its way
     ids = here(ids);      // waited for at this place, not where a number is used in the loop
   };
   auto group_of = [&](int step, int t, int id) {
     const int key = step * STEP + 16 * t;
     Group x;
-    x.exists = (unsigned)id < (unsigned)c.pages;
+    x.exists = (unsigned)id < (unsigned)c.pages && step < step1 && key < len;
     const size_t row = ((size_t)(x.exists ? id : 0) * c.h + hh) * c.page + (key & (c.page - 1));
     x.left = x.exists ? min(len - key, 16) : 0;
     x.K = (const char *)c.K + row * BYTES;
@@ -352,15 +405,23 @@ __global__ void __launch_bounds__(64 * WAVES, RT == 1 && ONE ? 3 : 2)
   fetch_pages(0);
   Group now[2] = {group_of(s, 0, at_lane(ids, 0)), group_of(s, 1, at_lane(ids, 1))};
 #pragma unroll
-  for (int t = 0; t < 2; ++t) k.load(t, now[t], k_at, lane);
+  for (int t = 0; t < 2; ++t) k.template load<ONCE>(t, now[t], k_at, lane);
 #pragma unroll
-  for (int t = 0; t < 2; ++t) v.load(t, now[t], v_at, lane);
-#pragma unroll 1
-  for (int i = 1; s < step1; s += WAVES, ++i) {
+  for (int t = 0; t < 2; ++t) v.template load<ONCE>(t, now[t], v_at, lane);
+  if (RT > 1) {
+#pragma unroll
+    for (int f = 0; f < RT * KS; ++f)
+      if (f % WAVES == wave) s_q[f][lane] = q[f / KS][f % KS];
+    __syncthreads();
+  }
+  int i = 1;                // which of the wavefront's steps is next
+  // TAIL: not every query sees every key of the step.
+  auto take_step = [&](auto tail) {
+    constexpr bool TAIL = decltype(tail)::value;
     const int key0 = s * STEP, q_at = here(lane);
     if ((i & 31) == 0) fetch_pages(i);
     const Group next[2] = {group_of(s + WAVES, 0, at_lane(ids, 2 * (i & 31))), group_of(s + WAVES, 1, at_lane(ids, 2 * (i & 31) + 1))};
-    const bool whole = key0 + STEP <= all_see && now[0].exists && now[1].exists;
+    ++i;
     f32x4 sc[RT][2];
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
@@ -374,17 +435,17 @@ __global__ void __launch_bounds__(64 * WAVES, RT == 1 && ONE ? 3 : 2)
       }
     }
 #pragma unroll
-    for (int t = 0; t < 2; ++t) k.load(t, next[t], k_at, lane);
+    for (int t = 0; t < 2; ++t) k.template load<ONCE>(t, next[t], k_at, lane);
     bf16x8 pb[RT];
 #pragma unroll
     for (int t = 0; t < RT; ++t) {
       f32x4 (&x)[2] = sc[t];
-      if (!whole) {
+      if (TAIL || !now[0].exists || !now[1].exists) {
 #pragma unroll
         for (int i = 0; i < 2; ++i)
 #pragma unroll
           for (int e = 0; e < 4; ++e)
-            if (key0 + 16 * i + 4 * g + e >= seen[t] || !now[i].exists) x[i][e] = -INFINITY;
+            if ((TAIL && key0 + 16 * i + 4 * g + e >= seen[t]) || !now[i].exists) x[i][e] = -INFINITY;
       }
       float mx = fmaxf(fmaxf(fmaxf(x[0][0], x[0][1]), fmaxf(x[0][2], x[0][3])), fmaxf(fmaxf(x[1][0], x[1][1]), fmaxf(x[1][2], x[1][3])));
       mx = max_of_query(mx);
@@ -410,7 +471,7 @@ __global__ void __launch_bounds__(64 * WAVES, RT == 1 && ONE ? 3 : 2)
     }
     const int left[2] = {now[0].left, now[1].left};
     const Columns<D> y(v, left, g);
-    if (!ONE && !whole && __any(y.odd())) {
+    if (!ONE && TAIL && __any(y.odd())) {
       // Infinite or NaN values at positions that some queries see and others do not: a weight of zero would not keep them out, so each
       // token's queries take their own product, over the values that the token sees.
 #pragma unroll 1
@@ -438,10 +499,15 @@ __global__ void __launch_bounds__(64 * WAVES, RT == 1 && ONE ? 3 : 2)
     }
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
-      v.load(t, next[t], v_at, lane);
+      v.template load<ONCE>(t, next[t], v_at, lane);
       now[t] = next[t];
     }
-  }
+    s += WAVES;
+  };
+#pragma unroll 1
+  while (s < step1 && (s + 1) * STEP <= all_see) take_step(std::false_type{});
+#pragma unroll 1
+  while (s < step1) take_step(std::true_type{});
 
   // The wavefronts' parts meet in LDS.  A lane holds columns 4 COLS g + COLS e + j of its query, j and e running.
 #pragma unroll
@@ -499,35 +565,55 @@ __global__ void __launch_bounds__(64 * WAVES, RT == 1 && ONE ? 3 : 2)
 }
 
 // ------------------------------------------------------------------------------------------------ the join
-// A block for each row of a cut unit: eight wavefronts' worth of lanes take its pieces in turn, D / 4 lanes a piece, and the groups' sums
-// meet in LDS in a fixed order.
-constexpr int JOIN_THREADS = 512;
-template <int D> __global__ void __launch_bounds__(JOIN_THREADS) cached_attention_join_kernel(smoe_places p, Dims d, int h, const float *ws, bf16_t *O, float *LSE) {
+// A block takes some rows of a cut unit, D / 4 lanes a row, or several such groups, which take its pieces in turn and meet in LDS in a
+// fixed order: one row a block where few units are cut, into many pieces, and more of them where the units fill the chip.
+// A thousand lanes a block only where there are hardly any blocks: one sequence of 131072 positions, one head, 8 rows 21.0 us (22.5 with 256);
+// one of 4096 with 4 heads of 4 rows 12.5 (11.6).
+constexpr int JOIN_AHEAD = 8, JOIN_FEW = 16;
+template <int D, int JOIN_THREADS> __global__ void __launch_bounds__(JOIN_THREADS)
+    cached_attention_join_kernel(smoe_places p, Dims d, int h, int rows_log2, const float *ws, bf16_t *O, float *LSE) {
   constexpr int LANES = D / 4, GROUPS = JOIN_THREADS / LANES;
   __shared__ __attribute__((aligned(16))) float s_acc[GROUPS][D + 4];
   __shared__ float s_m[GROUPS], s_l[GROUPS];
   const int lane = threadIdx.x & 63;
   Place at;
   if (!find_piece<true>(p.lens, p.sequences, d, (int)blockIdx.x, lane, at)) return;
-  const int unit = at.local, tile = unit / h, hh = unit - tile * h, r = blockIdx.y;
-  if (tile * d.rows + r >= d.R) return;
+  const int unit = at.local, tile = unit / h, hh = unit - tile * h;
+  const int each = GROUPS >> rows_log2;                     // groups of a row
+  const int group = threadIdx.x / LANES, x = (threadIdx.x % LANES) * 4;
+  const int r = ((int)blockIdx.y << rows_log2) + group / each, sub = group & (each - 1);
+  const bool mine = r < d.rows && tile * d.rows + r < d.R;
   const float scale = 1.4426950408889634f / sqrtf((float)D);
   const size_t stride = slot_floats(d.rows, D);
   const float *base = ws + (size_t)(at.slot + unit * at.n) * stride;
-  const int group = threadIdx.x / LANES, x = (threadIdx.x % LANES) * 4;
   f32x4 acc = f32x4{0.f, 0.f, 0.f, 0.f};
   float m = -INFINITY, l = 0.f;
-#pragma unroll 4
-  for (int i = group; i < at.n; i += GROUPS) {
-    const float *src = base + (size_t)i * stride;
-    const float pm = src[(size_t)d.rows * D + r], pl = src[(size_t)d.rows * (D + 1) + r];
-    const f32x4 y = *reinterpret_cast<const f32x4 *>(src + (size_t)r * D + x);
-    const float top = fmaxf(m, pm), safe = top == -INFINITY ? 0.f : top;
-    const float old = __builtin_amdgcn_exp2f((m - safe) * scale), now = __builtin_amdgcn_exp2f((pm - safe) * scale);
-    m = top;
-    l = fmaf(l, old, pl * now);
+  if (mine) {
+#pragma unroll 1
+    for (int i0 = sub; i0 < at.n; i0 += each * JOIN_AHEAD) {
+      float pm[JOIN_AHEAD], pl[JOIN_AHEAD];
+      f32x4 y[JOIN_AHEAD];
 #pragma unroll
-    for (int e = 0; e < 4; ++e) acc[e] = fmaf(acc[e], old, y[e] * now);
+      for (int u = 0; u < JOIN_AHEAD; ++u) {
+        const int i = i0 + u * each;
+        if (i < at.n) {
+          const float *src = base + (size_t)i * stride;
+          pm[u] = src[(size_t)d.rows * D + r];
+          pl[u] = src[(size_t)d.rows * (D + 1) + r];
+          y[u] = *reinterpret_cast<const f32x4 *>(src + (size_t)r * D + x);
+        }
+      }
+#pragma unroll
+      for (int u = 0; u < JOIN_AHEAD; ++u) {
+        if (i0 + u * each >= at.n) break;
+        const float top = fmaxf(m, pm[u]), safe = top == -INFINITY ? 0.f : top;
+        const float old = __builtin_amdgcn_exp2f((m - safe) * scale), now = __builtin_amdgcn_exp2f((pm[u] - safe) * scale);
+        m = top;
+        l = fmaf(l, old, pl[u] * now);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) acc[e] = fmaf(acc[e], old, y[u][e] * now);
+      }
+    }
   }
   *reinterpret_cast<f32x4 *>(&s_acc[group][x]) = acc;
   if (x == 0) {
@@ -535,19 +621,17 @@ template <int D> __global__ void __launch_bounds__(JOIN_THREADS) cached_attentio
     s_l[group] = l;
   }
   __syncthreads();
-  if (threadIdx.x >= LANES) return;
-  float top = s_m[0];
-#pragma unroll
-  for (int w = 1; w < GROUPS; ++w) top = fmaxf(top, s_m[w]);
+  if (!mine || sub != 0) return;
+  float top = m;
+  for (int w = 1; w < each; ++w) top = fmaxf(top, s_m[group + w]);
   const float safe = top == -INFINITY ? 0.f : top;
   f32x4 sum = f32x4{0.f, 0.f, 0.f, 0.f};
   float total = 0.f;
+  for (int w = 0; w < each; ++w) {
+    const float f = __builtin_amdgcn_exp2f((s_m[group + w] - safe) * scale);
+    total = fmaf(s_l[group + w], f, total);
 #pragma unroll
-  for (int w = 0; w < GROUPS; ++w) {
-    const float f = __builtin_amdgcn_exp2f((s_m[w] - safe) * scale);
-    total = fmaf(s_l[w], f, total);
-#pragma unroll
-    for (int e = 0; e < 4; ++e) sum[e] = fmaf(s_acc[w][x + e], f, sum[e]);
+    for (int e = 0; e < 4; ++e) sum[e] = fmaf(s_acc[group + w][x + e], f, sum[e]);
   }
   const float inv = total == 0.f ? 0.f : 1.f / total;
   typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
@@ -564,7 +648,7 @@ int row_tiles(int R) { return R > 16 ? 2 : 1; }
 
 }  // namespace
 
-constexpr size_t MAX_SLOTS = 2 * TARGET;
+constexpr size_t MAX_SLOTS = 2 * MAX_TARGET;
 size_t cached_attention_workspace_bytes(int N, int G, int d_head) {
   const long long R = (long long)N * G;
   return MAX_SLOTS * slot_floats((int)std::min<long long>(R, 16 * row_tiles((int)std::min<long long>(R, 1 << 20))), d_head) * sizeof(float);
@@ -581,23 +665,43 @@ int launch_cached_attention(hipStream_t s, const void *Q, int N, int G, const sm
   d.shift = __builtin_ctz((unsigned int)c.page);
   d.cap = p.width * c.page;
   const long long units = (long long)d.tiles * c.h, all = units * p.sequences;
-  if (all > 0x7fffffffLL / 256 - 2 * TARGET) return SMOE_ERR_UNSUPPORTED;    // one-dimensional grids
+  if (all > 0x7fffffffLL / 256 - 2 * MAX_TARGET) return SMOE_ERR_UNSUPPORTED;    // one-dimensional grids
   d.units = (int)units;
-  auto go = [&](auto kernel, auto join) {
-    kernel<<<(unsigned int)all + TARGET, 64 * WAVES, 0, s>>>((const bf16_t *)Q, c, p, d, (bf16_t *)O, LSE, (float *)ws);
+  d.target = rt == 1 && N == 1 ? T_ONE : rt == 1 ? T_MULTI : T_TWO;
+  d.whole = d.cap <= WHOLE_STEPS * STEP;
+  // pieces at most: a sequence's are ceil(steps / per) <= 1 + steps / per, and at most its share of the table's positions; without cuts a
+  // block numbers its unit directly, so the grid is exact
+  const long long most = d.whole ? all : std::min<long long>(all + d.target, all * ceil_div(ceil_div(d.cap, STEP), MIN_STEPS));
+  auto go = [&](auto kernel, auto join, auto join_few) {
+    kernel<<<(unsigned int)most, 64 * WAVES, 0, s>>>((const bf16_t *)Q, c, p, d, (bf16_t *)O, LSE, (float *)ws);
     if (hipGetLastError() != hipSuccess) return SMOE_ERR_HIP;
-    if (d.cap <= MIN_STEPS * STEP) return SMOE_OK;                           // no sequence can be cut
-    join<<<dim3((unsigned int)std::min<long long>(all, TARGET), d.rows), JOIN_THREADS, 0, s>>>(p, d, c.h, (const float *)ws, (bf16_t *)O, LSE);
+    if (d.whole) return SMOE_OK;
+    const long long cut = std::min<long long>(all, d.target);                  // units, at most
+    const bool few = cut * d.rows <= JOIN_FEW;
+    int rows_log2 = 0;
+    while ((2 << rows_log2) <= 256 * 4 / c.d_head && (1 << rows_log2) < d.rows && cut * ceil_div(d.rows, 2 << rows_log2) >= 512) ++rows_log2;
+    const dim3 grid((unsigned int)cut, ceil_div(d.rows, 1 << rows_log2));
+    if (few) join_few<<<grid, 1024, 0, s>>>(p, d, c.h, rows_log2, (const float *)ws, (bf16_t *)O, LSE);
+    else join<<<grid, 256, 0, s>>>(p, d, c.h, rows_log2, (const float *)ws, (bf16_t *)O, LSE);
     return hipGetLastError() == hipSuccess ? SMOE_OK : SMOE_ERR_HIP;
   };
-  auto by_rows = [&](auto d_c, auto f_c) {
+  auto by_rows = [&](auto d_c, auto f_c, auto once_c) {
     constexpr int D = decltype(d_c)::value, F = decltype(f_c)::value;
-    return rt > 1   ? go(cached_attention_kernel<D, F, 2, false>, cached_attention_join_kernel<D>)
-           : N > 1 ? go(cached_attention_kernel<D, F, 1, false>, cached_attention_join_kernel<D>)
-                   : go(cached_attention_kernel<D, F, 1, true>, cached_attention_join_kernel<D>);
+    constexpr bool ONCE = decltype(once_c)::value;
+    auto join = cached_attention_join_kernel<D, 256>, join_few = cached_attention_join_kernel<D, 1024>;
+    return rt > 1   ? go(cached_attention_kernel<D, F, 2, false, ONCE>, join, join_few)
+           : N > 1 ? go(cached_attention_kernel<D, F, 1, false, ONCE>, join, join_few)
+                   : go(cached_attention_kernel<D, F, 1, true, ONCE>, join, join_few);
   };
+  // Where one tile holds all rows a key is read by one block, and the next call reads another layer's: past the caches, then, unless the
+  // cache is so small that several layers' stay in the last-level cache (256 MB) from one token to the next.  64 sequences of up to 8192
+  // positions, 135 MB, read in turn with four more such caches: 33.0 us past the caches, 36.4 through them; 64 of 100 to 8192, 240 MB, 51.2 /
+  // 55.9; one of 4096, 17 MB, 11.6 / 11.8 in turn with 35 more, but 15.0 / 13.3 where all stay; one of 301 7.3 / 6.5.
+  const size_t held = (size_t)std::min<long long>(c.pages, (long long)p.sequences * p.width) * c.page * c.h * c.d_head * (c.format == SMOE_CACHE_BF16 ? 4 : 2);
+  const bool once = d.tiles == 1 && held > LAST_LEVEL_CACHE / 4;
+  auto by_once = [&](auto d_c, auto f_c) { return once ? by_rows(d_c, f_c, std::true_type{}) : by_rows(d_c, f_c, std::false_type{}); };
   auto by_format = [&](auto d_c) {
-    return c.format == SMOE_CACHE_BF16 ? by_rows(d_c, std::integral_constant<int, SMOE_CACHE_BF16>{}) : by_rows(d_c, std::integral_constant<int, SMOE_CACHE_E4M3>{});
+    return c.format == SMOE_CACHE_BF16 ? by_once(d_c, std::integral_constant<int, SMOE_CACHE_BF16>{}) : by_once(d_c, std::integral_constant<int, SMOE_CACHE_E4M3>{});
   };
   return c.d_head == 128 ? by_format(std::integral_constant<int, 128>{}) : by_format(std::integral_constant<int, 64>{});
 }
