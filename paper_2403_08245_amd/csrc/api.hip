@@ -1012,7 +1012,7 @@ size_t smoe_momha_decode_workspace_bytes(int B, int N, int k, int d_model, int h
   const size_t attention = smoe_cached_attention_workspace_bytes(B, N, k, h_expert, d_head);
   if (!attention || d_model < 1) return 0;
   MomhaSizes z = momha_sizes(B, N, k, d_model, h_expert, d_head);
-  return 256 + S2S_TAIL_WS_BYTES + 2 * z.kv + z.q + z.lse + z.yhat + attention;
+  return 256 + S2S_TAIL_WS_BYTES + 2 * z.kv + z.q + z.lse + z.yhat + attention;   // the shares of K and V lie where partial tiles do
 }
 
 int smoe_momha_decode(smoe_ctx *ctx, void *stream, smoe_dtype dtype, const void *X, int N, int d_model, const void *W_K, const void *W_V,
@@ -1041,14 +1041,29 @@ int smoe_momha_decode(smoe_ctx *ctx, void *stream, smoe_dtype dtype, const void 
   void *Yhat = p;  p += z.yhat;
   hipStream_t s = (hipStream_t)stream;
   auto product = [&](S2SArgs a) { a.tail_ws = tail_ws; return run_s2s(ctx, s, dtype, a); };
-  S2SArgs pv = dense_s2s(X, W_V, V, dense_off, M, d_model, d_out, false);
-  S2SArgs pk = dense_s2s(X, W_K, K, dense_off, M, d_model, d_out, false);
-  pv.tail_ws = pk.tail_ws = tail_ws;
-  rc = run_s2s_pair(ctx, s, pv, pk, dense_off);
+  rc = product(make_s2s(X, W_Q, Q, r, d_model, d_out, false, false, k, false));   // first: it may leave partial tiles where the shares go next
   if (rc != SMOE_OK) return rc;
-  rc = product(make_s2s(X, W_Q, Q, r, d_model, d_out, false, false, k, false));
-  if (rc != SMOE_OK) return rc;
-  rc = smoe_cache_append(ctx, stream, dtype, cache, places, K, V, M, rotary, rotary ? Q : nullptr, k * h, rotary ? Q : nullptr);
+  TurnArgs t;
+  t.Q = t.Qr = rotary ? Q : nullptr;
+  t.K = K;
+  t.V = V;
+  t.hq = rotary ? k * h : 0;
+  t.hk = h;
+  t.rows = M;
+  t.d = d_head;
+  if (rotary) t.rotary = *rotary;
+  const int shares = ctx->kernel_mode == 0 ? skinny_shares(M, d_model, d_out) : 0;
+  if (shares && (size_t)shares * 2 * M * d_out * sizeof(float) <= S2S_TAIL_WS_BYTES) {
+    t.parts = tail_ws;
+    t.shares = shares;
+    rc = launch_skinny_pair(s, X, W_K, W_V, M, d_model, d_out, shares, tail_ws);
+  } else {
+    S2SArgs pv = dense_s2s(X, W_V, V, dense_off, M, d_model, d_out, false);
+    S2SArgs pk = dense_s2s(X, W_K, K, dense_off, M, d_model, d_out, false);
+    pv.tail_ws = pk.tail_ws = tail_ws;
+    rc = run_s2s_pair(ctx, s, pv, pk, dense_off);
+  }
+  if (rc == SMOE_OK) rc = launch_cache_append(s, t, *cache, *places);
   if (rc != SMOE_OK) return rc;
   rc = smoe_cached_attention_fwd(ctx, stream, dtype, Q, N, k, cache, places, Q, LSE, p, need - (size_t)(p - (char *)ws));
   if (rc != SMOE_OK) return rc;

@@ -2,6 +2,7 @@
 #pragma once
 #include "common.h"
 #include "smoe_cache.h"
+#include <algorithm>
 
 // Rows of Q, K and V of one launch that turns rows by their positions and, for a cache, stores those of K and V.
 struct TurnArgs {
@@ -12,10 +13,18 @@ struct TurnArgs {
   const int32_t *positions = nullptr;
   smoe_rotary rotary{nullptr, 0, 0, 1.f}; // turns NULL: nothing is turned
   bool back = false;                      // by the opposite angle
+  // With a cache: K and V as fp32 shares [shares][2][rows][hk * d] that add up to them (launch_skinny_pair), in the place of bf16 rows.
+  const float *parts = nullptr;
+  int shares = 0;
 };
 int launch_turn(hipStream_t s, smoe_dtype dt, const TurnArgs &a);
 int launch_cache_append(hipStream_t s, const TurnArgs &a, const smoe_cache &c, const smoe_places &p);
 int launch_cache_read(hipStream_t s, const smoe_cache &c, const smoe_places &p, int rows, void *K, void *V);
+
+// Two dense products X [M, K] W [K, N] of few rows, left as shares of the contraction, P [shares][2][M][N] fp32 (gemm_skinny.hip).
+constexpr int SKINNY_MAX_ROWS = 128;
+int skinny_shares(int M, int K, int N);      // 0: not for this kernel
+int launch_skinny_pair(hipStream_t s, const void *X, const void *W0, const void *W1, int M, int K, int N, int shares, float *P);
 
 size_t cached_attention_workspace_bytes(int N, int G, int d_head);
 int launch_cached_attention(hipStream_t s, const void *Q, int N, int G, const smoe_cache &c, const smoe_places &p, void *O, float *LSE, void *ws);

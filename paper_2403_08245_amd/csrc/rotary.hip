@@ -33,6 +33,23 @@ template <> struct Eight<float> {
   __device__ __forceinline__ void set(int i, float x) { v[i >> 2][i & 3] = x; }
 };
 
+// the sum of 8 elements' shares, in their order
+__device__ __forceinline__ void sum_parts(const float *src, size_t stride, int shares, int e0, Eight<float> &y) {
+  typedef float f32x4 __attribute__((ext_vector_type(4)));
+  f32x4 lo = f32x4{0.f, 0.f, 0.f, 0.f}, hi = lo;
+#pragma unroll 4
+  for (int k = 0; k < shares; ++k) {
+    const f32x4 *p = reinterpret_cast<const f32x4 *>(src + k * stride + e0);
+    lo += p[0];
+    hi += p[1];
+  }
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    y.set(i, lo[i]);
+    y.set(4 + i, hi[i]);
+  }
+}
+
 struct Work {          // how the rows of a launch are dealt to wavefronts
   int groups;          // wavefronts a token
   int per;             // rows of each
@@ -64,8 +81,8 @@ __device__ __forceinline__ uint2 to_e4m3(float (&y)[8], int lanes, unsigned int 
   return q;
 }
 
-// CACHE: -1 none (Q and K go to Qr and Kr), else the cache's format, and the rows of K and V go there.
-template <typename T, int CACHE>
+// CACHE: -1 none (Q and K go to Qr and Kr), else the cache's format, and the rows of K and V go there.  PARTS: those rows come as fp32 shares.
+template <typename T, int CACHE, bool PARTS>
 __global__ void __launch_bounds__(64 * WAVES) turn_rows_kernel(TurnArgs a, smoe_cache c, smoe_places places, Work w, int N, int page_shift) {
   __shared__ float2 angle[WAVES][MAX_PAIRS];
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
@@ -115,10 +132,32 @@ __global__ void __launch_bounds__(64 * WAVES) turn_rows_kernel(TurnArgs a, smoe_
   const int total = a.hq + a.hk + (CACHE >= 0 ? a.hk : 0), last = min((group + 1) * w.per, total);
   for (int j0 = group * w.per; j0 < last; j0 += rows_at_once * BATCH) {
     Eight<T> x[BATCH], p[BATCH];
+    Eight<float> xf[PARTS ? BATCH : 1], pf[PARTS ? BATCH : 1];
 #pragma unroll
     for (int u = 0; u < BATCH; ++u) {
       const int j = j0 + u * rows_at_once + sub;
-      if (j < last && active) {
+      if (PARTS && j >= a.hq) {
+        if (j < last) {
+          const bool value = j >= a.hq + a.hk;
+          const size_t width = (size_t)a.hk * a.d, slab = width * a.rows;
+          const float *src = a.parts + (value ? slab : 0) + (size_t)row * width + (size_t)(j - a.hq - (value ? a.hk : 0)) * a.d;
+          sum_parts(src, 2 * slab, a.shares, e0, xf[PARTS ? u : 0]);
+          if (!value && !a.rotary.interleaved && e0 < rot) {
+            if (whole) {
+              sum_parts(src, 2 * slab, a.shares, e0 < half ? e0 + half : e0 - half, pf[PARTS ? u : 0]);
+            } else {
+#pragma unroll
+              for (int i = 0; i < 8; ++i) {
+                const int e = e0 + i;
+                float sum = 0.f;
+                if (e < rot)
+                  for (int k = 0; k < a.shares; ++k) sum += src[k * 2 * slab + (e < half ? e + half : e - half)];
+                pf[PARTS ? u : 0].set(i, sum);
+              }
+            }
+          }
+        }
+      } else if (j < last && active) {
         const T *src = j < a.hq ? (const T *)a.Q + ((size_t)row * a.hq + j) * a.d
                        : j < a.hq + a.hk ? (const T *)a.K + ((size_t)row * a.hk + (j - a.hq)) * a.d
                                          : (const T *)a.V + ((size_t)row * a.hk + (j - a.hq - a.hk)) * a.d;
@@ -144,7 +183,9 @@ __global__ void __launch_bounds__(64 * WAVES) turn_rows_kernel(TurnArgs a, smoe_
       float y[8];
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        const float v = x[u].get(i), other = a.rotary.interleaved ? x[u].get(i ^ 1) : p[u].get(i);
+        const bool part = PARTS && j >= a.hq;
+        const float v = part ? xf[PARTS ? u : 0].get(i) : x[u].get(i);
+        const float other = a.rotary.interleaved ? (part ? xf[PARTS ? u : 0].get(i ^ 1) : x[u].get(i ^ 1)) : (part ? pf[PARTS ? u : 0].get(i) : p[u].get(i));
         y[i] = turned && e0 + i < rot ? fmaf(other, si[i], v * co[i]) : v;
       }
       if (CACHE < 0 || j < a.hq) {
@@ -244,8 +285,8 @@ int launch_turn(hipStream_t s, smoe_dtype dt, const TurnArgs &a) {
   const Work w = deal(a.rows, a.hq + a.hk, a.d);
   unsigned int blocks;
   if (!grid_of(w, a.rows, blocks)) return SMOE_ERR_UNSUPPORTED;
-  if (dt == SMOE_BF16) turn_rows_kernel<bf16_t, -1><<<blocks, 64 * WAVES, 0, s>>>(a, smoe_cache{}, smoe_places{}, w, 1, 0);
-  else turn_rows_kernel<float, -1><<<blocks, 64 * WAVES, 0, s>>>(a, smoe_cache{}, smoe_places{}, w, 1, 0);
+  if (dt == SMOE_BF16) turn_rows_kernel<bf16_t, -1, false><<<blocks, 64 * WAVES, 0, s>>>(a, smoe_cache{}, smoe_places{}, w, 1, 0);
+  else turn_rows_kernel<float, -1, false><<<blocks, 64 * WAVES, 0, s>>>(a, smoe_cache{}, smoe_places{}, w, 1, 0);
   SMOE_LAUNCH_CHECK();
   return SMOE_OK;
 }
@@ -255,8 +296,9 @@ int launch_cache_append(hipStream_t s, const TurnArgs &a, const smoe_cache &c, c
   unsigned int blocks;
   if (!grid_of(w, a.rows, blocks)) return SMOE_ERR_UNSUPPORTED;
   const int N = p.lens ? a.rows / p.sequences : 1, shift = log2_of(c.page);
-  if (c.format == SMOE_CACHE_BF16) turn_rows_kernel<bf16_t, SMOE_CACHE_BF16><<<blocks, 64 * WAVES, 0, s>>>(a, c, p, w, N, shift);
-  else turn_rows_kernel<bf16_t, SMOE_CACHE_E4M3><<<blocks, 64 * WAVES, 0, s>>>(a, c, p, w, N, shift);
+  auto go = [&](auto kernel) { kernel<<<blocks, 64 * WAVES, 0, s>>>(a, c, p, w, N, shift); };
+  if (c.format == SMOE_CACHE_BF16) a.parts ? go(turn_rows_kernel<bf16_t, SMOE_CACHE_BF16, true>) : go(turn_rows_kernel<bf16_t, SMOE_CACHE_BF16, false>);
+  else a.parts ? go(turn_rows_kernel<bf16_t, SMOE_CACHE_E4M3, true>) : go(turn_rows_kernel<bf16_t, SMOE_CACHE_E4M3, false>);
   SMOE_LAUNCH_CHECK();
   return SMOE_OK;
 }

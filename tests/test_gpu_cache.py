@@ -526,6 +526,66 @@ def test_decoding_continues_the_layer(smoe, B, P, new, N, k, h, quantised):
         assert err <= (2 * TOL[torch.bfloat16] if not quantised else 2.0 ** -3), (t, err)
 
 
+@pytest.mark.parametrize("lens,N,d_model,E,k,h,d,rot,quantised", [
+    ([40, 3, 17], 1, 256, 8, 2, 2, 128, 128, False), ([1], 1, 64, 4, 4, 1, 64, 0, False), ([9, 30], 2, 104, 4, 2, 1, 64, 20, False), ([25] * 70, 1, 128, 8, 2, 1, 64, 64, False),
+    ([20] * 45, 3, 96, 4, 1, 2, 64, 0, False), ([50, 0, 1, 64, 33], 2, 2080, 4, 3, 3, 64, 64, True), ([30] * 20, 1, 160, 16, 8, 2, 128, 128, True)])
+def test_decoding_layer_sizes(smoe, lens, N, d_model, E, k, h, d, rot, quantised):
+    """The layer's decoding pass against the oracle's pieces: rows in one and several tiles, widths that fill a block of columns or not, contractions
+    off the steps of 32, more rows than the small dense kernel takes, fewer positions than new tokens.  Tolerance: that of the layer's other
+    tests, of the largest entry; for a cache in 8 bits another 2^-4, half a step of its values, and as much for the keys'."""
+    _log(f"decode layer B={len(lens)} N={N} d_model={d_model} E={E} k={k} h={h} d={d} rot={rot} e4m3={quantised}")
+    B, page = len(lens), 16
+    M = B * N
+    w = _layer(d_model, E, h, 211, d)
+    before = [max(0, n - N) for n in lens]
+    cache, table, K, V = _case(smoe, before, page, h, d, quantised, 215, width=-(-max(lens) // page) + 1, behind=0)
+    need = [-(-n // page) for n in lens]
+    pages = cache.pages
+    # pages of their own for all positions, the old ones moved there
+    fresh = smoe.kv_cache(sum(need) + 1, page, h, d, quantised)
+    at, new_table = 0, torch.zeros_like(table)
+    for b, n in enumerate(need):
+        new_table[b, :n] = torch.arange(at, at + n)
+        at += n
+    seqs = torch.tensor([b for b, n in enumerate(before) for _ in range(n)], dtype=torch.int32)
+    pos = torch.tensor([p for n in before for p in range(n)], dtype=torch.int32)
+    if len(seqs):
+        old = smoe.cache_read(cache, table.cuda(), seqs=seqs.cuda(), positions=pos.cuda())
+        smoe.cache_append(fresh, *old, new_table.cuda(), seqs=seqs.cuda(), positions=pos.cuda())
+    X, logits = _normal((M, d_model), 216), _normal((M, E), 217, torch.float32)
+    ei, g = smoe.topk_gate(logits.cuda(), k)
+    rotary = smoe.rotary_table(rot) if rot else None
+    told = torch.tensor(lens, dtype=torch.int32)
+    O = smoe.momha_decode(X.cuda(), w["W_K"], w["W_V"], w["W_Q"], w["W_O"], smoe.route(ei, E), k, g, fresh, new_table.cuda(), told.cuda(), rotary=rotary)
+    oei, og = oracle.topk_gate(logits.numpy(), k)
+    assert np.array_equal(ei.cpu().numpy(), oei)
+    x, W = _f64(X), {n: _f64(t) for n, t in w.items()}
+    newK, newV = (x @ W[n] for n in ("W_K", "W_V"))
+    newQ = np.stack([[x[m] @ W["W_Q"][e] for e in oei[m]] for m in range(M)]).reshape(M, k * h, d)
+    at = (told.long()[:, None] - N + torch.arange(N)).reshape(-1).numpy()
+    newK = newK.reshape(M, h, d)
+    if rot:
+        freqs, _ = oracle.rotary_frequencies(rot)
+        newK, newQ = oracle.rotate_rows(newK, at, freqs), oracle.rotate_rows(newQ, at, freqs)
+    full = lambda old, new: [np.concatenate([old[b], new[b * N:(b + 1) * N][max(0, N - lens[b]):]]) for b in range(B)]
+    att, _ = oracle.cached_attention(newQ.reshape(B, N, k, h, d), full(K, newK), full(V, newV.reshape(M, h, d)), lens)
+    att = att.reshape(M, k, h * d)
+    want = np.stack([sum(og[m, j] * (att[m, j] @ W["W_O"][e]) for j, e in enumerate(oei[m])) for m in range(M)])
+    err = np.abs(_f64(O) - want).max() / np.abs(want).max()
+    _log(f"  error {err:.2e}")
+    assert err <= TOL[torch.bfloat16] + (2 * 2.0 ** -4 if quantised else 0)
+    # the new rows are in the cache, the keys turned
+    k_row, v_row = (_f64(t) for t in smoe.cache_read(fresh, new_table.cuda(), lens=told.cuda(), N=N))
+    real = at >= 0
+    for got, ref in ((k_row, newK), (v_row, newV.reshape(M, h, d))):
+        # A projection may be rounded to bf16 before it is turned: a' = a cos w - b sin w is then off by 2^-8 (|a| + |b|), and
+        # |a| + |b| <= sqrt(2) |(a, b)| = sqrt(2) |(a', b')| <= 2 max |a'| over the row.  What is stored is rounded once more, by half a step of
+        # its type (2^-4 in e4m3, or half its smallest step, 2^-10 at a scale of at most max / 224).  Sums in fp32: 2^-15 of the largest.
+        scale = np.abs(ref).max(-1, keepdims=True)
+        tol = (2.0 ** -4 if quantised else HALF_STEP) * np.abs(ref) * (1 + HALF_STEP) + (2 * HALF_STEP + 2.0 ** -15) * scale + (2.0 ** -10 / 224 * scale if quantised else 0)
+        assert (np.abs(got - ref)[real] <= tol[real]).all() and not got[~real].any()
+
+
 def test_prefill_and_decoding_with_positions(smoe):
     """Rotary prefill (turn, causal attention, append), then tokens one by one (turn and append in one launch, attention over the cache),
     against the oracle's causal attention over turned rows of the whole sequence."""
