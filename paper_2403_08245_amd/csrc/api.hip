@@ -1040,7 +1040,12 @@ int smoe_momha_decode(smoe_ctx *ctx, void *stream, smoe_dtype dtype, const void 
   float *LSE = (float *)p;  p += z.lse;
   void *Yhat = p;  p += z.yhat;
   hipStream_t s = (hipStream_t)stream;
-  auto product = [&](S2SArgs a) { a.tail_ws = tail_ws; return run_s2s(ctx, s, dtype, a); };
+  const size_t weights = 2 * (size_t)d_model * d_out * 2 * ((size_t)r->E + 1);   // all that the call may read
+  auto product = [&](S2SArgs a) {
+    a.tail_ws = tail_ws;
+    a.call_weights = weights;
+    return run_s2s(ctx, s, dtype, a);
+  };
   rc = product(make_s2s(X, W_Q, Q, r, d_model, d_out, false, false, k, false));   // first: it may leave partial tiles where the shares go next
   if (rc != SMOE_OK) return rc;
   TurnArgs t;
