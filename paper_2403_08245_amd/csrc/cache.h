@@ -22,7 +22,7 @@ int launch_cache_append(hipStream_t s, const TurnArgs &a, const smoe_cache &c, c
 int launch_cache_read(hipStream_t s, const smoe_cache &c, const smoe_places &p, int rows, void *K, void *V);
 
 // Two dense products X [M, K] W [K, N] of few rows, left as shares of the contraction, P [shares][2][M][N] fp32 (gemm_skinny.hip).
-constexpr int SKINNY_MAX_ROWS = 128;
+constexpr int SKINNY_MAX_ROWS = 512;
 int skinny_shares(int M, int K, int N);      // 0: not for this kernel
 int launch_skinny_pair(hipStream_t s, const void *X, const void *W0, const void *W1, int M, int K, int N, int shares, float *P);
 

@@ -101,6 +101,10 @@ template <int MT> __global__ void __launch_bounds__(64 * SWAVES, 2) skinny_pair_
 
 }  // namespace
 
+// The line at 512 rows: the attention layer's decoding pass in us, these kernels / the persistent ones (up to 32 rows the decoding ones), 2048
+// wide, 16 experts, k = 4, 4 heads: 4 rows 41 / 59, 64 rows 58 / 76, 128 rows 76 / 93, 256 rows 126 / 140, 512 rows 120 / 135 (shorter
+// contexts); 4096 wide, 64 experts, k = 8: 128 rows 163 / 176, 256 rows 223 / 239, 512 rows 218 / 230.  They win wherever tried; past that the shares
+// outgrow their room and the large tiles fill the chip.
 int skinny_shares(int M, int K, int N) {
   if (M < 1 || M > SKINNY_MAX_ROWS || K < HK || K % HK || N % 8) return 0;
   // a step or two for each wavefront, and about a block for each compute unit at most
