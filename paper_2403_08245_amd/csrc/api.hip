@@ -1012,7 +1012,8 @@ size_t smoe_momha_decode_workspace_bytes(int B, int N, int k, int d_model, int h
   const size_t attention = smoe_cached_attention_workspace_bytes(B, N, k, h_expert, d_head);
   if (!attention || d_model < 1) return 0;
   MomhaSizes z = momha_sizes(B, N, k, d_model, h_expert, d_head);
-  return 256 + S2S_TAIL_WS_BYTES + 2 * z.kv + z.q + z.lse + z.yhat + attention;   // the shares of K and V lie where partial tiles do
+  // Q and Yhat in fp32 where the products are the decoding kernels'; the shares of K and V lie where partial tiles do
+  return 256 + S2S_TAIL_WS_BYTES + 2 * z.kv + 3 * z.q + z.lse + 2 * z.yhat + attention;
 }
 
 int smoe_momha_decode(smoe_ctx *ctx, void *stream, smoe_dtype dtype, const void *X, int N, int d_model, const void *W_K, const void *W_V,
@@ -1026,7 +1027,7 @@ int smoe_momha_decode(smoe_ctx *ctx, void *stream, smoe_dtype dtype, const void 
   const int B = places->sequences, h = cache->h, d_head = cache->d_head;
   if ((long long)B * N * k != r->Tk) return SMOE_ERR_INVALID_ARG;
   const size_t need = smoe_momha_decode_workspace_bytes(B, N, k, d_model, h, d_head);
-  if (dtype != SMOE_BF16 || !width_ok(dtype, d_model) || !need || (long long)k * h > 65535) return SMOE_ERR_UNSUPPORTED;
+  if (dtype != SMOE_BF16 || !width_ok(dtype, d_model) || !need || (long long)k * h > 65535 || !cache_append_fits(B * N, k * h, h, d_head)) return SMOE_ERR_UNSUPPORTED;
   if (!aligned16(X) || !aligned16(W_K) || !aligned16(W_V) || !aligned16(W_Q) || !aligned16(W_O) || !aligned16(O)) return SMOE_ERR_UNSUPPORTED;
   if (!ws || ((uintptr_t)ws & 255) || ws_bytes < need) return SMOE_ERR_WORKSPACE;
   const int M = B * N, d_out = h * d_head;
@@ -1036,17 +1037,27 @@ int smoe_momha_decode(smoe_ctx *ctx, void *stream, smoe_dtype dtype, const void 
   float *tail_ws = (float *)p;  p += S2S_TAIL_WS_BYTES;
   void *K = p;  p += z.kv;
   void *V = p;  p += z.kv;
-  void *Q = p;  p += z.q;              // turned in place, then the attention's output in its place
+  void *Q = p;  p += 2 * z.q;          // turned in place
+  void *Ohat = p;  p += z.q;
   float *LSE = (float *)p;  p += z.lse;
-  void *Yhat = p;  p += z.yhat;
+  void *Yhat = p;  p += 2 * z.yhat;
   hipStream_t s = (hipStream_t)stream;
   const size_t weights = 2 * (size_t)d_model * d_out * 2 * ((size_t)r->E + 1);   // all that the call may read
+  // Of the layer's tensors the decoding kernels leave Q, the shares of K and V, and Yhat in fp32: O then carries two roundings to bf16, its own
+  // and Ohat's, beside the cache's (error against 64 bits 2.3e-3; 3.7e-3 with every tensor rounded, as the
+  // prefill pass does; 64 sequences of the 4096-wide layer 190 -> 194 us).
+  S2SArgs aq = make_s2s(X, W_Q, Q, r, d_model, d_out, false, false, k, false);
+  S2SArgs ao = make_s2s(Ohat, W_O, Yhat, r, d_out, d_model, false, false, 1, false);
+  const int shares = ctx->kernel_mode == 0 ? skinny_shares(M, d_model, d_out) : 0;
+  const bool parts = shares && (size_t)shares * 2 * M * d_out * sizeof(float) <= S2S_TAIL_WS_BYTES;
+  const bool wide = parts && s2s_decode_supported(aq) && s2s_decode_supported(ao);
   auto product = [&](S2SArgs a) {
     a.tail_ws = tail_ws;
     a.call_weights = weights;
+    a.wide = wide;
     return run_s2s(ctx, s, dtype, a);
   };
-  rc = product(make_s2s(X, W_Q, Q, r, d_model, d_out, false, false, k, false));   // first: it may leave partial tiles where the shares go next
+  rc = product(aq);                    // first: it may leave partial tiles where the shares go next
   if (rc != SMOE_OK) return rc;
   TurnArgs t;
   t.Q = t.Qr = rotary ? Q : nullptr;
@@ -1057,8 +1068,8 @@ int smoe_momha_decode(smoe_ctx *ctx, void *stream, smoe_dtype dtype, const void 
   t.rows = M;
   t.d = d_head;
   if (rotary) t.rotary = *rotary;
-  const int shares = ctx->kernel_mode == 0 ? skinny_shares(M, d_model, d_out) : 0;
-  if (shares && (size_t)shares * 2 * M * d_out * sizeof(float) <= S2S_TAIL_WS_BYTES) {
+  t.wide = wide;
+  if (parts) {
     t.parts = tail_ws;
     t.shares = shares;
     rc = launch_skinny_pair(s, X, W_K, W_V, M, d_model, d_out, shares, tail_ws);
@@ -1070,11 +1081,10 @@ int smoe_momha_decode(smoe_ctx *ctx, void *stream, smoe_dtype dtype, const void 
   }
   if (rc == SMOE_OK) rc = launch_cache_append(s, t, *cache, *places);
   if (rc != SMOE_OK) return rc;
-  rc = smoe_cached_attention_fwd(ctx, stream, dtype, Q, N, k, cache, places, Q, LSE, p, need - (size_t)(p - (char *)ws));
+  rc = launch_cached_attention(s, Q, wide, N, k, *cache, *places, Ohat, LSE, p);
+  if (rc == SMOE_OK) rc = product(ao);
   if (rc != SMOE_OK) return rc;
-  rc = product(make_s2s(Q, W_O, Yhat, r, d_out, d_model, false, false, 1, false));
-  if (rc != SMOE_OK) return rc;
-  return launch_combine(s, dtype, Yhat, gates, O, M, k, d_model);
+  return wide ? launch_combine_wide(s, (const float *)Yhat, gates, O, M, k, d_model) : launch_combine(s, dtype, Yhat, gates, O, M, k, d_model);
 }
 
 }  // extern "C"

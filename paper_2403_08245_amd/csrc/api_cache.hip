@@ -121,13 +121,8 @@ int smoe_cache_read(smoe_ctx *ctx, void *stream, smoe_dtype dtype, const smoe_ca
   return launch_cache_read((hipStream_t)stream, *cache, *places, rows, K, V);
 }
 
-static bool attention_sizes_ok(int B, int N, int G, int h) {
-  // rows of Q within 31 bits, and one-dimensional grids
-  return (long long)N * G <= 0x7fffffffLL && (long long)B * N * G <= 0x7fffffffLL / h && h <= 65535;
-}
-
 size_t smoe_cached_attention_workspace_bytes(int B, int N, int G, int h, int d_head) {
-  if (B < 1 || N < 1 || G < 1 || h < 1 || (d_head != 64 && d_head != 128) || !attention_sizes_ok(B, N, G, h)) return 0;
+  if (B < 1 || N < 1 || G < 1 || h < 1 || (d_head != 64 && d_head != 128) || h > 65535 || !cached_attention_fits(B, N, G, h)) return 0;
   return align256(cached_attention_workspace_bytes(N, G, d_head));
 }
 
@@ -137,12 +132,12 @@ int smoe_cached_attention_fwd(smoe_ctx *ctx, void *stream, smoe_dtype dtype, con
   int rc = cache_args_ok(cache);
   if (rc == SMOE_OK) rc = lengths_ok(cache, places);
   if (rc != SMOE_OK) return rc;
-  if (dtype != SMOE_BF16 || !attention_sizes_ok(places->sequences, N, G, cache->h)) return SMOE_ERR_UNSUPPORTED;
+  if (dtype != SMOE_BF16 || !cached_attention_fits(places->sequences, N, G, cache->h)) return SMOE_ERR_UNSUPPORTED;
   if (!aligned16(Q) || !aligned16(O)) return SMOE_ERR_UNSUPPORTED;
   if (!ws || ((uintptr_t)ws & 255) || ws_bytes < smoe_cached_attention_workspace_bytes(places->sequences, N, G, cache->h, cache->d_head)) return SMOE_ERR_WORKSPACE;
   const size_t bytes = (size_t)places->sequences * N * G * cache->h * cache->d_head * 2;
   if (O != Q && overlap(O, bytes, Q, bytes)) return SMOE_ERR_INVALID_ARG;
-  return launch_cached_attention((hipStream_t)stream, Q, N, G, *cache, *places, O, LSE, ws);
+  return launch_cached_attention((hipStream_t)stream, Q, false, N, G, *cache, *places, O, LSE, ws);
 }
 
 }  // extern "C"

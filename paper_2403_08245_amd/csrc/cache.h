@@ -16,8 +16,10 @@ struct TurnArgs {
   // With a cache: K and V as fp32 shares [shares][2][rows][hk * d] that add up to them (launch_skinny_pair), in the place of bf16 rows.
   const float *parts = nullptr;
   int shares = 0;
+  bool wide = false;                      // with shares: Q and Qr are fp32
 };
 int launch_turn(hipStream_t s, smoe_dtype dt, const TurnArgs &a);
+bool cache_append_fits(int rows, int hq, int hk, int d);   // into one launch, however the rows come
 int launch_cache_append(hipStream_t s, const TurnArgs &a, const smoe_cache &c, const smoe_places &p);
 int launch_cache_read(hipStream_t s, const smoe_cache &c, const smoe_places &p, int rows, void *K, void *V);
 
@@ -26,8 +28,10 @@ constexpr int SKINNY_MAX_ROWS = 512;
 int skinny_shares(int M, int K, int N);      // 0: not for this kernel
 int launch_skinny_pair(hipStream_t s, const void *X, const void *W0, const void *W1, int M, int K, int N, int shares, float *P);
 
+bool cached_attention_fits(int B, int N, int G, int h);   // into one launch
 size_t cached_attention_workspace_bytes(int N, int G, int d_head);
-int launch_cached_attention(hipStream_t s, const void *Q, int N, int G, const smoe_cache &c, const smoe_places &p, void *O, float *LSE, void *ws);
+// wide: Q is fp32 (and not O), and meets the keys as two bf16 numbers
+int launch_cached_attention(hipStream_t s, const void *Q, bool wide, int N, int G, const smoe_cache &c, const smoe_places &p, void *O, float *LSE, void *ws);
 
 // What the entry points ask of a cache, its places and a rotary table, before anything is enqueued (host).
 int cache_args_ok(const smoe_cache *c);

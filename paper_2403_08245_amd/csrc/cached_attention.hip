@@ -318,11 +318,23 @@ template <int D> struct Columns {
 
 // ------------------------------------------------------------------------------------------------ one piece
 // ONE: a single new token a sequence, so that every position within the length is seen by every query.
-template <int D, int FORMAT, int RT, bool ONE, bool ONCE>
+// WIDE: the queries are fp32, and meet the keys as two bf16 numbers.
+template <int D, int FORMAT, int RT, bool ONE, bool ONCE, bool WIDE>
 __global__ void __launch_bounds__(64 * WAVES, RT == 1 && ONE ? 3 : 2)
-    cached_attention_kernel(const bf16_t *Q, smoe_cache c, smoe_places p, Dims d, bf16_t *O, float *LSE, float *ws) {
+    cached_attention_kernel(const void *Q, smoe_cache c, smoe_places p, Dims d, bf16_t *O, float *LSE, float *ws) {
   constexpr int KS = D / 32, COLS = D / 16, ROW = D + 4;     // padded: a wavefront's 16 rows start in 16 different banks
-  __shared__ __attribute__((aligned(16))) float s_acc[WAVES][RT * 16][ROW];
+  // The queries' fragments: in registers, or, two tiles of them or two numbers each, in LDS, until the piece ends (held in registers they
+  // spilled, and a reload in the loop waits for every request under way: two sequences of 90001 and 131072 positions in e4m3 133 us).
+  constexpr bool SHARED = RT > 1 || WIDE;
+  constexpr int FRAGS = RT * KS * (WIDE ? 2 : 1);
+  union Shared {
+    float acc[WAVES][RT * 16][ROW];
+    bf16x8 q[SHARED ? FRAGS : 1][64];
+  };
+  __shared__ __attribute__((aligned(16))) char s_mem[sizeof(Shared)];
+  Shared &shared = *reinterpret_cast<Shared *>(s_mem);
+  auto &s_acc = shared.acc;
+  auto &s_q = shared.q;
   __shared__ float s_m[WAVES][RT * 16], s_l[WAVES][RT * 16];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
   const int col = lane & 15, g = lane >> 4;
@@ -346,19 +358,30 @@ __global__ void __launch_bounds__(64 * WAVES, RT == 1 && ONE ? 3 : 2)
   // the lane's query of each 16, and the first position it does not see
   const int row0 = tile * RT * 16, rows = min(RT * 16, d.R - row0);
   int seen[RT], token[RT];
-  // The queries' fragments: in registers, or, two tiles of them, in LDS (held in registers they spilled, and a reload in the loop waits
-  // for every request under way: two sequences of 90001 and 131072 positions in e4m3 133 us).
-  __shared__ __attribute__((aligned(16))) bf16x8 s_q[RT > 1 ? RT * KS : 1][64];
-  bf16x8 q[RT][KS];
+  bf16x8 q[RT][KS], q_low[WIDE ? RT : 1][KS];
 #pragma unroll
   for (int t = 0; t < RT; ++t) {
     const int r = row0 + min(t * 16 + col, rows - 1);
     token[t] = r / d.G;
     seen[t] = len - d.N + token[t] + 1;
-    const bf16_t *src = Q + (((size_t)b * d.R + r) * c.h + hh) * D;
+    const size_t src = (((size_t)b * d.R + r) * c.h + hh) * D;
 #pragma unroll
-    for (int ks = 0; ks < KS; ++ks)
-      if (RT == 1 || (t * KS + ks) % WAVES == wave) q[t][ks] = *reinterpret_cast<const bf16x8 *>(src + Keys<D, FORMAT>::query_offset(ks, lane));
+    for (int ks = 0; ks < KS; ++ks) {
+      if (SHARED && (t * KS + ks) % WAVES != wave) continue;       // a wavefront's share of them
+      const size_t e = src + Keys<D, FORMAT>::query_offset(ks, lane);
+      if constexpr (WIDE) {
+        const f32x4 *x = reinterpret_cast<const f32x4 *>((const float *)Q + e);
+        const f32x4 lo = x[0], hi = x[1];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const float y = i < 4 ? lo[i] : hi[i - 4];
+          q[t][ks][i] = (bf16_t)y;
+          q_low[t][ks][i] = (bf16_t)(y - (float)q[t][ks][i]);
+        }
+      } else {
+        q[t][ks] = *reinterpret_cast<const bf16x8 *>((const bf16_t *)Q + e);
+      }
+    }
   }
   const int token0 = row0 / d.G, token1 = (row0 + rows - 1) / d.G;
   const int all_see = len - d.N + token0 + 1;               // every query of the tile sees the keys before this one
@@ -408,10 +431,13 @@ __global__ void __launch_bounds__(64 * WAVES, RT == 1 && ONE ? 3 : 2)
   for (int t = 0; t < 2; ++t) k.template load<ONCE>(t, now[t], k_at, lane);
 #pragma unroll
   for (int t = 0; t < 2; ++t) v.template load<ONCE>(t, now[t], v_at, lane);
-  if (RT > 1) {
+  if (SHARED) {
 #pragma unroll
     for (int f = 0; f < RT * KS; ++f)
-      if (f % WAVES == wave) s_q[f][lane] = q[f / KS][f % KS];
+      if (f % WAVES == wave) {
+        s_q[f][lane] = q[f / KS][f % KS];
+        if constexpr (WIDE) s_q[RT * KS + f][lane] = q_low[f / KS][f % KS];
+      }
     __syncthreads();
   }
   int i = 1;                // which of the wavefront's steps is next
@@ -431,7 +457,10 @@ __global__ void __launch_bounds__(64 * WAVES, RT == 1 && ONE ? 3 : 2)
       for (int ks = 0; ks < KS; ++ks) {
         const bf16x8 f = k.frag(i, ks);
 #pragma unroll
-        for (int t = 0; t < RT; ++t) sc[t][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f, RT == 1 ? q[t][ks] : s_q[t * KS + ks][q_at], sc[t][i], 0, 0, 0);
+        for (int t = 0; t < RT; ++t) {
+          sc[t][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f, SHARED ? s_q[t * KS + ks][q_at] : q[t][ks], sc[t][i], 0, 0, 0);
+          if constexpr (WIDE) sc[t][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f, s_q[RT * KS + t * KS + ks][q_at], sc[t][i], 0, 0, 0);
+        }
       }
     }
 #pragma unroll
@@ -518,6 +547,7 @@ __global__ void __launch_bounds__(64 * WAVES, RT == 1 && ONE ? 3 : 2)
 #pragma unroll 1
   while (s < step1) take_step(std::true_type{});
 
+  if (SHARED) __syncthreads();                // the queries are done with
   // The wavefronts' parts meet in LDS.  A lane holds columns 4 COLS g + COLS e + j of its query, j and e running.
 #pragma unroll
   for (int t = 0; t < RT; ++t) {
@@ -658,12 +688,19 @@ int row_tiles(int R) { return R > 16 ? 2 : 1; }
 }  // namespace
 
 constexpr size_t MAX_SLOTS = 2 * MAX_TARGET;
+bool cached_attention_fits(int B, int N, int G, int h) {
+  // query rows within 31 bits, and one-dimensional grids of fewer than 2^32 threads
+  const long long R = (long long)N * G;
+  return R <= 0x7fffffffLL && B * (double)R * h <= 0x7fffffff &&
+         (long long)ceil_div((int)R, 16 * row_tiles((int)R)) * h * B <= 0x7fffffffLL / 256 - 2 * MAX_TARGET;
+}
+
 size_t cached_attention_workspace_bytes(int N, int G, int d_head) {
   const long long R = (long long)N * G;
   return MAX_SLOTS * slot_floats((int)std::min<long long>(R, 16 * row_tiles((int)std::min<long long>(R, 1 << 20))), d_head) * sizeof(float);
 }
 
-int launch_cached_attention(hipStream_t s, const void *Q, int N, int G, const smoe_cache &c, const smoe_places &p, void *O, float *LSE, void *ws) {
+int launch_cached_attention(hipStream_t s, const void *Q, bool wide, int N, int G, const smoe_cache &c, const smoe_places &p, void *O, float *LSE, void *ws) {
   Dims d;
   d.N = N;
   d.G = G;
@@ -674,7 +711,6 @@ int launch_cached_attention(hipStream_t s, const void *Q, int N, int G, const sm
   d.shift = __builtin_ctz((unsigned int)c.page);
   d.cap = p.width * c.page;
   const long long units = (long long)d.tiles * c.h, all = units * p.sequences;
-  if (all > 0x7fffffffLL / 256 - 2 * MAX_TARGET) return SMOE_ERR_UNSUPPORTED;    // one-dimensional grids
   d.units = (int)units;
   d.target = rt == 1 && N == 1 ? T_ONE : rt == 1 ? T_MULTI : T_TWO;
   d.whole = d.cap <= WHOLE_STEPS * STEP;
@@ -682,7 +718,7 @@ int launch_cached_attention(hipStream_t s, const void *Q, int N, int G, const sm
   // block numbers its unit directly, so the grid is exact
   const long long most = d.whole ? all : std::min<long long>(all + d.target, all * ceil_div(ceil_div(d.cap, STEP), MIN_STEPS));
   auto go = [&](auto kernel, auto join, auto join_few) {
-    kernel<<<(unsigned int)most, 64 * WAVES, 0, s>>>((const bf16_t *)Q, c, p, d, (bf16_t *)O, LSE, (float *)ws);
+    kernel<<<(unsigned int)most, 64 * WAVES, 0, s>>>(Q, c, p, d, (bf16_t *)O, LSE, (float *)ws);
     if (hipGetLastError() != hipSuccess) return SMOE_ERR_HIP;
     if (d.whole) return SMOE_OK;
     const long long cut = std::min<long long>(all, d.target);                  // units, at most
@@ -694,21 +730,22 @@ int launch_cached_attention(hipStream_t s, const void *Q, int N, int G, const sm
     else join<<<grid, 256, 0, s>>>(p, d, c.h, rows_log2, (const float *)ws, (bf16_t *)O, LSE);
     return hipGetLastError() == hipSuccess ? SMOE_OK : SMOE_ERR_HIP;
   };
-  auto by_rows = [&](auto d_c, auto f_c, auto once_c) {
+  auto by_rows = [&](auto d_c, auto f_c, auto once_c, auto wide_c) {
     constexpr int D = decltype(d_c)::value, F = decltype(f_c)::value;
-    constexpr bool ONCE = decltype(once_c)::value;
+    constexpr bool ONCE = decltype(once_c)::value, WIDE = decltype(wide_c)::value;
     auto join = cached_attention_join_kernel<D, 256>, join_few = cached_attention_join_kernel<D, 1024>;
-    return rt > 1   ? go(cached_attention_kernel<D, F, 2, false, ONCE>, join, join_few)
-           : N > 1 ? go(cached_attention_kernel<D, F, 1, false, ONCE>, join, join_few)
-                   : go(cached_attention_kernel<D, F, 1, true, ONCE>, join, join_few);
+    return rt > 1   ? go(cached_attention_kernel<D, F, 2, false, ONCE, WIDE>, join, join_few)
+           : N > 1 ? go(cached_attention_kernel<D, F, 1, false, ONCE, WIDE>, join, join_few)
+                   : go(cached_attention_kernel<D, F, 1, true, ONCE, WIDE>, join, join_few);
   };
+  auto by_wide = [&](auto d_c, auto f_c, auto once_c) { return wide ? by_rows(d_c, f_c, once_c, std::true_type{}) : by_rows(d_c, f_c, once_c, std::false_type{}); };
   // Where one tile holds all rows a key is read by one block, and the next call reads another layer's: past the caches, then, unless the
   // cache is so small that several layers' stay in the last-level cache (256 MB) from one token to the next.  64 sequences of up to 8192
   // positions, 135 MB, read in turn with four more such caches: 33.0 us past the caches, 36.4 through them; 64 of 100 to 8192, 240 MB, 51.2 /
   // 55.9; one of 4096, 17 MB, 11.6 / 11.8 in turn with 35 more, but 15.0 / 13.3 where all stay; one of 301 7.3 / 6.5.
   const size_t held = (size_t)std::min<long long>(c.pages, (long long)p.sequences * p.width) * c.page * c.h * c.d_head * (c.format == SMOE_CACHE_BF16 ? 4 : 2);
   const bool once = d.tiles == 1 && held > LAST_LEVEL_CACHE / 4;
-  auto by_once = [&](auto d_c, auto f_c) { return once ? by_rows(d_c, f_c, std::true_type{}) : by_rows(d_c, f_c, std::false_type{}); };
+  auto by_once = [&](auto d_c, auto f_c) { return once ? by_wide(d_c, f_c, std::true_type{}) : by_wide(d_c, f_c, std::false_type{}); };
   auto by_format = [&](auto d_c) {
     return c.format == SMOE_CACHE_BF16 ? by_once(d_c, std::integral_constant<int, SMOE_CACHE_BF16>{}) : by_once(d_c, std::integral_constant<int, SMOE_CACHE_E4M3>{});
   };

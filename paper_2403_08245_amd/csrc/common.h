@@ -89,6 +89,8 @@ int launch_act_bwd(hipStream_t s, smoe_act act, const void *Hpre, const void *dH
 // Y[t] = sum_j g[t*k+j] * Yhat[t*k+j] (+ more0[t] + more1[t], both or neither); g == nullptr means all ones.
 int launch_combine(hipStream_t s, smoe_dtype dt, const void *Yhat, const float *g, void *Y, int T, int k, int d, const void *more0 = nullptr,
                    const void *more1 = nullptr);
+// the same of fp32 rows, rounded to bf16 once
+int launch_combine_wide(hipStream_t s, const float *Yhat, const float *g, void *Y, int T, int k, int d);
 // out[i] = g[o[i]] * in[o[i] / fan]; g == nullptr means all ones
 int launch_group(hipStream_t s, smoe_dtype dt, const void *in, const int32_t *o, int fan, const float *g,
                  void *out, int Tk, int d);
@@ -184,6 +186,8 @@ struct S2SArgs {      // C[out(i), :] = A[in(i), :] * op(W[e(i)])   for sorted r
   int act = SMOE_ACT_NONE;
   const float *gates = nullptr;
   const int32_t *slots = nullptr;
+  // Decoding kernels, no activation: C is fp32.
+  bool wide = false;
 };
 struct DWArgs {       // dW[e] = sum_{i in segment e} A[i, :]^T B[i, :]   (rows expert-sorted, or read through the row maps)
   const void *A;      // [Tk, M]

@@ -119,9 +119,9 @@ __global__ void __launch_bounds__(256) act_bwd_kernel(const T *__restrict__ Hpre
 // Bound by HBM (the k slot rows are read once): K rows are in flight at once, all of them up to k = 8, and past the caches.  65536
 // rows of 4 KB: k = 3 61.5 -> 54.5 us, 5 59.5 -> 52, 6 59.5 -> 50.5, 7 57 -> 50.5, 12 56 -> 49.5 (one row at a time, through the
 // caches, before); k = 2, 4 and 8 61, 53 and 50.
-template <typename T, int K>
+template <typename T, int K, typename OUT = T>
 __global__ void __launch_bounds__(256) combine_kernel(const T *__restrict__ Yhat, const float *__restrict__ g,
-                                                      T *__restrict__ Y, int T_rows, int k, int d, RowLanes l,
+                                                      OUT *__restrict__ Y, int T_rows, int k, int d, RowLanes l,
                                                       const T *__restrict__ more0, const T *__restrict__ more1) {
   constexpr int V = 16 / sizeof(T);
   const int lane = (int)threadIdx.x & (l.shift == 8 ? 255 : l.lanes - 1);
@@ -153,7 +153,15 @@ __global__ void __launch_bounds__(256) combine_kernel(const T *__restrict__ Yhat
 #pragma unroll
         for (int i = 0; i < V; ++i) acc[i] += a[i] + b[i];
       }
-      store_vec<T>(Y + t * d + c, acc);
+      if constexpr (sizeof(OUT) == sizeof(T)) {
+        store_vec<T>(Y + t * d + c, acc);
+      } else {
+        typedef OUT half_vec __attribute__((ext_vector_type(V)));
+        half_vec r;
+#pragma unroll
+        for (int i = 0; i < V; ++i) r[i] = from_f32<OUT>(acc[i]);
+        *reinterpret_cast<half_vec *>(Y + t * d + c) = r;
+      }
     }
   }
 }
@@ -333,6 +341,18 @@ static int combine_t(hipStream_t s, const void *Yhat, const float *g, void *Y, i
   with_rows(k, [&](auto rows) {
     hipLaunchKernelGGL((combine_kernel<T, decltype(rows)::value>), dim3(blocks), dim3(l.lanes * l.rows), 0, s, (const T *)Yhat, g, (T *)Y, T_rows,
                        k, d, l, (const T *)m0, (const T *)m1);
+  });
+  SMOE_LAUNCH_CHECK();
+  return SMOE_OK;
+}
+int launch_combine_wide(hipStream_t s, const float *Yhat, const float *g, void *Y, int T_rows, int k, int d) {
+  if (!vec_ok<bf16_t>(d)) return SMOE_ERR_UNSUPPORTED;
+  if (T_rows < 1) return SMOE_OK;
+  const RowLanes l = row_lanes(d / 4);
+  const int blocks = row_blocks(T_rows, l.rows);
+  with_rows(k, [&](auto rows) {
+    hipLaunchKernelGGL((combine_kernel<float, decltype(rows)::value, bf16_t>), dim3(blocks), dim3(l.lanes * l.rows), 0, s, Yhat, g, (bf16_t *)Y, T_rows, k, d, l,
+                       (const float *)nullptr, (const float *)nullptr);
   });
   SMOE_LAUNCH_CHECK();
   return SMOE_OK;

@@ -35,8 +35,8 @@ template <int J> __device__ __forceinline__ bf16x8 w_frag(const WStep &w) {
 }
 
 // ACT 0: C = A W.  ACT 1 / 2: fused SwiGLU (a tile is 64 gate columns and the 64 up columns pairing with
-// them), keeping / not keeping the pre-activation.
-template <int ACT, bool SCATTER_OUT, int CW, int KW, bool ONCE>
+// them), keeping / not keeping the pre-activation.  WIDE: C is fp32.
+template <int ACT, bool SCATTER_OUT, int CW, int KW, bool ONCE, bool WIDE = false>
 __global__ void __launch_bounds__(64 * CW * KW, 2) s2s_decode_kernel(S2SArgs a, int n_chunks) {
   __shared__ float s_part[KW][CW][32][64];     // one fragment's sums of every wavefront
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
@@ -192,7 +192,13 @@ __global__ void __launch_bounds__(64 * CW * KW, 2) s2s_decode_kernel(S2SArgs a, 
         total(w, lane, v);
         if (i < row_end && exists(w, g)) {
           const size_t dst = SCATTER_OUT ? (size_t)a.c_map.o[i] : (size_t)i;
-          *reinterpret_cast<bf16x8 *>((bf16_t *)a.C + dst * a.N + column(w, g)) = rounded(v);
+          if constexpr (WIDE) {
+            f32x4 *out = reinterpret_cast<f32x4 *>((float *)a.C + dst * a.N + column(w, g));
+            out[0] = f32x4{v[0], v[1], v[2], v[3]};
+            out[1] = f32x4{v[4], v[5], v[6], v[7]};
+          } else {
+            *reinterpret_cast<bf16x8 *>((bf16_t *)a.C + dst * a.N + column(w, g)) = rounded(v);
+          }
         }
       } else if (CW > 1 || q < 2) {   // one wavefront across: column groups 0..7 are gates, 8..15 (lane + 32) their ups
         float gate[8], up[8], h[8];
@@ -222,6 +228,13 @@ template <int ACT, bool SCATTER_OUT, int CW, int KW> int launch_decode_as(hipStr
   const int n_chunks = ACT ? ceil_div(a.N / 2, CW * DN / 2) : ceil_div(a.N, CW * DN);
   const long long m_bound = a.Tk / DM + a.E;           // >= sum_e ceil(n_e / 32)
   const dim3 grid((unsigned)(m_bound * n_chunks)), block(64 * CW * KW);
+  if constexpr (ACT == 0 && SCATTER_OUT)
+    if (a.wide) {
+      if (weights_pass_caches(a)) hipLaunchKernelGGL((s2s_decode_kernel<ACT, SCATTER_OUT, CW, KW, true, true>), grid, block, 0, s, a, n_chunks);
+      else hipLaunchKernelGGL((s2s_decode_kernel<ACT, SCATTER_OUT, CW, KW, false, true>), grid, block, 0, s, a, n_chunks);
+      SMOE_LAUNCH_CHECK();
+      return SMOE_OK;
+    }
   if (weights_pass_caches(a)) hipLaunchKernelGGL((s2s_decode_kernel<ACT, SCATTER_OUT, CW, KW, true>), grid, block, 0, s, a, n_chunks);
   else hipLaunchKernelGGL((s2s_decode_kernel<ACT, SCATTER_OUT, CW, KW, false>), grid, block, 0, s, a, n_chunks);
   SMOE_LAUNCH_CHECK();
@@ -267,7 +280,7 @@ bool s2s_decode_supported(const S2SArgs &a) {
 }
 
 int launch_s2s_decode(hipStream_t s, const S2SArgs &a) {
-  if (!s2s_decode_supported(a)) return SMOE_ERR_UNSUPPORTED;
+  if (!s2s_decode_supported(a) || (a.wide && (a.H || !a.c_map.o))) return SMOE_ERR_UNSUPPORTED;
   if (a.H) return a.C ? launch_decode<1, false>(s, a) : launch_decode<2, false>(s, a);
   return a.c_map.o ? launch_decode<0, true>(s, a) : launch_decode<0, false>(s, a);
 }

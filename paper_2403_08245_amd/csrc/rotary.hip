@@ -107,8 +107,9 @@ __device__ __forceinline__ uint2 to_e4m3(float (&y)[8], int lanes, unsigned int 
   return q;
 }
 
-// CACHE: -1 none (Q and K go to Qr and Kr), else the cache's format, and the rows of K and V go there.  PARTS: those rows come as fp32 shares.
-template <typename T, int CACHE, bool PARTS>
+// CACHE: -1 none (Q and K go to Qr and Kr), else the cache's format, and the rows of K and V go there.  PARTS: those rows come as fp32 shares, and those of
+// Q, with WIDE, as fp32.
+template <typename T, int CACHE, bool PARTS, bool WIDE = false>
 __global__ void __launch_bounds__(64 * WAVES) turn_rows_kernel(TurnArgs a, smoe_cache c, smoe_places places, Work w, int N, int page_shift) {
   __shared__ float2 s_angle[WAVES][MAX_PAIRS];
   constexpr int AHEAD = PARTS ? 1 : BATCH;        // a decoding pass has few rows for many wavefronts
@@ -123,7 +124,7 @@ __global__ void __launch_bounds__(64 * WAVES) turn_rows_kernel(TurnArgs a, smoe_
   const int total = a.hq + a.hk + (CACHE >= 0 ? a.hk : 0), end = min((item.group + 1) * w.per, total);
 
   Eight<T> x[AHEAD], p[AHEAD];                    // elements, and their partners where those are another chunk's
-  Eight<float> xf, pf;                            // the same as sums of shares
+  Eight<float> xf, pf;                            // the same in fp32: sums of shares, wide queries
   auto mine = [&](int j) { return j < end && sub < w.at_once; };
   auto load = [&](int u, int j) {
     if (!mine(j)) return;
@@ -146,6 +147,21 @@ __global__ void __launch_bounds__(64 * WAVES) turn_rows_kernel(TurnArgs a, smoe_
 #pragma unroll
         for (int t = 0; t < 8; ++t)
           if (t == i) pf.set(t, sum);
+      }
+      return;
+    }
+    if (WIDE) {
+      const float *src = (const float *)a.Q + ((size_t)row * a.hq + j) * a.d;
+      xf.load(src + e0);
+      if (a.rotary.interleaved || e0 >= rot) return;
+      if (whole) {
+        pf.load(src + (e0 < half ? e0 + half : e0 - half));
+        return;
+      }
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const int e = e0 + i;
+        pf.set(i, e < rot ? src[e < half ? e + half : e - half] : 0.f);
       }
       return;
     }
@@ -204,7 +220,7 @@ __global__ void __launch_bounds__(64 * WAVES) turn_rows_kernel(TurnArgs a, smoe_
 #pragma unroll
     for (int u = 0; u < AHEAD; ++u) {
       const int j = j0 + u * w.at_once;
-      const bool turned = j < a.hq + a.hk, part = PARTS && j >= a.hq;
+      const bool turned = j < a.hq + a.hk, part = PARTS && (WIDE || j >= a.hq);
       float y[8];
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
@@ -213,7 +229,11 @@ __global__ void __launch_bounds__(64 * WAVES) turn_rows_kernel(TurnArgs a, smoe_
         y[i] = turned && e0 + i < rot ? fmaf(other, si[i], v * co[i]) : v;
       }
       if (CACHE < 0 || j < a.hq) {
-        if (mine(j)) {
+        if (WIDE && mine(j)) {
+#pragma unroll
+          for (int i = 0; i < 8; ++i) xf.set(i, y[i]);
+          xf.store((float *)a.Qr + ((size_t)row * a.hq + j) * a.d + e0);
+        } else if (mine(j)) {
           T *dst = j < a.hq ? (T *)a.Qr + ((size_t)row * a.hq + j) * a.d : (T *)a.Kr + ((size_t)row * a.hk + (j - a.hq)) * a.d;
 #pragma unroll
           for (int i = 0; i < 8; ++i) x[u].set(i, y[i]);
@@ -381,6 +401,11 @@ template <bool WRITE> int launch_rows(hipStream_t s, const smoe_cache &c, const 
 }
 }  // namespace
 
+bool cache_append_fits(int rows, int hq, int hk, int d) {
+  unsigned int blocks;
+  return grid_of(deal(rows, hq + 2 * hk, d, 1), rows, blocks);   // a round of rows each: the most wavefronts
+}
+
 int launch_cache_append(hipStream_t s, const TurnArgs &a, const smoe_cache &c, const smoe_places &p) {
   if (!a.rotary.turns && !a.parts) return launch_rows<true>(s, c, p, a.rows, (void *)a.K, (void *)a.V);
   const Work w = deal(a.rows, a.hq + 2 * a.hk, a.d, a.parts ? 1 : MOST);
@@ -388,8 +413,14 @@ int launch_cache_append(hipStream_t s, const TurnArgs &a, const smoe_cache &c, c
   if (!grid_of(w, a.rows, blocks)) return SMOE_ERR_UNSUPPORTED;
   const int N = p.lens ? a.rows / p.sequences : 1, shift = log2_of(c.page);
   auto go = [&](auto kernel) { kernel<<<blocks, 64 * WAVES, 0, s>>>(a, c, p, w, N, shift); };
-  if (c.format == SMOE_CACHE_BF16) a.parts ? go(turn_rows_kernel<bf16_t, SMOE_CACHE_BF16, true>) : go(turn_rows_kernel<bf16_t, SMOE_CACHE_BF16, false>);
-  else a.parts ? go(turn_rows_kernel<bf16_t, SMOE_CACHE_E4M3, true>) : go(turn_rows_kernel<bf16_t, SMOE_CACHE_E4M3, false>);
+  auto by_format = [&](auto f_c) {
+    constexpr int F = decltype(f_c)::value;
+    if (!a.parts) go(turn_rows_kernel<bf16_t, F, false>);
+    else if (a.wide) go(turn_rows_kernel<bf16_t, F, true, true>);
+    else go(turn_rows_kernel<bf16_t, F, true>);
+  };
+  if (c.format == SMOE_CACHE_BF16) by_format(std::integral_constant<int, SMOE_CACHE_BF16>{});
+  else by_format(std::integral_constant<int, SMOE_CACHE_E4M3>{});
   SMOE_LAUNCH_CHECK();
   return SMOE_OK;
 }

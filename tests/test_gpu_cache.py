@@ -529,7 +529,7 @@ def test_decoding_continues_the_layer(smoe, B, P, new, N, k, h, quantised):
 @pytest.mark.parametrize("lens,N,d_model,E,k,h,d,rot,quantised", [
     ([40, 3, 17], 1, 256, 8, 2, 2, 128, 128, False), ([1], 1, 64, 4, 4, 1, 64, 0, False), ([9, 30], 2, 104, 4, 2, 1, 64, 20, False), ([25] * 70, 1, 128, 8, 2, 1, 64, 64, False),
     ([20] * 45, 3, 96, 4, 1, 2, 64, 0, False), ([50, 0, 1, 64, 33], 2, 2080, 4, 3, 3, 64, 64, True), ([30] * 20, 1, 160, 16, 8, 2, 128, 128, True),
-    ([9] * 260, 2, 64, 4, 1, 1, 64, 64, False)])
+    ([9] * 260, 2, 64, 4, 1, 1, 64, 64, False), ([21, 2, 40], 1, 96, 8, 3, 2, 64, 20, False), ([40, 7], 3, 64, 32, 8, 1, 128, 52, True)])
 def test_decoding_layer_sizes(smoe, lens, N, d_model, E, k, h, d, rot, quantised):
     """The layer's decoding pass against the oracle's pieces: rows in one and several tiles, widths that fill a block of columns or not, contractions
     off the steps of 32, more rows than the small dense kernel takes, fewer positions than new tokens.  Tolerance: that of the layer's other
