@@ -104,8 +104,10 @@ int smoe_cache_read(smoe_ctx *ctx, void *stream, smoe_dtype dtype, const smoe_ca
  * A query with p < 0, or whose visible scores are all -infinity, attends nothing: O = 0, LSE = -infinity.  What lies in the cache at
  * positions that a query does not see never reaches it, NaN and infinities included.  Lengths count as at most width * page, and
  * positions on pages outside [0, pages) are not seen.
- * The places' seqs and positions are not read (NULL).  B >= 1, N >= 1, G >= 1.  O may be Q. */
-size_t smoe_cached_attention_workspace_bytes(int B, int N, int G, int h, int d_head);
+ * The places' seqs and positions are not read (NULL).  N >= 1, G >= 1.  O may be Q.  The workspace holds the partial sums of sequences that
+ * several blocks share; none is needed (0, ws may be NULL) where the table holds at most 512 positions.  The query looks at sizes only, and
+ * gives 0 for sizes that the call refuses, too. */
+size_t smoe_cached_attention_workspace_bytes(const smoe_cache *cache, const smoe_places *places, int N, int G);
 int smoe_cached_attention_fwd(smoe_ctx *ctx, void *stream, smoe_dtype dtype, const void *Q, int N, int G, const smoe_cache *cache,
                               const smoe_places *places, void *O, float *LSE, void *ws, size_t ws_bytes);
 

@@ -117,7 +117,7 @@ lib.smoe_rotary_frequencies.argtypes = [_i, _d, _i, _d, _d, _vp, _vp]
 lib.smoe_rotary_fwd.argtypes = lib.smoe_rotary_bwd.argtypes = [_vp, _vp, _i, _vp, _i, _vp, _i, _i, _i, _i, _vp, _op, _vp, _vp]
 lib.smoe_cache_append.argtypes = [_vp, _vp, _i, _cp, _pp, _vp, _vp, _i, _op, _vp, _i, _vp]
 lib.smoe_cache_read.argtypes = [_vp, _vp, _i, _cp, _pp, _i, _vp, _vp]
-lib.smoe_cached_attention_workspace_bytes.argtypes = [_i] * 5
+lib.smoe_cached_attention_workspace_bytes.argtypes = [_cp, _pp, _i, _i]
 lib.smoe_cached_attention_workspace_bytes.restype = _sz
 lib.smoe_cached_attention_fwd.argtypes = [_vp, _vp, _i, _vp, _i, _i, _cp, _pp, _vp, _vp, _vp, _sz]
 lib.smoe_momha_decode_workspace_bytes.argtypes = [_i] * 6
@@ -535,7 +535,7 @@ def _turn(entry, what, Q, K, table, positions, out):
         if positions.numel() != B * T:
             raise ValueError("positions must hold B*T entries")
     if out is None:
-        Qr, Kr = _like(Q), None if K is None else _like(K)
+        Qr, Kr = _new(*shape, dtype=dtype, device=Q.device), None if K is None else _new(*like, dtype=dtype, device=K.device)
     else:
         Qr, Kr = out
         for t, x in ((Qr, Q), (Kr, K)):
@@ -677,12 +677,13 @@ def cached_attention_fwd(Q, cache: KVCache, block_table, lens, out=None, ws=None
         if O.shape != Q.shape or LSE.numel() != B * N * G * h:
             raise ValueError("out must be a tensor like Q and one [B, N, G, h]")
     if ws is None:
-        ws = _ws(lib.smoe_cached_attention_workspace_bytes(B, N, G, h, d), Q.device)
+        nb = lib.smoe_cached_attention_workspace_bytes(cache._c, where, N, G)
+        ws = _ws(nb, Q.device) if nb else None
     else:
         _here(dev, torch.uint8, ws)
     c, stream = _where(dev)
-    _check(lib.smoe_cached_attention_fwd(c, stream, BF16, Q.data_ptr(), N, G, cache._c, where, O.data_ptr(), LSE.data_ptr(), ws.data_ptr(), ws.numel()),
-           "smoe_cached_attention_fwd")
+    _check(lib.smoe_cached_attention_fwd(c, stream, BF16, Q.data_ptr(), N, G, cache._c, where, O.data_ptr(), LSE.data_ptr(), _p(ws),
+                                         0 if ws is None else ws.numel()), "smoe_cached_attention_fwd")
     return O, LSE
 
 

@@ -1009,8 +1009,8 @@ int smoe_momha_bwd(smoe_ctx *ctx, void *stream, smoe_dtype dtype, const void *dO
 
 // ------------------------------------------------------------------------------ Alg. 4, decoding
 size_t smoe_momha_decode_workspace_bytes(int B, int N, int k, int d_model, int h_expert, int d_head) {
-  const size_t attention = smoe_cached_attention_workspace_bytes(B, N, k, h_expert, d_head);
-  if (!attention || d_model < 1) return 0;
+  if (B < 1 || N < 1 || k < 1 || h_expert < 1 || h_expert > 65535 || d_model < 1 || (d_head != 64 && d_head != 128) || !cached_attention_fits(B, N, k, h_expert)) return 0;
+  const size_t attention = cached_attention_workspace_bytes(N, k, d_head, 0x7fffffff);   // whatever the table holds
   MomhaSizes z = momha_sizes(B, N, k, d_model, h_expert, d_head);
   // Q and Yhat in fp32 where the products are the decoding kernels'; the shares of K and V lie where partial tiles do
   return 256 + S2S_TAIL_WS_BYTES + 2 * z.kv + 3 * z.q + z.lse + 2 * z.yhat + attention;

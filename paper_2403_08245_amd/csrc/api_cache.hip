@@ -121,9 +121,9 @@ int smoe_cache_read(smoe_ctx *ctx, void *stream, smoe_dtype dtype, const smoe_ca
   return launch_cache_read((hipStream_t)stream, *cache, *places, rows, K, V);
 }
 
-size_t smoe_cached_attention_workspace_bytes(int B, int N, int G, int h, int d_head) {
-  if (B < 1 || N < 1 || G < 1 || h < 1 || (d_head != 64 && d_head != 128) || h > 65535 || !cached_attention_fits(B, N, G, h)) return 0;
-  return align256(cached_attention_workspace_bytes(N, G, d_head));
+size_t smoe_cached_attention_workspace_bytes(const smoe_cache *cache, const smoe_places *places, int N, int G) {
+  if (cache_args_ok(cache) != SMOE_OK || table_ok(cache, places) != SMOE_OK || N < 1 || G < 1 || !cached_attention_fits(places->sequences, N, G, cache->h)) return 0;
+  return cached_attention_workspace_bytes(N, G, cache->d_head, places->width * cache->page);
 }
 
 int smoe_cached_attention_fwd(smoe_ctx *ctx, void *stream, smoe_dtype dtype, const void *Q, int N, int G, const smoe_cache *cache,
@@ -134,7 +134,8 @@ int smoe_cached_attention_fwd(smoe_ctx *ctx, void *stream, smoe_dtype dtype, con
   if (rc != SMOE_OK) return rc;
   if (dtype != SMOE_BF16 || !cached_attention_fits(places->sequences, N, G, cache->h)) return SMOE_ERR_UNSUPPORTED;
   if (!aligned16(Q) || !aligned16(O)) return SMOE_ERR_UNSUPPORTED;
-  if (!ws || ((uintptr_t)ws & 255) || ws_bytes < smoe_cached_attention_workspace_bytes(places->sequences, N, G, cache->h, cache->d_head)) return SMOE_ERR_WORKSPACE;
+  const size_t need = cached_attention_workspace_bytes(N, G, cache->d_head, places->width * cache->page);
+  if (need && (!ws || ((uintptr_t)ws & 255) || ws_bytes < need)) return SMOE_ERR_WORKSPACE;
   const size_t bytes = (size_t)places->sequences * N * G * cache->h * cache->d_head * 2;
   if (O != Q && overlap(O, bytes, Q, bytes)) return SMOE_ERR_INVALID_ARG;
   return launch_cached_attention((hipStream_t)stream, Q, false, N, G, *cache, *places, O, LSE, ws);

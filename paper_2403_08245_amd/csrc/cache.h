@@ -29,7 +29,7 @@ int skinny_shares(int M, int K, int N);      // 0: not for this kernel
 int launch_skinny_pair(hipStream_t s, const void *X, const void *W0, const void *W1, int M, int K, int N, int shares, float *P);
 
 bool cached_attention_fits(int B, int N, int G, int h);   // into one launch
-size_t cached_attention_workspace_bytes(int N, int G, int d_head);
+size_t cached_attention_workspace_bytes(int N, int G, int d_head, int positions);   // positions the table holds
 // wide: Q is fp32 (and not O), and meets the keys as two bf16 numbers
 int launch_cached_attention(hipStream_t s, const void *Q, bool wide, int N, int G, const smoe_cache &c, const smoe_places &p, void *O, float *LSE, void *ws);
 

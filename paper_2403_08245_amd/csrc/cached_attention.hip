@@ -169,7 +169,7 @@ template <bool JOIN> __device__ __forceinline__ bool find_piece(const int32_t *l
 }
 
 // What a piece leaves: its rows' sums of weighted values [rows][D], then their maxima and sums of weights [rows] each.
-__host__ __device__ inline size_t slot_floats(int rows, int D) { return (size_t)rows * (D + 2); }
+__host__ __device__ inline size_t slot_floats(int rows, int D) { return ((size_t)rows * (D + 2) + 3) & ~(size_t)3; }
 
 // ------------------------------------------------------------------------------------------------ a step's operands
 __device__ __forceinline__ __amdgpu_buffer_rsrc_t window(const void *p, int bytes) { return __builtin_amdgcn_make_buffer_rsrc((void *)p, 0, bytes, 0x00020000); }
@@ -695,9 +695,10 @@ bool cached_attention_fits(int B, int N, int G, int h) {
          (long long)ceil_div((int)R, 16 * row_tiles((int)R)) * h * B <= 0x7fffffffLL / 256 - 2 * MAX_TARGET;
 }
 
-size_t cached_attention_workspace_bytes(int N, int G, int d_head) {
-  const long long R = (long long)N * G;
-  return MAX_SLOTS * slot_floats((int)std::min<long long>(R, 16 * row_tiles((int)std::min<long long>(R, 1 << 20))), d_head) * sizeof(float);
+size_t cached_attention_workspace_bytes(int N, int G, int d_head, int positions) {
+  if (positions <= WHOLE_STEPS * STEP) return 0;           // nothing is cut
+  const int R = N * G;
+  return align256(MAX_SLOTS * slot_floats(std::min(R, 16 * row_tiles(R)), d_head) * sizeof(float));
 }
 
 int launch_cached_attention(hipStream_t s, const void *Q, bool wide, int N, int G, const smoe_cache &c, const smoe_places &p, void *O, float *LSE, void *ws) {

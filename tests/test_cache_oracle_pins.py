@@ -201,12 +201,16 @@ def test_refusals_of_attention_and_layer(calls):
         assert f(**bad) == -1, bad
     for bad in (dict(Q=q + 2), dict(O=f.values["O"] + 8), dict(N=2 ** 16, G=2 ** 16)):
         assert f(**bad) == -2, bad
-    need = calls["lib"].smoe_cached_attention_workspace_bytes(2, 1, 2, 2, 64)
+    query = calls["lib"].smoe_cached_attention_workspace_bytes
+    at = _cache_with(calls, "at", width=100)                      # 1600 positions: a sequence may be shared by blocks
+    need = query(ctypes.byref(calls["cache"]), at, 1, 2)
     assert need > 0 and need % 256 == 0
     for bad in (dict(ws=None), dict(ws=calls["mem"] + 16), dict(ws_bytes=need - 1)):
-        assert f(**bad) == -3, bad
-    for sizes in ((0, 1, 1, 1, 128), (1, 0, 1, 1, 128), (1, 1, 0, 1, 128), (1, 1, 1, 0, 128), (1, 1, 1, 1, 96), (2 ** 20, 2 ** 10, 2, 1, 128)):
-        assert calls["lib"].smoe_cached_attention_workspace_bytes(*sizes) == 0, sizes
+        assert f(places=at, **bad) == -3, bad
+    assert query(ctypes.byref(calls["cache"]), ctypes.byref(calls["at"]), 1, 2) == 0      # 48 positions: nothing to share
+    for sizes in ((None, at, 1, 2), (ctypes.byref(calls["cache"]), None, 1, 2), (ctypes.byref(calls["cache"]), at, 0, 2), (ctypes.byref(calls["cache"]), at, 1, 0),
+                  (_cache_with(calls, d_head=96), at, 1, 2), (ctypes.byref(calls["cache"]), at, 2 ** 16, 2 ** 16)):
+        assert query(*sizes) == 0
     f = calls["decode"]
     for bad in (dict(X=None), dict(W_K=None), dict(W_V=None), dict(W_Q=None), dict(W_O=None), dict(r=None), dict(gates=None), dict(O=None), dict(N=0), dict(N=2), dict(k=0),
                 dict(k=3), dict(d_model=0), dict(places=ctypes.byref(calls["listed"]))):

@@ -258,6 +258,25 @@ def test_append_last_places_and_turn(smoe, quantised, N, rot, layout):
         assert (np.abs(k - wantK)[real] <= tol[real]).all()
 
 
+@pytest.mark.parametrize("quantised", [False, True])
+def test_append_turns_keys_alone(smoe, quantised):
+    """Without queries the stored keys are the same bits as with them, and as those of listed places."""
+    page, h, d = 16, 3, 64
+    lens = torch.tensor([20, 7, 33], dtype=torch.int32)
+    table, pages = _table(lens, page, 171)
+    table, K, V, Q = table.cuda(), _normal((6, h, d), 172).cuda(), _normal((6, h, d), 173).cuda(), _normal((6, 5, d), 174).cuda()
+    rotary = smoe.rotary_table(32, scaling="linear", factor=2.0)
+    seqs = torch.tensor([0, 0, 1, 1, 2, 2], dtype=torch.int32)
+    positions = (lens[seqs.long()] - 2 + torch.tensor([0, 1] * 3)).to(torch.int32)
+    out = []
+    for more in (dict(lens=lens.cuda(), Q=Q), dict(lens=lens.cuda()), dict(seqs=seqs.cuda(), positions=positions.cuda())):
+        cache = smoe.kv_cache(pages, page, h, d, quantised)
+        smoe.cache_append(cache, K, V, table, rotary=rotary, **more)
+        out.append([t for t in (cache.K, cache.V, cache.K_exp, cache.V_exp) if t is not None])
+    for a, b, c in zip(*out):
+        assert torch.equal(a.view(torch.uint8), b.view(torch.uint8)) and torch.equal(a.view(torch.uint8), c.view(torch.uint8))
+
+
 def test_append_leaves_out_bad_pages_and_reads_zeros(smoe):
     lens, page = torch.tensor([30, 20], dtype=torch.int32), 16
     table, pages = _table(lens, page, 31)
@@ -444,6 +463,8 @@ def test_cached_attention_hidden_positions_do_not_reach_a_query(smoe, what):
     O, L = smoe.cached_attention_fwd(Q.cuda(), cache, table.cuda(), torch.tensor(lens, dtype=torch.int32).cuda())
     cut = [n - 1 for n in lens]
     _check_attention(O[:, :3].contiguous(), L[:, :3].contiguous(), Q[:, :3], K, V, cut)
+    if what == "nan":
+        assert bool(O[:, 3].isnan().all()) and bool(L[:, 3].isnan().all())       # who sees it has it
 
 
 def test_cached_attention_scores_of_minus_infinity_and_extremes(smoe):
