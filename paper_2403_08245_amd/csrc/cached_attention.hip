@@ -608,7 +608,7 @@ __global__ void __launch_bounds__(64 * WAVES, RT == 1 && ONE ? 3 : 2)
 // fixed order: one row a block where few units are cut, into many pieces, and more of them where the units fill the chip.
 // A thousand lanes a block only where there are hardly any blocks: one sequence of 131072 positions, one head, 8 rows 21.0 us (22.5 with 256);
 // one of 4096 with 4 heads of 4 rows 12.5 (11.6).
-constexpr int JOIN_AHEAD = 8, JOIN_FEW = 16;
+constexpr int JOIN_AHEAD = 8, JOIN_FEW = 8;
 template <int D, int JOIN_THREADS> __global__ void __launch_bounds__(JOIN_THREADS)
     cached_attention_join_kernel(smoe_places p, Dims d, int h, int rows_log2, const float *ws, bf16_t *O, float *LSE) {
   constexpr int LANES = D / 4, GROUPS = JOIN_THREADS / LANES;

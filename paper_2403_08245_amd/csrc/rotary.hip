@@ -25,10 +25,7 @@ template <> struct Eight<bf16_t> {
   vec v;
   __device__ __forceinline__ void load(const bf16_t *p) { v = *reinterpret_cast<const vec *>(p); }
   __device__ __forceinline__ void store(bf16_t *p) const { *reinterpret_cast<vec *>(p) = v; }
-  template <bool ONCE> __device__ __forceinline__ void load_as(const bf16_t *p) {
-    if constexpr (ONCE) v = __builtin_nontemporal_load(reinterpret_cast<const vec *>(p));
-    else load(p);
-  }
+  __device__ __forceinline__ void load_once(const bf16_t *p) { v = __builtin_nontemporal_load(reinterpret_cast<const vec *>(p)); }   // kept by no cache
   template <bool ONCE> __device__ __forceinline__ void store_as(bf16_t *p) const {
     if constexpr (ONCE) __builtin_nontemporal_store(v, reinterpret_cast<vec *>(p));
     else store(p);
@@ -266,9 +263,11 @@ __global__ void __launch_bounds__(64 * WAVES) turn_rows_kernel(TurnArgs a, smoe_
 
 // Rows to the cache without a turn (WRITE), or back from it as bf16, where both formats' values are exact.  A wavefront takes 16 tokens' rows
 // of one head, keys or values: positions that follow one another lie side by side on a page, so that what it writes there (or
-// reads) is 2 or 4 KB in a row, and the 16 exponents one piece.  ONCE: what the caches could not hold until it is used passes them by.
-// Quantising 51 thousand tokens of 8 heads, 213 MB: 46.8 us so, 53.6 through the caches, 51 with a token a wavefront; of 4 heads of 64
-// 15.8, 18.1 and 35.5 us.  Reading the former back: 33.1 us, 47.9 through the caches.
+// reads) is 2 or 4 KB in a row, and the 16 exponents one piece.  Rows on their way into the cache are dead afterwards and kept by no cache;
+// ONCE: nor is what is written, where it is more than the caches could hold until it is used.
+// Quantising 51 thousand tokens of 8 heads, 213 MB, us: 49.5 so (46.8 with the pages past the caches, too, which costs 12 if they are read
+// back next; 53.6 all through the caches; 51 with a token a wavefront); of 4 heads of 64 16.6 (18.1; 35.5 with a token a wavefront).  Reading the
+// former back, 209 MB of rows: 33.1 past the caches, 47.9 through them.
 template <int FORMAT, bool WRITE, int D, bool ONCE>
 __global__ void __launch_bounds__(64 * WAVES) cache_rows_kernel(smoe_cache c, smoe_places places, bf16_t *K, bf16_t *V, int tokens, int N, int page_shift, unsigned int items) {
   constexpr int LANES = D / 8, AT_ONCE = 64 / LANES, ROUNDS = TOKENS / AT_ONCE;
@@ -288,7 +287,7 @@ __global__ void __launch_bounds__(64 * WAVES) cache_rows_kernel(smoe_cache c, sm
     const long long t = (long long)tile * TOKENS + u * AT_ONCE + sub;
     mine[u] = t < tokens;
     const int token = mine[u] ? (int)t : 0;
-    if (WRITE && mine[u]) x[u].template load_as<ONCE>(outside + (size_t)token * c.h * D);
+    if (WRITE && mine[u]) x[u].load_once(outside + (size_t)token * c.h * D);
     int seq, pos;
     find_place(places, N, token, seq, pos);
     const int id = find_page(places, c.pages, page_shift, seq, pos);
@@ -392,8 +391,9 @@ template <bool WRITE> int launch_rows(hipStream_t s, const smoe_cache &c, const 
     constexpr bool ONCE = decltype(once_c)::value;
     c.format == SMOE_CACHE_BF16 ? go(cache_rows_kernel<SMOE_CACHE_BF16, WRITE, D, ONCE>) : go(cache_rows_kernel<SMOE_CACHE_E4M3, WRITE, D, ONCE>);
   };
-  // a quarter of the last-level cache: the attention that comes next, or the next layer's rows, would not find more of it there
-  const bool once = (size_t)tokens * c.h * c.d_head * (c.format == SMOE_CACHE_BF16 ? 8 : 6) > LAST_LEVEL_CACHE / 4;
+  // pages are read again from half the last-level cache down, rows by the launch that comes next, with as much of its own
+  const size_t written = (size_t)tokens * c.h * c.d_head * (WRITE && c.format == SMOE_CACHE_E4M3 ? 2 : 4);
+  const bool once = written > LAST_LEVEL_CACHE / (WRITE ? 2 : 4);
   auto by_d = [&](auto d_c) { once ? by_once(d_c, std::true_type{}) : by_once(d_c, std::false_type{}); };
   c.d_head == 128 ? by_d(std::integral_constant<int, 128>{}) : by_d(std::integral_constant<int, 64>{});
   SMOE_LAUNCH_CHECK();
