@@ -9,13 +9,14 @@
 // S^T[key][query] = K Q^T on 16 x 16 x 32 matrix instructions, so a lane owns one query column: its running maximum and sum are scalars of
 // the lane, and its eight weights of a step already lie as the second product's operand, O^T[column][query] = V^T P^T, whose contraction
 // runs over the keys in the order the lanes hold them.  A lane reads its eight keys' values for D / 16 columns and turns them
-// into the operands of D / 16 instructions by byte permutations.  No LDS traffic of theirs and no barrier until a piece ends.
+// into the operands of D / 16 instructions by byte permutations.  No LDS traffic of theirs (two tiles of queries, and fp32 ones,
+// wait in LDS) and no barrier until a piece ends.
 // Values in e4m3 are widened to bf16, scaled, as they are used: exactly, and at half the bytes.
 //
 // Measured (reads alone reach 6.5 TB/s here, a copy 5.1): 256 sequences of 500, 8 heads, 524 MB 81 us (6.5 TB/s); 64 of 100 to 8192, 4 heads,
-// 240 MB 50 us; 64 of 3 to 8192, 135 MB 31 us (4.6); 90001 and 131072 in e4m3, 8 heads of 24 rows, 453 MB 83 to 87 us (5.3); one of 301
-// 6.6 us.  What bounds the short ones is a chain of dependent reads (lengths, page numbers, keys) and, where sequences are cut, the second
-// launch of 4 us; the counters show every byte of the cache read once.
+// 240 MB 50 us; 64 of 3 to 8192, 142 MB 31 us (4.6); 90001 and 131072 in e4m3, 8 heads of 24 rows, 456 MB 85.5 us (5.3); one of 301
+// 6.8 us.  What bounds the short ones is a chain of dependent reads (lengths, page numbers, keys) and, where sequences are cut, the second
+// launch of 4 us; the counters show 1.02 times the bytes of the cache fetched.
 #include "cache.h"
 #include <algorithm>
 #include <type_traits>
@@ -35,11 +36,12 @@ constexpr int MAX_TARGET = 768;  // pieces that the whole batch is cut into, abo
 // sequences of up to 8192 positions: 768 pieces 31.1 us, 1024 33.0; two long ones of three tokens: 512 82.8, 1024 94.4).
 constexpr int T_ONE = 768, T_MULTI = 512, T_TWO = 512;
 // Sequences of no more steps are not cut, and where the table holds no longer ones there is no second kernel (one of 301 positions 6.5 us, with a line
-// at 8 steps 9.4; a thousand of up to 300 21 and 170).
+// at 8 steps 9.4; a thousand of up to 300 21.3 and 170).
 constexpr int WHOLE_STEPS = 16;
-// Steps of a piece, at least: one sequence of 4096, 4 heads, 16 12.5 us, 8 10.7, 4 10.0; four of 900 to 4096 12.8, 11.1, 12.5.
+// Steps of a piece, at least: one sequence of 4096, 4 heads, 16 12.5 us, 8 10.7, 4 10.0; four of 900 to 4096 12.8, 11.1, 12.5
+// (taken before the reads went past the caches).
 constexpr int MIN_STEPS = 8;
-constexpr int MOST_PIECES = 256; // of a unit (one of 131072, one head: 21.2 us; 512 23.5)
+constexpr int MOST_PIECES = 256; // of a unit (one of 131072, one head: 21.4 us; 512 23.5)
 
 struct Dims {
   int N, G, R;                   // R = N * G query rows of a (sequence, head)

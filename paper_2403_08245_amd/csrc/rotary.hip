@@ -4,7 +4,7 @@
 // A wavefront takes one token's rows, or some of them, d_head / 8 lanes a row and 8 elements a lane.  The angles belong to the token:
 // each lane works out the sine and cosine of one pair (more for rows over 128), and the wavefront shares them through LDS, so they cost
 // a token one evaluation a lane, however many heads it has.  Its first rows are on their way meanwhile.
-// Measured: queries and keys of 8192 tokens, 16 + 4 heads of 128, bf16, 84 MB: 19.5 us (4.3 TB/s; 14 to 16 where the caches hold them); of 32768
+// Measured: queries and keys of 8192 tokens, 16 + 4 heads of 128, bf16, 84 MB: 19.6 us (4.3 TB/s; 15.8 where the caches hold them); of 32768
 // tokens, 32 + 4 heads, 604 MB: 104 us (5.8 TB/s).  A large copy runs at 5.1.
 //
 // An angle is p f modulo one turn, of the 64-bit fraction of a turn that a position adds: one integer product that wraps, whose upper 32
@@ -17,7 +17,7 @@ namespace {
 constexpr int WAVES = 4;
 constexpr int MAX_PAIRS = 256;      // rows of at most 512 elements
 // Rows a lane has in flight.  2: a decoding step's four tokens 3.0 us, the queries and keys of 8192 tokens (16 + 4 heads of 128) 19.4; 4: 3.5
-// and 21.2; 1: 2.9 and 18.5, but rows of 64 half turned 26.4 instead of 22.4.
+// and 21.2; 1: 2.9 and 18.5, but rows of 64 half turned 26.4 instead of 22.2.
 constexpr int BATCH = 2;
 constexpr int TOKENS = 16;          // of a wavefront, where rows are copied between the cache and plain tensors
 constexpr int MOST = 8;             // rounds of rows a wavefront takes (32768 tokens of 36 heads: 4 108.6, 8 107.9, 16 116 us)
