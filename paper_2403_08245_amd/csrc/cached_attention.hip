@@ -194,6 +194,11 @@ template <bool UPPER> __device__ __forceinline__ uint32_t widen(uint32_t codes, 
   return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(codes, scale, UPPER));
 }
 
+// The upper of the two bf16 numbers that stand for x: cut towards zero, from the next number below it, so that what is left for the lower is
+// never zero and both have x's sign.  Infinity times x is then infinity times either, and their sum, not a NaN; rounded to the nearest, the
+// lower would be zero or of the other sign for half of all x.  The two are within 2^-16 of x (2^-17 with the nearest).
+__device__ __forceinline__ float upper_part(float x) { return __uint_as_float(__float_as_uint(x * (1.f - 0x1p-23f)) & 0xffff0000u); }
+
 // The same offset, but what is added to it stays an immediate of the loads: hoisted out of the loop, every sum would take a register.
 __device__ __forceinline__ int here(int at) {
   __asm__ volatile("" : "+v"(at));
@@ -386,8 +391,9 @@ __global__ void __launch_bounds__(64 * WAVES, RT == 1 && ONE ? 3 : 2)
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
           const float y = i < 4 ? lo[i] : hi[i - 4];
-          q[t][ks][i] = (bf16_t)y;
-          q_low[t][ks][i] = (bf16_t)(y - (float)q[t][ks][i]);
+          const float up = upper_part(y);
+          q[t][ks][i] = (bf16_t)up;
+          q_low[t][ks][i] = (bf16_t)(y - up);
         }
       } else {
         q[t][ks] = *reinterpret_cast<const bf16x8 *>((const bf16_t *)Q + e);
@@ -502,8 +508,9 @@ __global__ void __launch_bounds__(64 * WAVES, RT == 1 && ONE ? 3 : 2)
         for (int e = 0; e < 4; ++e) {
           const float w = __builtin_amdgcn_exp2f((x[i][e] - base) * scale);   // the difference first: huge scores cancel exactly
           sum += w;
-          pb[t][4 * i + e] = (bf16_t)w;
-          pl[t][4 * i + e] = (bf16_t)(w - (float)pb[t][4 * i + e]);
+          const float up = upper_part(w);
+          pb[t][4 * i + e] = (bf16_t)up;
+          pl[t][4 * i + e] = (bf16_t)(w - up);
         }
       l[t] = l[t] * alpha + sum;
       if (__any(alpha != 1.f)) {

@@ -490,6 +490,25 @@ def test_cached_attention_scores_of_minus_infinity_and_extremes(smoe):
     assert np.allclose(_f64(L[2]), 40.0 * 64 / 8)
 
 
+@pytest.mark.parametrize("lens,N,G", [([40, 1, 700], 1, 2), ([40, 9, 700], 3, 2), ([40, 9, 700], 2, 12)])
+def test_cached_attention_infinite_values_that_are_seen(smoe, lens, N, G):
+    """An infinite value that a query sees makes that column infinite, of its sign, and no other column anything: every weight here is far
+    from underflow (scores of normal rows differ by less than 2^6), so infinity times it is infinity, not NaN."""
+    _log(f"cached attention infinite values {lens} N={N} G={G}")
+    cache, table, K, V = _case(smoe, lens, 16, 1, 128, False, 191)
+    for b in range(3):
+        for p in range(0, lens[b] - N + 1, 5):           # positions that every query sees
+            for column, x in ((3, float("inf")), (64, float("-inf"))):
+                cache.V[table[b, p // 16], :, p % 16, column] = x
+    Q = _normal((3, N, G, 1, 128), 194)
+    O, L = smoe.cached_attention_fwd(Q.cuda(), cache, table.cuda(), torch.tensor(lens, dtype=torch.int32).cuda())
+    assert bool((O[..., 3] == float("inf")).all()) and bool((O[..., 64] == float("-inf")).all())
+    O[..., 3], O[..., 64] = 0.0, 0.0                      # and the other columns are what they are without these two
+    for v in V:
+        v[..., 3], v[..., 64] = 0.0, 0.0
+    _check_attention(O, L, Q, K, V, lens)
+
+
 def test_cached_attention_refusals(smoe):
     cache = smoe.kv_cache(3, 16, 2, 64)
     table, lens = torch.zeros(2, 1, dtype=torch.int32).cuda(), torch.ones(2, dtype=torch.int32).cuda()
