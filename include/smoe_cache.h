@@ -92,7 +92,7 @@ typedef struct {
 int smoe_cache_append(smoe_ctx *ctx, void *stream, smoe_dtype dtype, const smoe_cache *cache, const smoe_places *places,
                       const void *K, const void *V, int rows, const smoe_rotary *rotary, const void *Q, int hq, void *Qr);
 
-/* Reads the rows' places back into K, V [rows, h, d_head] (bf16); rows without one become zeros. */
+/* Reads the rows' places back into K, V [rows, h, d_head] (bf16); rows without one become zeros.  K and V do not overlap. */
 int smoe_cache_read(smoe_ctx *ctx, void *stream, smoe_dtype dtype, const smoe_cache *cache, const smoe_places *places, int rows,
                     void *K, void *V);
 
@@ -104,7 +104,7 @@ int smoe_cache_read(smoe_ctx *ctx, void *stream, smoe_dtype dtype, const smoe_ca
  * A query with p < 0, or whose visible scores are all -infinity, attends nothing: O = 0, LSE = -infinity.  What lies in the cache at
  * positions that a query does not see never reaches it, NaN and infinities included.  Lengths count as at most width * page, and
  * positions on pages outside [0, pages) are not seen.
- * The places' seqs and positions are not read (NULL).  N >= 1, G >= 1.  O may be Q.  The workspace holds the partial sums of sequences that
+ * The places' seqs and positions are not read (NULL).  N >= 1, G >= 1.  O may be Q; else Q, O, LSE and the workspace do not overlap.  The workspace holds the partial sums of sequences that
  * several blocks share; none is needed (0, ws may be NULL) where the table holds at most 512 positions.  The query looks at sizes only, and
  * gives 0 for sizes that the call refuses, too. */
 size_t smoe_cached_attention_workspace_bytes(const smoe_cache *cache, const smoe_places *places, int N, int G);

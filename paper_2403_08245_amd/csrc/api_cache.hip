@@ -118,6 +118,8 @@ int smoe_cache_read(smoe_ctx *ctx, void *stream, smoe_dtype dtype, const smoe_ca
   if (rows == 0) return SMOE_OK;
   if (!K || !V) return SMOE_ERR_INVALID_ARG;
   if (!aligned16(K) || !aligned16(V)) return SMOE_ERR_UNSUPPORTED;
+  const size_t bytes = (size_t)rows * cache->h * cache->d_head * 2;
+  if (overlap(K, bytes, V, bytes)) return SMOE_ERR_INVALID_ARG;
   return launch_cache_read((hipStream_t)stream, *cache, *places, rows, K, V);
 }
 
@@ -137,7 +139,9 @@ int smoe_cached_attention_fwd(smoe_ctx *ctx, void *stream, smoe_dtype dtype, con
   const size_t need = cached_attention_workspace_bytes(N, G, cache->d_head, places->width * cache->page);
   if (need && (!ws || ((uintptr_t)ws & 255) || ws_bytes < need)) return SMOE_ERR_WORKSPACE;
   const size_t bytes = (size_t)places->sequences * N * G * cache->h * cache->d_head * 2;
-  if (O != Q && overlap(O, bytes, Q, bytes)) return SMOE_ERR_INVALID_ARG;
+  const size_t lse = (size_t)places->sequences * N * G * cache->h * sizeof(float);
+  if ((O != Q && overlap(O, bytes, Q, bytes)) || overlap(LSE, lse, Q, bytes) || overlap(LSE, lse, O, bytes)) return SMOE_ERR_INVALID_ARG;
+  if (need && (overlap(ws, need, Q, bytes) || overlap(ws, need, O, bytes) || overlap(ws, need, LSE, lse))) return SMOE_ERR_INVALID_ARG;
   return launch_cached_attention((hipStream_t)stream, Q, false, N, G, *cache, *places, O, LSE, ws);
 }
 

@@ -231,3 +231,17 @@ def test_header_and_export_list_agree(calls):
     assert sorted(set(re.findall(r"\b(smoe_[a-z0-9_]+)\s*\(", text))) == sorted(calls["m"].CACHE_EXPORTS)
     for name in calls["m"].CACHE_EXPORTS:
         assert hasattr(calls["lib"], name)
+
+
+def test_refusals_of_outputs_that_overlap(calls):
+    """One launch writes them all, or reads one while it writes another."""
+    f = calls["read"]
+    for bad in (dict(V=f.values["K"]), dict(V=f.values["K"] + 256), dict(K=f.values["V"] + 496)):       # two rows of two heads of 64: 512 bytes each
+        assert f(**bad) == -1, bad
+    f = calls["attend"]
+    q, o = f.values["Q"], f.values["O"]
+    for bad in (dict(LSE=q), dict(LSE=o), dict(LSE=o + 1020)):                                           # Q and O: 2 x 2 x 2 x 64 bf16 = 1024 bytes
+        assert f(**bad) == -1, bad
+    at = _cache_with(calls, "at", width=100)
+    for bad in (dict(ws=q), dict(ws=o), dict(ws=f.values["LSE"])):
+        assert f(places=at, **bad) == -1, bad
