@@ -1044,7 +1044,7 @@ int smoe_momha_decode(smoe_ctx *ctx, void *stream, smoe_dtype dtype, const void 
   hipStream_t s = (hipStream_t)stream;
   const size_t weights = 2 * (size_t)d_model * d_out * 2 * ((size_t)r->E + 1);   // all that the call may read
   // Of the layer's tensors the decoding kernels leave Q, the shares of K and V, and Yhat in fp32: O then carries two roundings to bf16, its own
-  // and Ohat's, beside the cache's (error against 64 bits 2.3e-3; 3.7e-3 with every tensor rounded, as the
+  // and Ohat's, beside the cache's (error against 64 bits 2.4e-3; 3.7e-3 with every tensor rounded, as the
   // prefill pass does; 64 sequences of the 4096-wide layer 190 -> 194 us).
   S2SArgs aq = make_s2s(X, W_Q, Q, r, d_model, d_out, false, false, k, false);
   S2SArgs ao = make_s2s(Ohat, W_O, Yhat, r, d_out, d_model, false, false, 1, false);
