@@ -492,12 +492,22 @@ def _where(dev: int):
 ROTARY_SCALINGS = {"none": 0, "linear": 1, "base": 2, "blend": 3}
 
 
-class RotaryTable:
-    """Frequencies of the rotated pairs, on the device (made once; see smoe_rotary)."""
+class _Fixed:
+    """Attributes are set once, at construction: the C view that the calls pass on is made of them there."""
+
+    def __setattr__(self, name, value):
+        raise AttributeError(f"{type(self).__name__}.{name} is fixed: make a new {type(self).__name__}")
+
+    def __delattr__(self, name):
+        self.__setattr__(name, None)
+
+
+class RotaryTable(_Fixed):
+    """Frequencies of the rotated pairs, on the device (made once, attributes fixed; see smoe_rotary)."""
 
     def __init__(self, turns: torch.Tensor, rot: int, interleaved: bool, amplitude: float):
-        self.turns, self.rot, self.interleaved, self.amplitude = turns, rot, interleaved, amplitude
-        self._c = ctypes.byref(smoe_rotary(turns.data_ptr(), rot, int(interleaved), amplitude))
+        self.__dict__.update(turns=turns, rot=rot, interleaved=interleaved, amplitude=amplitude,
+                             _c=ctypes.byref(smoe_rotary(turns.data_ptr(), rot, int(interleaved), amplitude)))
 
 
 def rotary_table(rot: int, layout: str = "half", base: float = 10000.0, scaling: str = "none", factor: float = 1.0,
@@ -559,9 +569,10 @@ def rotary_bwd(dQ, dK, table: RotaryTable, positions=None, out=None):
     return _turn(lib.smoe_rotary_bwd, "smoe_rotary_bwd", dQ, dK, table, positions, out)
 
 
-class KVCache:
+class KVCache(_Fixed):
     """A paged cache of keys and values: K and V [pages, h, page, d_head], bf16, or uint8 holding e4m3 with the rows' exponents
-    K_exp and V_exp [pages, h, page] uint8 (see smoe_cache).  The tensors stay the caller's and are written in place."""
+    K_exp and V_exp [pages, h, page] uint8 (see smoe_cache).  The tensors stay the caller's and are written in place; which they are is
+    fixed (a larger cache is a new KVCache), and so is where they lie."""
 
     def __init__(self, K: torch.Tensor, V: torch.Tensor, K_exp: torch.Tensor | None = None, V_exp: torch.Tensor | None = None):
         quantised = K_exp is not None
@@ -575,10 +586,9 @@ class KVCache:
                 raise ValueError("exponents must be [pages, h, page]")
         if len({t.device for t in (K, V, K_exp, V_exp) if t is not None}) != 1:
             raise ValueError("the cache's tensors must be on one device")
-        self.K, self.V, self.K_exp, self.V_exp = K, V, K_exp, V_exp
-        self.pages, self.h, self.page, self.d_head = K.shape
-        self.device = K.get_device()
-        self._c = ctypes.byref(smoe_cache(_p(K), _p(V), _p(K_exp), _p(V_exp), self.pages, self.page, self.h, self.d_head, int(quantised)))
+        pages, h, page, d_head = K.shape
+        self.__dict__.update(K=K, V=V, K_exp=K_exp, V_exp=V_exp, pages=pages, h=h, page=page, d_head=d_head, device=K.get_device(),
+                             _c=ctypes.byref(smoe_cache(_p(K), _p(V), _p(K_exp), _p(V_exp), pages, page, h, d_head, int(quantised))))
 
 
 def kv_cache(pages: int, page: int, h: int, d_head: int, quantised: bool = False, device=None) -> KVCache:

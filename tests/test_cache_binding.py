@@ -1,0 +1,72 @@
+"""The binding's checks in front of the cache's and positions' entry points, with stand-ins for device tensors (CPU): what a call refuses never
+reaches the library."""
+import math
+
+import pytest
+import torch
+
+
+class Tensor:
+    """What the binding asks of a device tensor, without memory."""
+    is_cuda = True
+
+    def __init__(self, *shape, dtype=torch.bfloat16, device=0, contiguous=True):
+        self.shape, self.dtype, self.index, self.contiguous = torch.Size(shape), dtype, device, contiguous
+
+    device = property(lambda self: torch.device("cuda", self.index))
+    get_device = lambda self: self.index
+    is_contiguous = lambda self: self.contiguous
+    numel = lambda self: math.prod(self.shape)
+    dim = lambda self: len(self.shape)
+    data_ptr = lambda self: 4096
+
+
+def ints(*shape, **kw):
+    return Tensor(*shape, dtype=torch.int32, **kw)
+
+
+class Library:
+    """Records the calls that would have been made."""
+
+    def __init__(self):
+        self.calls = []
+
+    def __getattr__(self, name):
+        def call(*args):
+            self.calls.append(name)
+            return 512 if name.endswith("_workspace_bytes") else 0
+        return call
+
+
+@pytest.fixture
+def smoe(monkeypatch):
+    import paper_2403_08245_amd as m
+    monkeypatch.setattr(m, "lib", Library())
+    monkeypatch.setattr(m, "_new", lambda *shape, dtype, device: Tensor(*shape, dtype=dtype))
+    monkeypatch.setattr(m, "_device", lambda first: 0)
+    monkeypatch.setattr(m, "_where", lambda dev: (None, None))
+    return m
+
+
+def a_cache(m, h=2, d=64, quantised=False):
+    t = torch.uint8 if quantised else torch.bfloat16
+    exps = [Tensor(4, h, 16, dtype=torch.uint8) for _ in "KV"] if quantised else []
+    return m.KVCache(Tensor(4, h, 16, d, dtype=t), Tensor(4, h, 16, d, dtype=t), *exps)
+
+
+def a_table(m, device=0):
+    return m.RotaryTable(Tensor(32, dtype=torch.int64, device=device), 64, False, 1.0)
+
+
+@pytest.mark.parametrize("quantised", [False, True])
+def test_what_a_cache_and_a_table_are_made_of_does_not_change(smoe, quantised):
+    """The library's view of them holds the addresses they were made with: tensors put in later would leave it writing to the old ones."""
+    cache, table = a_cache(smoe, quantised=quantised), a_table(smoe)
+    for thing, names in ((cache, ("K", "V", "K_exp", "V_exp", "pages", "h", "page", "d_head", "device")), (table, ("turns", "rot", "interleaved", "amplitude"))):
+        for name in names:
+            before = getattr(thing, name)
+            with pytest.raises(AttributeError):
+                setattr(thing, name, Tensor(8, 2, 16, 64))
+            with pytest.raises(AttributeError):
+                delattr(thing, name)
+            assert getattr(thing, name) is before
