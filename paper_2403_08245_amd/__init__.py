@@ -626,8 +626,9 @@ def cache_append(cache: KVCache, K, V, block_table, lens=None, seqs=None, positi
     _here(dev, torch.bfloat16, K, V)
     row, n = cache.h * cache.d_head, K.numel()
     M = n // row
-    if n != M * row or V.numel() != n or (M != rows if rows is not None else M % block_table.shape[0]):
-        raise ValueError("K and V must be [rows, h, d_head]")
+    B = block_table.shape[0]
+    if n != M * row or V.numel() != n or (M != rows if rows is not None else B == 0 or M % B):
+        raise ValueError("K and V must be [rows, h, d_head], as many rows for each sequence")
     if rotary is not None and rotary.turns.get_device() != dev:
         raise ValueError(f"table on {rotary.turns.device}, but the current device is {dev}")
     hq, Qr = 0, None

@@ -70,3 +70,14 @@ def test_what_a_cache_and_a_table_are_made_of_does_not_change(smoe, quantised):
             with pytest.raises(AttributeError):
                 delattr(thing, name)
             assert getattr(thing, name) is before
+
+
+def test_append_to_a_table_of_no_sequences_is_refused(smoe):
+    cache, rows = a_cache(smoe), Tensor(0, 2, 64)
+    with pytest.raises(ValueError):
+        smoe.cache_append(cache, rows, rows, ints(0, 3), lens=ints(0))
+    with pytest.raises(ValueError):
+        smoe.cache_append(cache, Tensor(4, 2, 64), Tensor(4, 2, 64), ints(0, 3), lens=ints(0))
+    assert not smoe.lib.calls
+    smoe.cache_append(cache, rows, rows, ints(2, 3), lens=ints(2))              # no rows of two sequences are fine
+    assert smoe.lib.calls == ["smoe_cache_append"]
