@@ -701,7 +701,7 @@ def cached_attention_fwd(Q, cache: KVCache, block_table, lens, out=None, ws=None
 def momha_decode(X, W_K, W_V, W_Q, W_O, r: Routing, k: int, gates, cache: KVCache, block_table, lens, rotary: RotaryTable | None = None,
                  out=None, ws=None):
     """The SMoE attention layer on the last N positions of every sequence, X [B*N, d_model], over a cache that holds the earlier ones and
-    receives these.  Returns O [B*N, d_model]."""
+    receives these; W_K and W_V [d_model, h * d_head], W_Q [E, d_model, h * d_head], W_O [E, h * d_head, d_model].  Returns O [B*N, d_model]."""
     dev = _device(X)
     where, _ = _places(dev, cache, block_table, lens)
     _here(dev, torch.bfloat16, X, W_K, W_V, W_Q, W_O)
@@ -712,7 +712,10 @@ def momha_decode(X, W_K, W_V, W_Q, W_O, r: Routing, k: int, gates, cache: KVCach
     B, d_out = block_table.shape[0], cache.h * cache.d_head
     if B == 0 or M == 0 or M % B or gates.numel() != M * k:
         raise ValueError("X must be [sequences * N, d_model] and gates hold k for each row")
-    if W_K.numel() != d_model * d_out or W_V.numel() != W_K.numel() or W_Q.shape != (r.E, d_model, d_out) or W_O.shape != (r.E, d_out, d_model):
+    for W in (W_K, W_V):
+        if W.shape[0] != d_model or W.numel() != d_model * d_out:
+            raise ValueError("W_K and W_V must be [d_model, h * d_head]")
+    if W_Q.shape != (r.E, d_model, d_out) or W_O.shape != (r.E, d_out, d_model):
         raise ValueError("weights do not fit d_model and the cache's h * d_head")
     N = M // B
     O = _like(X) if out is None else out

@@ -81,3 +81,22 @@ def test_append_to_a_table_of_no_sequences_is_refused(smoe):
     assert not smoe.lib.calls
     smoe.cache_append(cache, rows, rows, ints(2, 3), lens=ints(2))              # no rows of two sequences are fine
     assert smoe.lib.calls == ["smoe_cache_append"]
+
+
+def a_layer(m, B=3, N=2, k=2, E=4, d_model=256, h=2, d=64, **other):
+    """Arguments of momha_decode, some of them replaced."""
+    args = dict(X=Tensor(B * N, d_model), W_K=Tensor(d_model, h * d), W_V=Tensor(d_model, h * d), W_Q=Tensor(E, d_model, h * d), W_O=Tensor(E, h * d, d_model),
+                r=m.Routing(ints(B * N * k), ints(B * N * k), ints(E + 1), B * N * k, E), k=k, gates=Tensor(B * N, k, dtype=torch.float32), cache=a_cache(m, h, d),
+                block_table=ints(B, 3), lens=ints(B), rotary=a_table(m))
+    return m.momha_decode(**(args | other))
+
+
+def test_decoding_takes_key_and_value_weights_as_they_are_laid_out(smoe):
+    """A transposed matrix has as many elements, and would be read as another."""
+    for bad in (dict(W_K=Tensor(128, 256)), dict(W_V=Tensor(128, 256)), dict(W_K=Tensor(256, 64)), dict(W_V=Tensor(255, 128))):
+        with pytest.raises(ValueError):
+            a_layer(smoe, **bad)
+    assert not smoe.lib.calls
+    a_layer(smoe)
+    a_layer(smoe, W_K=Tensor(256, 2, 64), W_V=Tensor(256, 2, 64))               # the heads apart
+    assert smoe.lib.calls.count("smoe_momha_decode") == 2
