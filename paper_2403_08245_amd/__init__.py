@@ -618,6 +618,12 @@ def _places(dev: int, cache: KVCache, block_table, lens=None, seqs=None, positio
     return ctypes.byref(smoe_places(block_table.data_ptr(), B, width, seqs.data_ptr(), positions.data_ptr(), None)), seqs.numel()
 
 
+def _rows_of(cache: KVCache, t) -> bool:
+    """Does a row of t end as [h, d_head], or as both in one?  (Any other order of as many elements would be read as other rows.)"""
+    shape = t.shape
+    return shape[-2:] == (cache.h, cache.d_head) or shape[-1:] == (cache.h * cache.d_head,)
+
+
 def cache_append(cache: KVCache, K, V, block_table, lens=None, seqs=None, positions=None, rotary: RotaryTable | None = None, Q=None, out=None):
     """Writes the rows K, V [rows, h, d_head] (bf16) to the last places of every sequence (lens), or to the listed ones; with `rotary` K is
     turned first, and Q [rows, ..., d_head] into the returned tensor (`out`, which may be Q)."""
@@ -627,7 +633,7 @@ def cache_append(cache: KVCache, K, V, block_table, lens=None, seqs=None, positi
     row, n = cache.h * cache.d_head, K.numel()
     M = n // row
     B = block_table.shape[0]
-    if n != M * row or V.numel() != n or (M != rows if rows is not None else B == 0 or M % B):
+    if n != M * row or V.numel() != n or (M != rows if rows is not None else B == 0 or M % B) or not _rows_of(cache, K) or not _rows_of(cache, V):
         raise ValueError("K and V must be [rows, h, d_head], as many rows for each sequence")
     if rotary is not None and rotary.turns.get_device() != dev:
         raise ValueError(f"table on {rotary.turns.device}, but the current device is {dev}")
@@ -661,7 +667,7 @@ def cache_read(cache: KVCache, block_table, lens=None, seqs=None, positions=None
     else:
         K, V = out
         _here(dev, torch.bfloat16, K, V)
-        if K.numel() != rows * cache.h * cache.d_head or V.numel() != K.numel():
+        if K.numel() != rows * cache.h * cache.d_head or V.numel() != K.numel() or not _rows_of(cache, K) or not _rows_of(cache, V):
             raise ValueError("out must be two tensors [rows, h, d_head]")
     c, stream = _where(dev)
     _check(lib.smoe_cache_read(c, stream, BF16, cache._c, where, rows, K.data_ptr(), V.data_ptr()), "smoe_cache_read")

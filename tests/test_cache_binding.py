@@ -100,3 +100,22 @@ def test_decoding_takes_key_and_value_weights_as_they_are_laid_out(smoe):
     a_layer(smoe)
     a_layer(smoe, W_K=Tensor(256, 2, 64), W_V=Tensor(256, 2, 64))               # the heads apart
     assert smoe.lib.calls.count("smoe_momha_decode") == 2
+
+
+def test_rows_are_taken_as_they_are_laid_out(smoe):
+    """Rows that end in [h, d_head] or [h * d_head]; the same number of elements in another order would be read as other rows."""
+    cache, table, lens = a_cache(smoe), ints(3, 3), ints(3)
+    good = [Tensor(6, 2, 64), Tensor(3, 2, 2, 64), Tensor(6, 128), Tensor(3, 2, 128)]
+    bad = [Tensor(6, 64, 2), Tensor(2, 6, 64), Tensor(2, 3, 128, 1), Tensor(128, 6), Tensor(768), Tensor(12, 64)]
+    for x in good:
+        smoe.cache_append(cache, x, x, table, lens=lens)
+        smoe.cache_append(cache, x, good[0], table, lens=lens)
+        smoe.cache_read(cache, table, lens=lens, N=2, out=(x, x))
+    made = len(smoe.lib.calls)
+    assert made == 12
+    for x in bad:
+        for call in (lambda: smoe.cache_append(cache, x, good[0], table, lens=lens), lambda: smoe.cache_append(cache, good[0], x, table, lens=lens),
+                     lambda: smoe.cache_read(cache, table, lens=lens, N=2, out=(x, good[0])), lambda: smoe.cache_read(cache, table, lens=lens, N=2, out=(good[0], x))):
+            with pytest.raises(ValueError):
+                call()
+    assert len(smoe.lib.calls) == made
