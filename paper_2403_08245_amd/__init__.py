@@ -621,7 +621,8 @@ def _places(dev: int, cache: KVCache, block_table, lens=None, seqs=None, positio
 def _rows_of(cache: KVCache, t) -> bool:
     """Does a row of t end as [h, d_head], or as both in one?  (Any other order of as many elements would be read as other rows.)"""
     shape = t.shape
-    return shape[-2:] == (cache.h, cache.d_head) or shape[-1:] == (cache.h * cache.d_head,)
+    last = shape[-1]
+    return (last == cache.d_head and len(shape) > 1 and shape[-2] == cache.h) or last == cache.h * cache.d_head
 
 
 def cache_append(cache: KVCache, K, V, block_table, lens=None, seqs=None, positions=None, rotary: RotaryTable | None = None, Q=None, out=None):
@@ -633,7 +634,8 @@ def cache_append(cache: KVCache, K, V, block_table, lens=None, seqs=None, positi
     row, n = cache.h * cache.d_head, K.numel()
     M = n // row
     B = block_table.shape[0]
-    if n != M * row or V.numel() != n or (M != rows if rows is not None else B == 0 or M % B) or not _rows_of(cache, K) or not _rows_of(cache, V):
+    if n != M * row or (M != rows if rows is not None else B == 0 or M % B) or not _rows_of(cache, K) or \
+            (V.shape != K.shape and (V.numel() != n or not _rows_of(cache, V))):
         raise ValueError("K and V must be [rows, h, d_head], as many rows for each sequence")
     if rotary is not None and rotary.turns.get_device() != dev:
         raise ValueError(f"table on {rotary.turns.device}, but the current device is {dev}")
