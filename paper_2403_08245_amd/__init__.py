@@ -714,6 +714,7 @@ def momha_decode(X, W_K, W_V, W_Q, W_O, r: Routing, k: int, gates, cache: KVCach
     where, _ = _places(dev, cache, block_table, lens)
     _here(dev, torch.bfloat16, X, W_K, W_V, W_Q, W_O)
     _here(dev, torch.float32, gates)
+    _here(dev, torch.int32, r.sorted_expert_idxs, r.sorted_scattered_idxs, r.expert_offsets)
     if rotary is not None and rotary.turns.get_device() != dev:
         raise ValueError(f"table on {rotary.turns.device}, but the current device is {dev}")
     M, d_model = X.shape

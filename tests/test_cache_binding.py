@@ -119,3 +119,14 @@ def test_rows_are_taken_as_they_are_laid_out(smoe):
             with pytest.raises(ValueError):
                 call()
     assert len(smoe.lib.calls) == made
+
+
+def test_decoding_takes_routing_of_the_current_device(smoe):
+    """Its index arrays are read by the kernels as everything else is."""
+    for i in range(3):
+        arrays = [ints(12), ints(12), ints(5)]
+        for wrong, error in ((ints(*arrays[i].shape, device=1), ValueError), (ints(*arrays[i].shape, contiguous=False), ValueError),
+                             (Tensor(*arrays[i].shape, dtype=torch.int64), TypeError)):
+            with pytest.raises(error):
+                a_layer(smoe, r=smoe.Routing(*arrays[:i], wrong, *arrays[i + 1:], 12, 4))
+    assert not smoe.lib.calls
