@@ -484,6 +484,9 @@ def _here(dev: int, dtype, *tensors):
             raise ValueError(f"tensor on {t.device}, but the current device is {dev}")
 
 
+INT_MAX = 2 ** 31 - 1            # the library's sizes are 32 bits wide, and ctypes cuts a longer one down to them
+
+
 def _where(dev: int):
     """Context and stream of a launch."""
     return _ctx_by_device.get(dev) or ctx(dev), torch._C._cuda_getCurrentRawStream(dev)
@@ -540,6 +543,8 @@ def _turn(entry, what, Q, K, table, positions, out):
         if len(like) < 3 or like[0] != B or like[1] != T or like[-1] != d:
             raise ValueError("K must be [B, T, heads..., d] like Q")
         hk = math.prod(like[2:-1])
+    if B * T > INT_MAX or hq > INT_MAX or hk > INT_MAX or d > INT_MAX:
+        raise ValueError("more rows, heads or elements than 32 bits count")
     if positions is not None:
         _here(dev, torch.int32, positions)
         if positions.numel() != B * T:
@@ -607,6 +612,8 @@ def _places(dev: int, cache: KVCache, block_table, lens=None, seqs=None, positio
     if block_table.dim() != 2:
         raise ValueError("block_table must be [sequences, width]")
     B, width = block_table.shape
+    if B > INT_MAX or width > INT_MAX:
+        raise ValueError("block_table has more sequences or pages than 32 bits count")
     if lens is not None:
         _here(dev, torch.int32, lens)
         if seqs is not None or positions is not None or lens.numel() != B:

@@ -130,3 +130,23 @@ def test_decoding_takes_routing_of_the_current_device(smoe):
             with pytest.raises(error):
                 a_layer(smoe, r=smoe.Routing(*arrays[:i], wrong, *arrays[i + 1:], 12, 4))
     assert not smoe.lib.calls
+
+
+def test_sizes_past_32_bits_are_refused(smoe):
+    """The library counts rows and table entries in 32 bits: one that wrapped would turn, or look up, the wrong ones."""
+    table, cache = a_table(smoe), a_cache(smoe)
+    for shape in ((2, 2 ** 30, 1, 64), (2 ** 32 + 1, 1, 1, 64), (1, 2 ** 32 + 5, 1, 64), (1, 1, 2 ** 32 + 1, 64), (1, 1, 1, 2 ** 32 + 64)):
+        for entry in (smoe.rotary_fwd, smoe.rotary_bwd):
+            with pytest.raises(ValueError):
+                entry(Tensor(*shape), None, table)
+    with pytest.raises(ValueError):
+        smoe.rotary_fwd(Tensor(1, 1, 1, 64), Tensor(1, 1, 2 ** 32 + 1, 64), table)
+    one = Tensor(1, 2, 64)
+    for block_table, lens in ((ints(1, 2 ** 32 + 1), ints(1)), (ints(2 ** 32 + 1, 1), ints(2 ** 32 + 1))):
+        for call in (lambda: smoe.cache_append(cache, one, one, block_table, seqs=ints(1), positions=ints(1)), lambda: smoe.cache_read(cache, block_table, lens=lens),
+                     lambda: smoe.cached_attention_fwd(Tensor(block_table.shape[0], 1, 1, 2, 64), cache, block_table, lens)):
+            with pytest.raises(ValueError):
+                call()
+    assert not smoe.lib.calls
+    smoe.rotary_fwd(Tensor(1, 2 ** 31 - 1, 1, 64), None, table)
+    assert smoe.lib.calls == ["smoe_rotary_fwd"]
