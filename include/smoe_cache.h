@@ -5,8 +5,8 @@
  * The conventions are those of smoe.h: device pointers (unless said otherwise) on the context's device, contiguous
  * row-major tensors, int32 indices, no allocation, no synchronisation and no host copies, workspaces from the caller,
  * errors found before anything is enqueued, outputs overwritten, identical calls give identical bits.  Every tensor starts on a
- * 16-byte line.  The contents of index arrays live on the device: values out of range never lead to an access out of
- * bounds; what they do instead is said at each entry point.
+ * 16-byte line.  Outputs and workspaces that lie over a cache's pages are SMOE_ERR_INVALID_ARG.  The contents of index arrays live on
+ * the device: values out of range never lead to an access out of bounds; what they do instead is said at each entry point.
  */
 #ifndef SMOE_CACHE_H_
 #define SMOE_CACHE_H_
@@ -116,7 +116,8 @@ int smoe_cached_attention_fwd(smoe_ctx *ctx, void *stream, smoe_dtype dtype, con
  *   K = X W_K, V = X W_V and Q = ParallelLinear(X, W_Q, o), Q and K turned (rotary, or NULL), K and V appended, attention over the cache,
  *   O = ParallelLinear(Ohat, W_O, o, p).
  * X, O [B * N, d_model] in sequence order; weights, r, k and gates as in smoe_momha_fwd with T = N (h_expert and d_head
- * are the cache's).  lens counts the new positions in; rows past the table's end or with lens[b] < N are computed but not stored. */
+ * are the cache's).  lens counts the new positions in; rows past the table's end or with lens[b] < N are computed but not stored.
+ * O may be X; the workspace lies apart from X, gates and O, and O from gates (else SMOE_ERR_INVALID_ARG). */
 size_t smoe_momha_decode_workspace_bytes(int B, int N, int k, int d_model, int h_expert, int d_head);
 int smoe_momha_decode(smoe_ctx *ctx, void *stream, smoe_dtype dtype, const void *X, int N, int d_model, const void *W_K,
                       const void *W_V, const void *W_Q, const void *W_O, const smoe_routing *r, int k, const float *gates,

@@ -33,6 +33,10 @@ int rotary_args_ok(const smoe_rotary *r, int d_head) {
   if (((uintptr_t)r->turns & 7) || !std::isfinite(r->amplitude)) return SMOE_ERR_INVALID_ARG;
   return SMOE_OK;
 }
+bool over_pages(const smoe_cache *c, const void *p, size_t bytes) {
+  const size_t rows = (size_t)c->pages * c->h * c->page, stored = rows * c->d_head * (c->format == SMOE_CACHE_BF16 ? 2 : 1);
+  return overlap(p, bytes, c->K, stored) || overlap(p, bytes, c->V, stored) || overlap(p, bytes, c->K_exp, rows) || overlap(p, bytes, c->V_exp, rows);
+}
 
 extern "C" {
 
@@ -101,7 +105,7 @@ int smoe_cache_append(smoe_ctx *ctx, void *stream, smoe_dtype dtype, const smoe_
   if (!aligned16(K) || !aligned16(V) || !aligned16(Q) || !aligned16(Qr)) return SMOE_ERR_UNSUPPORTED;
   const int d = cache->d_head;
   const size_t q = (size_t)rows * hq * d * 2, k = (size_t)rows * cache->h * d * 2;
-  if (Q && ((Qr != Q && overlap(Qr, q, Q, q)) || overlap(Qr, q, K, k) || overlap(Qr, q, V, k))) return SMOE_ERR_INVALID_ARG;
+  if (Q && ((Qr != Q && overlap(Qr, q, Q, q)) || overlap(Qr, q, K, k) || overlap(Qr, q, V, k) || over_pages(cache, Qr, q))) return SMOE_ERR_INVALID_ARG;
   TurnArgs a;
   a.Q = Q; a.K = K; a.V = V; a.Qr = Qr;
   a.hq = Q ? hq : 0; a.hk = cache->h; a.rows = rows; a.d = d;
@@ -119,7 +123,7 @@ int smoe_cache_read(smoe_ctx *ctx, void *stream, smoe_dtype dtype, const smoe_ca
   if (!K || !V) return SMOE_ERR_INVALID_ARG;
   if (!aligned16(K) || !aligned16(V)) return SMOE_ERR_UNSUPPORTED;
   const size_t bytes = (size_t)rows * cache->h * cache->d_head * 2;
-  if (overlap(K, bytes, V, bytes)) return SMOE_ERR_INVALID_ARG;
+  if (overlap(K, bytes, V, bytes) || over_pages(cache, K, bytes) || over_pages(cache, V, bytes)) return SMOE_ERR_INVALID_ARG;
   return launch_cache_read((hipStream_t)stream, *cache, *places, rows, K, V);
 }
 
@@ -142,6 +146,7 @@ int smoe_cached_attention_fwd(smoe_ctx *ctx, void *stream, smoe_dtype dtype, con
   const size_t lse = (size_t)places->sequences * N * G * cache->h * sizeof(float);
   if ((O != Q && overlap(O, bytes, Q, bytes)) || overlap(LSE, lse, Q, bytes) || overlap(LSE, lse, O, bytes)) return SMOE_ERR_INVALID_ARG;
   if (need && (overlap(ws, need, Q, bytes) || overlap(ws, need, O, bytes) || overlap(ws, need, LSE, lse))) return SMOE_ERR_INVALID_ARG;
+  if (over_pages(cache, O, bytes) || over_pages(cache, LSE, lse) || (need && over_pages(cache, ws, need))) return SMOE_ERR_INVALID_ARG;
   return launch_cached_attention((hipStream_t)stream, Q, false, N, G, *cache, *places, O, LSE, ws);
 }
 
