@@ -603,11 +603,12 @@ __global__ void __launch_bounds__(64 * WAVES, RT == 1 && ONE ? 3 : 2)
       for (int e = 0; e < 4; ++e) sum[e] = fmaf(y[e], f, sum[e]);
     }
     if (pieces == 1) {
-      const float inv = total == 0.f ? 0.f : 1.f / total;
+      // nothing attended: zeros, also where weights of zero met infinite values and the sums are NaN
+      const float inv = 1.f / total;
       typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
       bf16x4 o;
 #pragma unroll
-      for (int e = 0; e < 4; ++e) o[e] = (bf16_t)(sum[e] * inv);
+      for (int e = 0; e < 4; ++e) o[e] = (bf16_t)(total == 0.f ? 0.f : sum[e] * inv);
       const size_t row = ((size_t)b * d.R + row0 + r) * c.h + hh;
       *reinterpret_cast<bf16x4 *>(O + row * D + x) = o;
       if (x == 0) LSE[row] = total == 0.f ? -INFINITY : fmaf(top, scale, __builtin_amdgcn_logf(total)) * 0.6931471805599453f;
@@ -690,11 +691,11 @@ template <int D, int JOIN_THREADS> __global__ void __launch_bounds__(JOIN_THREAD
 #pragma unroll
     for (int e = 0; e < 4; ++e) sum[e] = fmaf(s_acc[group + w][x + e], f, sum[e]);
   }
-  const float inv = total == 0.f ? 0.f : 1.f / total;
+  const float inv = 1.f / total;
   typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
   bf16x4 o;
 #pragma unroll
-  for (int e = 0; e < 4; ++e) o[e] = (bf16_t)(sum[e] * inv);
+  for (int e = 0; e < 4; ++e) o[e] = (bf16_t)(total == 0.f ? 0.f : sum[e] * inv);      // nothing attended: zeros, also where the sums are NaN
   const size_t row = ((size_t)at.b * d.R + tile * d.rows + r) * h + hh;
   *reinterpret_cast<bf16x4 *>(O + row * D + x) = o;
   if (x == 0) LSE[row] = total == 0.f ? -INFINITY : fmaf(top, scale, __builtin_amdgcn_logf(total)) * 0.6931471805599453f;
