@@ -76,7 +76,7 @@ typedef struct {
  * j * page .. j * page + page - 1 of a sequence.  Either
  *   seqs [rows], positions [rows] given, lens NULL: row i is that position of that sequence, in any order; or
  *   lens [sequences] given, seqs and positions NULL: rows = sequences * N, and row b * N + n is position
- *     lens[b] - N + n of sequence b: the last N positions of every sequence.
+ *     lens[b] - N + n (at least -2^31) of sequence b: the last N positions of every sequence.
  * A row whose sequence is outside [0, sequences), whose position is negative or past the table's width * page positions, or whose
  * page is outside [0, pages) has no place (padding). */
 typedef struct {

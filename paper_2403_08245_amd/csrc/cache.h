@@ -49,7 +49,8 @@ __device__ __forceinline__ int find_page(const smoe_places &p, int pages, int pa
 __device__ __forceinline__ void find_place(const smoe_places &p, int N, int row, int &seq, int &pos) {
   if (p.lens) {
     seq = row / N;
-    pos = p.lens[seq] - N + (row - seq * N);
+    const int back = N - (row - seq * N);
+    pos = max(p.lens[seq], (int)0x80000000 + back) - back;      // a length whose position would pass the least int32 has that one: no place
   } else {
     seq = p.seqs[row];
     pos = p.positions[row];

@@ -38,3 +38,23 @@ def test_a_query_that_attends_nothing_gives_zeros_whatever_the_values_hold(smoe,
     for b in (0, 2):
         assert bool((O[b] == 0).all()) and bool((L[b] == -np.inf).all())
     assert torch.equal(O[1], want[0][1]) and torch.equal(L[1], want[1][1])
+
+
+@pytest.mark.parametrize("rotary", [False, True])
+def test_lengths_at_the_ends_of_int32_have_no_places(smoe, rotary):
+    """lens[b] - N under -2^31 does not come out as a position at the other end: nothing is written, and reads are zeros.  (65540 new positions in a
+    table of 32767 pages of 65536, all of them the one page there is: 2^31 - 65540 would be one of its positions.)"""
+    N, page, width = 65540, 65536, 32767
+    _log(f"lengths at the ends of int32 rotary={rotary}")
+    cache = smoe.kv_cache(1, page, 1, 64)
+    for t in (cache.K, cache.V):
+        t.fill_(3.0)
+    table = torch.zeros(1, width, dtype=torch.int32).cuda()
+    K = torch.ones(N, 1, 64, dtype=torch.bfloat16).cuda()
+    more = dict(rotary=smoe.rotary_table(64)) if rotary else {}
+    for told in (-2 ** 31, -2 ** 31 + 3, -2 ** 31 + N - 1, -1, 0):
+        lens = torch.tensor([told], dtype=torch.int64).to(torch.int32).cuda()
+        smoe.cache_append(cache, K, K, table, lens=lens, **more)
+        assert bool((cache.K == 3.0).all()) and bool((cache.V == 3.0).all()), told
+        k, v = smoe.cache_read(cache, table, lens=lens, N=N)
+        assert not k.any() and not v.any(), told
