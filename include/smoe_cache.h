@@ -61,8 +61,10 @@ int smoe_rotary_bwd(smoe_ctx *ctx, void *stream, smoe_dtype dtype, const void *d
  *   E4M3  8-bit floating point (4 exponent and 3 mantissa bits, largest value 448, no infinities) with one power of two for each row
  *         and head: x is stored as round(x 2^-e) to the nearest, ties to even, and stands for it times 2^e; e is the smallest
  *         whole number >= -126 for which the row's largest finite |x| 2^-e is at most 448, kept as e + 127 in K_exp, V_exp
- *         [pages, h, page].  Powers of two cost a floating format no precision, and the stored values are exact in bf16.
- *         Infinities and NaN are stored as NaN.
+ *         [pages, h, page].  Powers of two cost a floating format no precision.  Infinities and NaN are stored as NaN; finite values that
+ *         would come out as 2^128 (from 1.9375 * 2^127 on) are stored as 240 * 2^120.  The stored values are exact in bf16 for
+ *         e >= -124, and for the rows of smaller e that were bf16 when they were stored; a key turned or projected as it is stored
+ *         (in fp32) may hold steps under bf16's least there, and is read rounded to the nearest.
  * page is a power of two, 16 .. 65536; d_head 64 or 128; K_exp and V_exp are NULL for BF16. */
 typedef enum { SMOE_CACHE_BF16 = 0, SMOE_CACHE_E4M3 = 1 } smoe_cache_format;
 typedef struct {

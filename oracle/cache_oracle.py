@@ -52,7 +52,7 @@ def e4m3_values():
 
 def e4m3_encode(row):
     """(codes, e): the smallest whole e >= -126 with the largest finite |x| 2^-e at most 448, and each x 2^-e as the code of the nearest
-    value, the even code of two equally near ones; NaN and infinities as a NaN code (0x7f)."""
+    value under 2^128, the even code of two equally near ones; NaN and infinities as a NaN code (0x7f)."""
     row = np.asarray(row, dtype=np.float64)
     finite = np.isfinite(row)
     amax = np.abs(row[finite]).max() if finite.any() else 0.0
@@ -71,6 +71,8 @@ def e4m3_encode(row):
             lo, hi = y - grid[j - 1], grid[j] - y
             if lo < hi or (lo == hi and (j - 1) % 2 == 0):
                 j -= 1
+        if grid[j] * 2.0 ** e >= 2.0 ** 128:     # finite values stay finite: 240 * 2^120 is the largest stored
+            j -= 1
         codes[i] = j | (128 if np.signbit(x) else 0)
     return codes, e
 

@@ -102,6 +102,10 @@ __device__ __forceinline__ uint2 to_e4m3(float (&y)[8], int lanes, unsigned int 
   const float inv = __uint_as_float((254u - byte) << 23);
 #pragma unroll
   for (int i = 0; i < 8; ++i) y[i] *= inv;
+  if (byte == 247u) {      // e = 120, of values past 1.75 * 2^127: the code above 240 would stand for 2^128, which neither bf16 nor fp32 holds
+#pragma unroll
+    for (int i = 0; i < 8; ++i) y[i] = fabsf(y[i]) > 240.f ? copysignf(240.f, y[i]) : y[i];
+  }
   uint2 q;
   int lo = __builtin_amdgcn_cvt_pk_fp8_f32(y[0], y[1], 0, false);
   q.x = (unsigned int)__builtin_amdgcn_cvt_pk_fp8_f32(y[2], y[3], lo, true);

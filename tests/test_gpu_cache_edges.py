@@ -5,6 +5,7 @@ import numpy as np
 import pytest
 import torch
 
+import oracle
 from test_gpu_cache import _case, _normal
 
 pytestmark = pytest.mark.gpu
@@ -58,3 +59,55 @@ def test_lengths_at_the_ends_of_int32_have_no_places(smoe, rotary):
         assert bool((cache.K == 3.0).all()) and bool((cache.V == 3.0).all()), told
         k, v = smoe.cache_read(cache, table, lens=lens, N=N)
         assert not k.any() and not v.any(), told
+
+
+@pytest.mark.parametrize("turned", [False, True])
+def test_the_largest_values_stay_finite_in_8_bits(smoe, turned):
+    """bf16 holds finite values up to (2 - 2^-7) 2^127.  Of a row whose scale is 2^120, those from 248 2^120 on are nearer to 2^128 than to 240 2^120,
+    but no type here holds 2^128: they are stored as the latter.  Everything else as ever.  (Turned by position 0, which changes nothing.)"""
+    _log(f"largest values in 8 bits turned={turned}")
+    top, page, d = torch.finfo(torch.bfloat16).max, 16, 64
+    big = 2.0 ** 127
+    heads = [top, -top, 1.9375 * big, -1.9375 * big, 1.9296875 * big, 1.875 * big, -1.8828125 * big, 1.75 * big]
+    x = _normal((8, 1, d), 321)
+    x[:, 0, ::7] *= 2.0 ** 120
+    for i, v in enumerate(heads):
+        x[i, 0, i] = v
+        x[i, 0, 20] = -v / 3
+    cache = smoe.kv_cache(1, page, 1, d, True)
+    table, lens = torch.zeros(1, 1, dtype=torch.int32).cuda(), torch.tensor([8], dtype=torch.int32).cuda()
+    at = dict(seqs=torch.zeros(8, dtype=torch.int32).cuda(), positions=torch.zeros(8, dtype=torch.int32).cuda()) if turned else dict(lens=lens)
+    if turned:                            # position 0 for each of them: one sequence each
+        table = torch.arange(8, dtype=torch.int32)[:, None].cuda()
+        cache = smoe.kv_cache(8, page, 1, d, True)
+        at["seqs"] = torch.arange(8, dtype=torch.int32).cuda()
+    smoe.cache_append(cache, x.cuda(), x.cuda(), table, rotary=smoe.rotary_table(d) if turned else None, **at)
+    read = smoe.cache_read(cache, table, **(at if turned else dict(at, N=8)))
+    value = oracle.e4m3_values()
+    want = np.stack([value[c] * 2.0 ** e for c, e in map(oracle.e4m3_encode, x.double().numpy().reshape(8, d))])
+    want = np.clip(want, -240 * 2.0 ** 120, 240 * 2.0 ** 120)
+    for t in read:
+        assert bool(t.isfinite().all()) and np.array_equal(t.double().cpu().numpy().reshape(8, d), want)
+
+
+def test_every_stored_value_is_read_as_it_is(smoe):
+    """All 256 codes at scales over the whole range: exact in bf16, but for e < -124, where the smallest steps (2^-9 2^e) lie under bf16's least (2^-133)
+    and the value is rounded to the nearest once."""
+    _log("every stored value")
+    bytes_ = [1, 2, 3, 4, 60, 127, 200, 246]
+    codes = torch.arange(256, dtype=torch.uint8).view(4, 64)
+    cache = smoe.kv_cache(len(bytes_), 16, 1, 64, True)
+    for i, e in enumerate(bytes_):
+        for t, exps in ((cache.K, cache.K_exp), (cache.V, cache.V_exp)):
+            t[i, 0, :4] = codes.cuda()
+            exps[i, 0, :4] = e
+    table = torch.arange(len(bytes_), dtype=torch.int32)[:, None].cuda()
+    lens = torch.full((len(bytes_),), 4, dtype=torch.int32).cuda()
+    for t in smoe.cache_read(cache, table, lens=lens, N=4):
+        got = t.double().cpu().numpy().reshape(len(bytes_), 256)
+        for row, e in zip(got, bytes_):
+            want = oracle.e4m3_values() * 2.0 ** (e - 127)
+            step = np.exp2(np.maximum(np.floor(np.log2(np.maximum(np.abs(want), 2.0 ** -126))) - 7, -133))
+            nearest = np.where(np.isnan(want), want, np.rint(want / step) * step)
+            assert np.array_equal(row, nearest, equal_nan=True), e
+            assert e < 3 or np.array_equal(nearest, want, equal_nan=True)
