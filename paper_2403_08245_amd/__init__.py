@@ -476,11 +476,11 @@ def _device(first: torch.Tensor) -> int:
 def _here(dev: int, dtype, *tensors):
     """_chk, and that the tensors live on the current device."""
     for t in tensors:
-        if not t.is_cuda or not t.is_contiguous():
+        if not t.is_contiguous():
             raise ValueError("tensors must be contiguous device tensors")
         if t.dtype != dtype:
             raise TypeError(f"expected {dtype}, got {t.dtype}")
-        if t.get_device() != dev:
+        if t.get_device() != dev:                 # -1 for one in host memory
             raise ValueError(f"tensor on {t.device}, but the current device is {dev}")
 
 
@@ -543,7 +543,7 @@ def _turn(entry, what, Q, K, table, positions, out):
         if len(like) < 3 or like[0] != B or like[1] != T or like[-1] != d:
             raise ValueError("K must be [B, T, heads..., d] like Q")
         hk = math.prod(like[2:-1])
-    if B * T > INT_MAX or hq > INT_MAX or hk > INT_MAX or d > INT_MAX:
+    if (B * T | hq | hk | d) > INT_MAX:           # any of them
         raise ValueError("more rows, heads or elements than 32 bits count")
     if positions is not None:
         _here(dev, torch.int32, positions)
@@ -605,24 +605,24 @@ def kv_cache(pages: int, page: int, h: int, d_head: int, quantised: bool = False
 
 
 def _places(dev: int, cache: KVCache, block_table, lens=None, seqs=None, positions=None):
-    """The ctypes view of where rows live, and how many rows `seqs` names (None with lens)."""
+    """The ctypes view of where rows live, how many sequences the table has and how many rows `seqs` names (None with lens)."""
     if cache.device != dev:
         raise ValueError(f"cache on device {cache.device}, but the current device is {dev}")
     _here(dev, torch.int32, block_table)
     if block_table.dim() != 2:
         raise ValueError("block_table must be [sequences, width]")
     B, width = block_table.shape
-    if B > INT_MAX or width > INT_MAX:
+    if (B | width) > INT_MAX:                     # either
         raise ValueError("block_table has more sequences or pages than 32 bits count")
     if lens is not None:
         _here(dev, torch.int32, lens)
         if seqs is not None or positions is not None or lens.numel() != B:
             raise ValueError("give lens [sequences], or seqs and positions")
-        return ctypes.byref(smoe_places(block_table.data_ptr(), B, width, None, None, lens.data_ptr())), None
+        return ctypes.byref(smoe_places(block_table.data_ptr(), B, width, None, None, lens.data_ptr())), B, None
     if seqs is None or positions is None or seqs.numel() != positions.numel():
         raise ValueError("give lens [sequences], or seqs and positions of the same length")
     _here(dev, torch.int32, seqs, positions)
-    return ctypes.byref(smoe_places(block_table.data_ptr(), B, width, seqs.data_ptr(), positions.data_ptr(), None)), seqs.numel()
+    return ctypes.byref(smoe_places(block_table.data_ptr(), B, width, seqs.data_ptr(), positions.data_ptr(), None)), B, seqs.numel()
 
 
 def _rows_of(cache: KVCache, t) -> bool:
@@ -636,11 +636,10 @@ def cache_append(cache: KVCache, K, V, block_table, lens=None, seqs=None, positi
     """Writes the rows K, V [rows, h, d_head] (bf16) to the last places of every sequence (lens), or to the listed ones; with `rotary` K is
     turned first, and Q [rows, ..., d_head] into the returned tensor (`out`, which may be Q)."""
     dev = _device(K)
-    where, rows = _places(dev, cache, block_table, lens, seqs, positions)
+    where, B, rows = _places(dev, cache, block_table, lens, seqs, positions)
     _here(dev, torch.bfloat16, K, V)
     row, n = cache.h * cache.d_head, K.numel()
     M = n // row
-    B = block_table.shape[0]
     if n != M * row or (M != rows if rows is not None else B == 0 or M % B) or not _rows_of(cache, K) or \
             (V.shape != K.shape and (V.numel() != n or not _rows_of(cache, V))):
         raise ValueError("K and V must be [rows, h, d_head], as many rows for each sequence")
@@ -649,8 +648,9 @@ def cache_append(cache: KVCache, K, V, block_table, lens=None, seqs=None, positi
     hq, Qr = 0, None
     if Q is not None:
         _here(dev, torch.bfloat16, Q)
-        hq = Q.numel() // max(1, M * cache.d_head)
-        if rotary is None or Q.numel() != M * hq * cache.d_head or Q.shape[-1] != cache.d_head:
+        of_q, of_head = Q.numel(), M * cache.d_head
+        hq = of_q // max(1, of_head)
+        if rotary is None or of_q != of_head * hq or Q.shape[-1] != cache.d_head:
             raise ValueError("Q must be [rows, heads..., d_head], and goes with rotary")
         if out is None:
             Qr = _like(Q)
@@ -669,8 +669,8 @@ def cache_append(cache: KVCache, K, V, block_table, lens=None, seqs=None, positi
 def cache_read(cache: KVCache, block_table, lens=None, seqs=None, positions=None, N: int = 1, out=None):
     """K, V [rows, h, d_head] (bf16) of the listed places, or of the last N of every sequence (lens)."""
     dev = _device(cache.K)
-    where, rows = _places(dev, cache, block_table, lens, seqs, positions)
-    rows = block_table.shape[0] * N if rows is None else rows
+    where, B, rows = _places(dev, cache, block_table, lens, seqs, positions)
+    rows = B * N if rows is None else rows
     if out is None:
         K, V = (_new(rows, cache.h, cache.d_head, dtype=torch.bfloat16, device=cache.K.device) for _ in "KV")
     else:
@@ -687,12 +687,12 @@ def cached_attention_fwd(Q, cache: KVCache, block_table, lens, out=None, ws=None
     """Q [B, N, G, h, d_head] (bf16), the last N positions of every sequence, over the cache -> O like Q, LSE [B, N, G, h] fp32.
     out = (O, LSE) and ws reuse tensors; O may be Q."""
     dev = _device(Q)
-    where, _ = _places(dev, cache, block_table, lens)
+    where, sequences, _ = _places(dev, cache, block_table, lens)
     _here(dev, torch.bfloat16, Q)
     if Q.dim() != 5:
         raise ValueError("Q must be [sequences, N, G, h, d_head]")
     B, N, G, h, d = Q.shape
-    if h != cache.h or d != cache.d_head or B != block_table.shape[0]:
+    if h != cache.h or d != cache.d_head or B != sequences:
         raise ValueError("Q must be [sequences, N, G, h, d_head] with the cache's h and d_head")
     if out is None:
         O, LSE = _new(B, N, G, h, d, dtype=torch.bfloat16, device=Q.device), _new(B, N, G, h, dtype=torch.float32, device=Q.device)
@@ -718,18 +718,18 @@ def momha_decode(X, W_K, W_V, W_Q, W_O, r: Routing, k: int, gates, cache: KVCach
     """The SMoE attention layer on the last N positions of every sequence, X [B*N, d_model], over a cache that holds the earlier ones and
     receives these; W_K and W_V [d_model, h * d_head], W_Q [E, d_model, h * d_head], W_O [E, h * d_head, d_model].  Returns O [B*N, d_model]."""
     dev = _device(X)
-    where, _ = _places(dev, cache, block_table, lens)
+    where, B, _ = _places(dev, cache, block_table, lens)
     _here(dev, torch.bfloat16, X, W_K, W_V, W_Q, W_O)
     _here(dev, torch.float32, gates)
     _here(dev, torch.int32, r.sorted_expert_idxs, r.sorted_scattered_idxs, r.expert_offsets)
     if rotary is not None and rotary.turns.get_device() != dev:
         raise ValueError(f"table on {rotary.turns.device}, but the current device is {dev}")
     M, d_model = X.shape
-    B, d_out = block_table.shape[0], cache.h * cache.d_head
+    d_out = cache.h * cache.d_head
     if B == 0 or M == 0 or M % B or gates.numel() != M * k:
         raise ValueError("X must be [sequences * N, d_model] and gates hold k for each row")
     for W in (W_K, W_V):
-        if W.shape[0] != d_model or W.numel() != d_model * d_out:
+        if W.shape != (d_model, d_out) and W.shape != (d_model, cache.h, cache.d_head):
             raise ValueError("W_K and W_V must be [d_model, h * d_head]")
     if W_Q.shape != (r.E, d_model, d_out) or W_O.shape != (r.E, d_out, d_model):
         raise ValueError("weights do not fit d_model and the cache's h * d_head")
