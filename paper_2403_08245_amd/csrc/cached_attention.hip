@@ -710,8 +710,9 @@ constexpr size_t MAX_SLOTS = 2 * MAX_TARGET;
 bool cached_attention_fits(int B, int N, int G, int h) {
   // query rows within 31 bits, and one-dimensional grids of fewer than 2^32 threads
   const long long R = (long long)N * G;
-  return R <= 0x7fffffffLL && B * (double)R * h <= 0x7fffffff &&
-         (long long)ceil_div((int)R, 16 * row_tiles((int)R)) * h * B <= 0x7fffffffLL / 256 - 2 * MAX_TARGET;
+  if (R > 0x7fffffffLL || B * (double)R * h > 0x7fffffff) return false;
+  const long long rows = 16 * row_tiles((int)R);
+  return (R + rows - 1) / rows * h * B <= 0x7fffffffLL / 256 - 2 * MAX_TARGET;
 }
 
 size_t cached_attention_workspace_bytes(int N, int G, int d_head, int positions) {

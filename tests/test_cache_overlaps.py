@@ -70,3 +70,17 @@ def test_calls_whose_arrays_lie_apart_are_not_refused(world):
     for name in ("append", "read", "attend", "decode"):
         assert call(name, caches["bf16"], **far) == -4, name
     assert call("decode", caches["bf16"], **(far | dict(O=at["X"]))) == -4           # X is read before O is written
+
+
+def test_more_query_rows_than_a_launch_holds(world):
+    """Up to 2^31 - 1 of them: refused, and no workspace asked for, where the count of their tiles would pass 32 bits, too."""
+    import paper_2403_08245_amd as m
+    _, at, caches, keep = world
+    ref, ctx = ctypes.byref, ctypes.addressof(keep)
+    one = m.smoe_cache(at["K"], at["V"], None, None, 4, 16, 1, 64, 0)
+    where = m.smoe_places(at["table"], 1, 100, None, None, at["lens"])
+    for N, G in ((2 ** 31 - 1, 1), (1, 2 ** 31 - 1), (2 ** 31 - 31, 1), (2 ** 30, 1), (32768, 65535)):
+        assert m.lib.smoe_cached_attention_workspace_bytes(ref(one), ref(where), N, G) == 0, (N, G)
+        assert m.lib.smoe_cached_attention_fwd(ctx, None, 1, 1 << 50, N, G, ref(one), ref(where), 1 << 51, 1 << 52, 1 << 53, 1 << 40) == -2, (N, G)
+        assert m.lib.smoe_momha_decode_workspace_bytes(1, N, G, 64, 1, 64) == 0, (N, G)
+    assert m.lib.smoe_cached_attention_workspace_bytes(ref(one), ref(where), 2 ** 20, 1) > 0
