@@ -65,7 +65,8 @@ int smoe_rotary_bwd(smoe_ctx *ctx, void *stream, smoe_dtype dtype, const void *d
  *         would come out as 2^128 (from 1.9375 * 2^127 on) are stored as 240 * 2^120.  The stored values are exact in bf16 for
  *         e >= -124, and for the rows of smaller e that were bf16 when they were stored; a key turned or projected as it is stored
  *         (in fp32) may hold steps under bf16's least there, and is read rounded to the nearest.
- * page is a power of two, 16 .. 65536; d_head 64 or 128; K_exp and V_exp are NULL for BF16. */
+ * page is a power of two, 16 .. 65536; d_head 64 or 128; K_exp and V_exp are NULL for BF16.  Calls that write to a cache refuse one whose
+ * arrays share memory. */
 typedef enum { SMOE_CACHE_BF16 = 0, SMOE_CACHE_E4M3 = 1 } smoe_cache_format;
 typedef struct {
   void *K, *V;             /* bf16 or e4m3 */

@@ -1033,7 +1033,7 @@ int smoe_momha_decode(smoe_ctx *ctx, void *stream, smoe_dtype dtype, const void 
   const int M = B * N, d_out = h * d_head;
   // O may be X, which only earlier launches read
   const size_t rows = (size_t)M * d_model * 2, weighing = (size_t)M * k * sizeof(float);
-  if (over_pages(cache, O, rows) || over_pages(cache, ws, need) || overlap(ws, need, O, rows) || overlap(ws, need, X, rows) || overlap(ws, need, gates, weighing) || overlap(O, rows, gates, weighing))
+  if (!pages_apart(cache) || over_pages(cache, O, rows) || over_pages(cache, ws, need) || overlap(ws, need, O, rows) || overlap(ws, need, X, rows) || overlap(ws, need, gates, weighing) || overlap(O, rows, gates, weighing))
     return SMOE_ERR_INVALID_ARG;
   MomhaSizes z = momha_sizes(B, N, k, d_model, h, d_head);
   char *p = (char *)ws;

@@ -37,6 +37,11 @@ bool over_pages(const smoe_cache *c, const void *p, size_t bytes) {
   const size_t rows = (size_t)c->pages * c->h * c->page, stored = rows * c->d_head * (c->format == SMOE_CACHE_BF16 ? 2 : 1);
   return overlap(p, bytes, c->K, stored) || overlap(p, bytes, c->V, stored) || overlap(p, bytes, c->K_exp, rows) || overlap(p, bytes, c->V_exp, rows);
 }
+bool pages_apart(const smoe_cache *c) {
+  const size_t rows = (size_t)c->pages * c->h * c->page, stored = rows * c->d_head * (c->format == SMOE_CACHE_BF16 ? 2 : 1);
+  return !overlap(c->K, stored, c->V, stored) && !overlap(c->K_exp, rows, c->V_exp, rows) && !overlap(c->K, stored, c->K_exp, rows) &&
+         !overlap(c->K, stored, c->V_exp, rows) && !overlap(c->V, stored, c->K_exp, rows) && !overlap(c->V, stored, c->V_exp, rows);
+}
 
 extern "C" {
 
@@ -106,6 +111,7 @@ int smoe_cache_append(smoe_ctx *ctx, void *stream, smoe_dtype dtype, const smoe_
   const int d = cache->d_head;
   const size_t q = (size_t)rows * hq * d * 2, k = (size_t)rows * cache->h * d * 2;
   if (Q && ((Qr != Q && overlap(Qr, q, Q, q)) || overlap(Qr, q, K, k) || overlap(Qr, q, V, k) || over_pages(cache, Qr, q))) return SMOE_ERR_INVALID_ARG;
+  if (!pages_apart(cache)) return SMOE_ERR_INVALID_ARG;
   TurnArgs a;
   a.Q = Q; a.K = K; a.V = V; a.Qr = Qr;
   a.hq = Q ? hq : 0; a.hk = cache->h; a.rows = rows; a.d = d;

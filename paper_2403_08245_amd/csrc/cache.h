@@ -38,6 +38,7 @@ int cache_args_ok(const smoe_cache *c);
 int lengths_ok(const smoe_cache *c, const smoe_places *p);   // the form with lens
 int rotary_args_ok(const smoe_rotary *r, int d_head);
 bool over_pages(const smoe_cache *c, const void *p, size_t bytes);   // does an array share memory with the cache's?
+bool pages_apart(const smoe_cache *c);                               // do its own arrays lie apart, as who writes to it needs?
 
 // The page of a sequence's position, or -1.
 __device__ __forceinline__ int find_page(const smoe_places &p, int pages, int page_shift, int seq, int pos) {

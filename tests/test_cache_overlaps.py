@@ -84,3 +84,20 @@ def test_more_query_rows_than_a_launch_holds(world):
         assert m.lib.smoe_cached_attention_fwd(ctx, None, 1, 1 << 50, N, G, ref(one), ref(where), 1 << 51, 1 << 52, 1 << 53, 1 << 40) == -2, (N, G)
         assert m.lib.smoe_momha_decode_workspace_bytes(1, N, G, 64, 1, 64) == 0, (N, G)
     assert m.lib.smoe_cached_attention_workspace_bytes(ref(one), ref(where), 2 ** 20, 1) > 0
+
+
+@pytest.mark.parametrize("format", ["bf16", "e4m3"])
+def test_writing_to_a_cache_whose_arrays_share_memory(world, format):
+    """Keys would be written over values.  (Attention and reads of such a cache are fine: one array for both, say.)"""
+    import paper_2403_08245_amd as m
+    call, at, caches, _ = world
+    far = {x: y + (1 << 36) for x, y in at.items() if x in ("gates", "routing", "rows", "vals")}
+    size = 4 * 2 * 16 * 64 * (2 if format == "bf16" else 1)
+    pairs = [("V", "K", 0), ("V", "K", size - 16), ("K", "V", size - 16)]
+    if format == "e4m3":
+        pairs += [("V_exp", "K_exp", 0), ("K_exp", "V", 32), ("V_exp", "K", size - 16), ("K", "V_exp", 112)]
+    for moved, onto, by in pairs:
+        c = m.smoe_cache.from_buffer_copy(caches[format])
+        setattr(c, moved, getattr(c, onto) + by)
+        for name in ("append", "decode"):
+            assert call(name, c, **far) == -1, (moved, onto, name)
