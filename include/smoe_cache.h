@@ -118,6 +118,10 @@ int smoe_cached_attention_fwd(smoe_ctx *ctx, void *stream, smoe_dtype dtype, con
  * smoe_momha_fwd for the last N positions of every sequence, over a cache that holds the earlier ones:
  *   K = X W_K, V = X W_V and Q = ParallelLinear(X, W_Q, o), Q and K turned (rotary, or NULL), K and V appended, attention over the cache,
  *   O = ParallelLinear(Ohat, W_O, o, p).
+ * What the layer's tensors are rounded to follows from the batch: up to 512 rows, d_model a multiple of 32 and 32 rows an expert or fewer on
+ * average, K and V are rounded once, as they are stored, Ohat once, and Q and the slots' outputs are fp32; past that Q and the slots'
+ * outputs are bf16, and past 512 rows or off the multiple of 32 so are K and V before they are turned.  (Error of O against 64 bits,
+ * root mean square: 1.6e-3 to 2.4e-3, and 3.0e-3 to 3.7e-3.)
  * X, O [B * N, d_model] in sequence order; weights, r, k and gates as in smoe_momha_fwd with T = N (h_expert and d_head
  * are the cache's).  lens counts the new positions in; rows past the table's end or with lens[b] < N are computed but not stored.
  * O may be X; the workspace lies apart from X, gates and O, and O from gates (else SMOE_ERR_INVALID_ARG). */

@@ -341,6 +341,8 @@ __global__ void __launch_bounds__(64 * WAVES, RT == 1 && ONE ? 3 : 2)
   constexpr int KS = D / 32, COLS = D / 16, ROW = D + 4;     // padded: a wavefront's 16 rows start in 16 different banks
   // The queries' fragments: in registers, or, two tiles of them or two numbers each, in LDS, until the piece ends (held in registers they
   // spilled, and a reload in the loop waits for every request under way: two sequences of 90001 and 131072 positions in e4m3 133 us).
+  // Two tiles of heads of 128 still take all 256 registers and spill some, 15 in bf16 and 4 in e4m3 (7 with fp32 queries): stored before, and
+  // reloaded in and behind, the loop of the last steps, where not every query sees every key; the loop of the others has no access to scratch.
   constexpr bool SHARED = RT > 1 || WIDE;
   constexpr int FRAGS = RT * KS * (WIDE ? 2 : 1);
   union Shared {
@@ -437,7 +439,7 @@ __global__ void __launch_bounds__(64 * WAVES, RT == 1 && ONE ? 3 : 2)
     return x;
   };
   // The keys of the next step are requested when this one's have met the queries, its values when this one's have met the weights: a
-  // wavefront always has requests of 8 to 16 KB under way.
+  // wavefront always has requests of 8 to 16 KB under way in bf16 and heads of 128, half of it in e4m3, and half of either in heads of 64.
   Keys<D, FORMAT> k;
   Values<D, FORMAT> v;
   const int k_at = Keys<D, FORMAT>::lane_offset(lane), v_at = Values<D, FORMAT>::lane_offset(lane);

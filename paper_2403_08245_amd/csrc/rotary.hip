@@ -17,7 +17,8 @@ namespace {
 constexpr int WAVES = 4;
 constexpr int MAX_PAIRS = 256;      // rows of at most 512 elements
 // Rows a lane has in flight.  2: a decoding step's four tokens 3.0 us, the queries and keys of 8192 tokens (16 + 4 heads of 128) 19.4; 4: 3.5
-// and 21.2; 1: 2.9 and 18.5, but rows of 64 half turned 26.4 instead of 22.2.
+// and 21.2; 1: 2.9 and 18.5, but rows of 64 half turned 26.4 instead of 22.2.  (One launch behind another, from a captured graph; by
+// itself, under a trace, the first is 3.5.)
 constexpr int BATCH = 2;
 constexpr int TOKENS = 16;          // of a wavefront, where rows are copied between the cache and plain tensors
 constexpr int MOST = 8;             // rounds of rows a wavefront takes (32768 tokens of 36 heads: 4 108.6, 8 107.9, 16 116 us)
@@ -275,9 +276,9 @@ __global__ void __launch_bounds__(64 * WAVES) turn_rows_kernel(TurnArgs a, smoe_
 // of one head, keys or values: positions that follow one another lie side by side on a page, so that what it writes there (or
 // reads) is 2 or 4 KB in a row, and the 16 exponents one piece.  Rows on their way into the cache are dead afterwards and kept by no cache;
 // ONCE: nor is what is written, where it is more than the caches could hold until it is used.
-// Quantising 51 thousand tokens of 8 heads, 213 MB, us: 49.5 so (46.8 with the pages past the caches, too, which costs 12 if they are read
+// Quantising 34.7 thousand tokens of 8 heads, 213 MB, us: 49.5 so (46.8 with the pages past the caches, too, which costs 12 if they are read
 // back next; 53.6 all through the caches; 51 with a token a wavefront); of 4 heads of 64 16.6 (18.1; 35.5 with a token a wavefront).  Reading the
-// former back, 209 MB of rows: 33.1 past the caches, 47.9 through them.
+// former back, 213 MB again: 33.1 past the caches, 47.9 through them.
 template <int FORMAT, bool WRITE, int D, bool ONCE>
 __global__ void __launch_bounds__(64 * WAVES) cache_rows_kernel(smoe_cache c, smoe_places places, bf16_t *K, bf16_t *V, int tokens, int N, int page_shift, unsigned int items) {
   constexpr int LANES = D / 8, AT_ONCE = 64 / LANES, ROUNDS = TOKENS / AT_ONCE;
