@@ -204,6 +204,7 @@ __global__ void __launch_bounds__(64 * WAVES) turn_rows_kernel(TurnArgs a, smoe_
   for (int i = lane; i < half; i += 64) {
     const uint32_t part = (uint32_t)((a.rotary.turns[i] * (uint64_t)(int64_t)pos) >> 32);
     float s, k;
+    // to 24 bits of half a turn, 9.4e-8 radians at most: fp32 rows come out 2.8e-8 off in the root mean square, 2.2e-8 with the angle in 64 bits
     sincospif((float)(int32_t)part * 0x1p-31f, &s, &k);
     angle[i] = make_float2(k * a.rotary.amplitude, (a.back ? -s : s) * a.rotary.amplitude);
   }
