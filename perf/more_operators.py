@@ -1,0 +1,412 @@
+"""Operators of a transformer block around its experts, as a training or serving program calls them.
+
+listed() names the calls that are timed, draw() samples more of the same ranges, prepare() makes what such a program
+holds before the call (logits, activations, packed weights, routing), run() is one pass: with `own` through the package's entry
+points, otherwise in plain torch operations in 32 bits.  work() says what a pass cannot do without, exact() computes its result
+in 64 bits from the definitions.
+
+The operators: the router's gate by softmax or sigmoid scores, with a bias for balance, groups of experts, renormalised weights and its
+gradient; the root-mean-square norm of a residual stream with the addition in front of it, its gradient, and its output in 8 bits; the
+experts' products (Alg. 1 and Alg. 3 forward) on activations and weights in 8 bits.  8 bits are e4m3 with a power of two for every 32
+elements of a row.  Sizes are those of the layers this repository benchmarks (2048 -> 2 x 512 on 64 experts with k = 8, 4096 -> 2 x 14336 on
+8 experts with k = 2) and generic ragged ones.
+"""
+from __future__ import annotations
+
+import math
+
+import torch
+
+own = False
+
+DTYPES = {"bf16": torch.bfloat16, "f32": torch.float32}
+BLOCK = 32                    # elements of a row that share a power of two
+
+
+# ---------------------------------------------------------------------------------------------------------------- cases
+def _gate(T, E, k, score, bias=False, groups=1, kept=1, best=1, renormalise=True, scale=1.0, grad=True, name=None):
+    """best: a group counts as the sum of so many of its largest scores."""
+    c = dict(kind="gate", T=T, E=E, k=k, score=score, bias=bias, groups=groups, kept=kept, best=best, renormalise=renormalise, scale=scale, grad=grad)
+    return dict(c, name=name) if name else c
+
+
+def _norm(kind, rows, d, dtype="bf16", residual=True, grad=True, name=None):
+    c = dict(kind=kind, rows=rows, d=d, dtype=dtype, residual=residual, grad=grad)
+    return dict(c, name=name) if name else c
+
+
+def _experts(T, d_model, d_expert, E, k, act="swiglu", skew=0.0, name=None):
+    c = dict(kind="experts", T=T, d_model=d_model, d_expert=d_expert, E=E, k=k, act=act, skew=skew)
+    return dict(c, name=name) if name else c
+
+
+def _linear(T, d_in, d_out, E, k, gates=True, skew=0.0, name=None):
+    c = dict(kind="linear", T=T, d_model=d_in, d_out=d_out, E=E, k=k, gates=gates, skew=skew)
+    return dict(c, name=name) if name else c
+
+
+def listed():
+    return [
+        # router of four decoding sequences, 256 experts in 8 groups of which 4 are kept, biased sigmoid scores: latency
+        _gate(4, 256, 8, "sigmoid", True, 8, 4, 2, True, 2.5, grad=False, name="gate-decode"),
+        # router of a training step of the granular layer with softmax scores over all experts, kept as they are, and its gradient
+        _gate(16384, 64, 8, "softmax", renormalise=False, name="gate-train"),
+        # router of a training step with many experts in groups, balanced by a bias
+        _gate(32768, 256, 8, "sigmoid", True, 8, 4, 2, True, 2.5, name="gate-grouped-train"),
+        # the norm in front of the experts in a decoding step of four sequences: latency
+        _norm("norm", 4, 4096, grad=False, name="norm-decode"),
+        # the same in a training step, with the gradient of the stream that goes on past it
+        _norm("norm", 8192, 2048, name="norm-train"),
+        # a validation run in fp32, rows of odd width, nothing added
+        _norm("norm", 1999, 999, "f32", residual=False, name="norm-f32"),
+        # the norm of a prompt batch, in bf16 for the router and in 8 bits for the experts, read back
+        _norm("norm8", 8191, 4096, grad=False, name="norm8-prompts"),
+        # experts of four decoding sequences, weights and activations in 8 bits: latency
+        _experts(4, 2048, 512, 64, 8, name="experts8-decode-4"),
+        # a full decoding batch of the same layer: its weights' bytes
+        _experts(64, 2048, 512, 64, 8, name="experts8-decode-64"),
+        # a prompt chunk of ragged length, between the decoding batches and the large ones
+        _experts(777, 2048, 512, 64, 8, name="experts8-prefill-777"),
+        # one product by itself with its weighted sum: an output projection over 16 experts, ragged length
+        _linear(4099, 2048, 1536, 16, 4, name="linear8-4099"),
+        # prompts through the wide layer, unbalanced experts: matrix rate
+        _experts(16384, 4096, 14336, 8, 2, skew=1.2, name="experts8-wide"),
+    ]
+
+
+def _spread(rng, lo, hi):
+    """A whole number from lo to hi, even over the logarithm."""
+    return int(round(math.exp(rng.uniform(math.log(lo), math.log(hi)))))
+
+
+def _width(rng, lo, hi):
+    """A row width of whole blocks; two in three are multiples of 128."""
+    step = rng.choice([128, 128, 32])
+    return max(step, int(round(_spread(rng, lo, hi) / step)) * step)
+
+
+def _draw_once(rng):
+    kind = rng.choice(["gate", "gate", "gate", "norm", "norm", "norm8", "experts", "experts", "experts", "linear"])
+    if kind == "gate":
+        E = rng.choice([8, 16, 60, 64, 96, 128, 160, 256, 384, 512])
+        groups = rng.choice([1, 1] + [g for g in (2, 4, 5, 8, 16) if E % g == 0 and E // g >= 2])
+        kept = rng.randint(1, groups)
+        k = rng.randint(1, min(16, kept * (E // groups)))
+        score = rng.choice(["softmax", "sigmoid"])
+        return _gate(_spread(rng, 1, 32768), E, k, score, rng.random() < 0.5, groups, kept, rng.choice([1, 2]), rng.random() < 0.6,
+                     rng.choice([1.0, 2.5, 16.0]), rng.random() < 0.7)
+    if kind == "norm":
+        d = rng.choice([_width(rng, 64, 8192), _width(rng, 64, 8192), _spread(rng, 33, 8192)])
+        return _norm(kind, _spread(rng, 1, 32768), d, rng.choice(["bf16", "bf16", "f32"]), rng.random() < 0.7, rng.random() < 0.7)
+    if kind == "norm8":
+        return _norm(kind, _spread(rng, 1, 32768), _width(rng, 64, 8192), rng.choice(["bf16", "bf16", "f32"]), rng.random() < 0.7, False)
+    E = _spread(rng, 4, 64)
+    k, skew = min(E, rng.choice([1, 2, 2, 3, 4, 6, 8])), rng.choice([0.0, 0.0, 0.6, 1.2])
+    if kind == "linear":
+        return _linear(_spread(rng, 1, 8192), _width(rng, 256, 4096), _width(rng, 256, 4096), E, k, rng.random() < 0.6, skew)
+    return _experts(_spread(rng, 1, 16384), _width(rng, 256, 4096), _width(rng, 128, 8192), E, k, rng.choice(["swiglu", "swiglu", "gelu"]), skew)
+
+
+def draw(rng):
+    most = {"gate": 2 ** 25, "norm": 2 ** 27, "norm8": 2 ** 27, "experts": 16384 * 2 * 3 * 4096 * 14336, "linear": 2 ** 40}
+    while True:
+        c = _draw_once(rng)
+        size = c["T"] * c["E"] * 2 if c["kind"] == "gate" else c["rows"] * c["d"] if "rows" in c else work(c)["flops"] // 2
+        if size <= most[c["kind"]] and ("rows" in c or c["kind"] == "gate" or _plain_bytes(c) <= 40e9):
+            return c
+
+
+def _hidden(c):
+    return 2 * c["d_expert"] if c["act"] == "swiglu" else c["d_expert"]
+
+
+def _plain_bytes(c):
+    """About what the plain form holds at once, were half of the rows one expert's."""
+    widths = c["d_model"] + (_hidden(c) + c["d_expert"] if c["kind"] == "experts" else c["d_out"])
+    weights = c["E"] * c["d_model"] * (_hidden(c) + c["d_expert"] if c["kind"] == "experts" else c["d_out"])
+    return 4 * (c["E"] * min(c["T"], max(64, c["T"] * c["k"] // 2)) * widths + 3 * weights)
+
+
+def work(c):
+    if c["kind"] == "gate":
+        n, Tk = c["T"] * c["E"], c["T"] * c["k"]
+        nbytes = 4 * n + 8 * Tk + (4 * c["E"] if c["bias"] else 0)
+        return {"bytes": nbytes + (4 * n + 4 * n + 8 * Tk if c["grad"] else 0), "flops": 10 * n * (2 if c["grad"] else 1)}
+    if c["kind"] in ("norm", "norm8"):
+        n, es = c["rows"] * c["d"], 4 if c["dtype"] == "f32" else 2
+        nbytes = n * es * (4 if c["residual"] else 2) + c["d"] * es
+        if c["kind"] == "norm8":                            # the 8-bit rows written, read, and written back as bf16
+            nbytes += 2 * (n + n // BLOCK) + 2 * n
+        if c["grad"]:                                       # dY, the stream and, where it goes on, its gradient in; dX out
+            nbytes += n * es * (4 if c["residual"] else 3) + 2 * c["d"] * es
+        return {"bytes": nbytes, "flops": n * (14 if c["grad"] else 5)}
+    Tk, used, d = c["T"] * c["k"], min(c["E"], c["T"] * c["k"]), c["d_model"]
+    if c["kind"] == "linear":
+        per, out = d * c["d_out"], c["d_out"] * (c["T"] if c["gates"] else Tk)
+    else:
+        per, out = d * (_hidden(c) + c["d_expert"]), c["T"] * d
+    stored = used * per + c["T"] * d
+    return {"bytes": stored + stored // BLOCK + 2 * out + 12 * Tk, "flops": 2 * Tk * per}
+
+
+# ----------------------------------------------------------------------------------------------------------- inputs
+def _normal(gen, *shape, dtype=torch.bfloat16, std=1.0):
+    return torch.empty(*shape, dtype=torch.float32, device="cuda").normal_(0.0, std, generator=gen).to(dtype)
+
+
+def _power(e):
+    """2^e in 32 bits, exactly, for whole e from -126 to 127."""
+    return ((e.int() + 127) << 23).view(torch.float32)
+
+
+def _packed(x):
+    """x [..., d] as e4m3 with one power of two for 32 elements: codes [..., d], and the exponents [..., d / 32], the smallest e from -126 on
+    with |x| 2^-e <= 448 = 1.75 * 2^8."""
+    x = x.float().unflatten(-1, (-1, BLOCK))
+    m, e = torch.frexp(x.abs().amax(-1))                    # amax = m 2^e, 0.5 <= m < 1
+    e = torch.where(m > 0, e - 9 + (m > 0.875).int(), torch.full_like(e, -126)).clamp(min=-126)
+    return (x * _power(-e)[..., None]).to(torch.float8_e4m3fn).flatten(-2), e
+
+
+def _unpacked(codes, e):
+    return (codes.float().unflatten(-1, (-1, BLOCK)) * _power(e)[..., None]).flatten(-2)
+
+
+def _gate_rule(c):
+    import paper_2403_08245_amd as smoe
+    return smoe.gate_rule(c["score"], groups=c["groups"], kept_groups=c["kept"], group_best=c["best"], renormalise=c["renormalise"], scale=c["scale"])
+
+
+def _own_rows(codes, e):
+    """The package's rows of 8 bits: the exponents of a row stand in whole groups of four bytes."""
+    import paper_2403_08245_amd as smoe
+    exps = torch.full((*e.shape[:-1], -(-e.shape[-1] // 4) * 4), 127, dtype=torch.uint8, device="cuda")
+    exps[..., :e.shape[-1]] = (e + 127).to(torch.uint8)
+    return smoe.Rows8(codes.view(torch.uint8), exps)
+
+
+def prepare(case, seed):
+    c = case
+    gen = torch.Generator(device="cuda").manual_seed(seed * 7919 + 13)
+    s = {"case": c}
+    if c["kind"] == "gate":
+        s["logits"] = _normal(gen, c["T"], c["E"], dtype=torch.float32)
+        s["bias"] = _normal(gen, c["E"], dtype=torch.float32, std=0.05) if c["bias"] else None
+        if c["grad"]:
+            s["dgates"] = _normal(gen, c["T"], c["k"], dtype=torch.float32)
+        if own:
+            s["rule"] = _gate_rule(c)
+        return s
+    if c["kind"] in ("norm", "norm8"):
+        rows, d, dt = c["rows"], c["d"], DTYPES[c["dtype"]]
+        s["X"] = _normal(gen, rows, d, dtype=dt)
+        s["R"] = _normal(gen, rows, d, dtype=dt, std=4.0) if c["residual"] else None
+        s["weight"] = (1.0 + _normal(gen, d, dtype=torch.float32, std=0.1)).to(dt)
+        if c["grad"]:
+            s["dY"] = _normal(gen, rows, d, dtype=dt)
+            s["dS"] = _normal(gen, rows, d, dtype=dt) if c["residual"] else None
+        return s
+    T, d, E, k = c["T"], c["d_model"], c["E"], c["k"]
+    share = 1.0 / torch.arange(1, E + 1, dtype=torch.float32, device="cuda") ** c["skew"]
+    gumbel = -torch.log(-torch.log(torch.rand(T, E, generator=gen, device="cuda").clamp(1e-6, 1 - 1e-6)))
+    top, idx = torch.topk(gumbel + torch.log(share), k, dim=1)
+    s["gates"] = torch.softmax(top, 1)
+    expert, order = torch.sort(idx.flatten(), stable=True)   # slots by expert
+    counts = torch.bincount(expert, minlength=E)
+    offsets = torch.cat([counts.new_zeros(1), counts.cumsum(0)])
+    s["idx"], s["most"] = idx, int(counts.max())
+    at = torch.arange(T * k, device="cuda") - offsets[expert]
+    s["slots"] = torch.full((E, s["most"]), T * k, device="cuda")          # each expert's slots, padded with one that does not exist
+    s["slots"][expert, at] = order
+    X = _normal(gen, T, d) * (0.2 + 4.0 * torch.rand(d, generator=gen, device="cuda")).bfloat16()      # features of unequal size
+    s["X"], s["X_e"] = _packed(X)
+    if own:
+        import paper_2403_08245_amd as smoe
+        s["r"] = smoe.Routing(expert.int(), order.int(), offsets.int(), T * k, E)
+        s["rows"] = _own_rows(s["X"], s["X_e"])
+    shapes = {"W": (d, c["d_out"])} if c["kind"] == "linear" else {"W1": (d, _hidden(c)), "W2": (c["d_expert"], d)}
+    for name, (d_in, d_out) in shapes.items():
+        W = torch.empty(E, d_in, d_out, dtype=torch.bfloat16, device="cuda").normal_(0.0, d_in ** -0.5, generator=gen)
+        if own:
+            s[name] = smoe.weights8(W)
+        else:                                                # blocks lie along the contraction
+            parts = [_packed(w.t()) for w in W]
+            s[name], s[name + "_e"] = torch.stack([p[0].t().contiguous() for p in parts]), torch.stack([p[1] for p in parts])
+    return s
+
+
+# ------------------------------------------------------------------------------------------------------- plain form
+def _scores(c, x):
+    return torch.softmax(x, 1) if c["score"] == "softmax" else torch.sigmoid(x)
+
+
+def _chosen(c, s):
+    """The experts of each token, by scores in 64 bits: those next to a border would go either way in 32."""
+    x = s["logits"].double()
+    rank = _scores(c, x) + (0 if s["bias"] is None else s["bias"].double())
+    if c["groups"] > 1:
+        of_group = rank.unflatten(1, (c["groups"], -1)).sort(2, descending=True)[0][..., :c["best"]].sum(2)
+        kept = torch.sort(of_group, dim=1, descending=True, stable=True)[1][:, :c["kept"]]
+        out = torch.ones_like(of_group, dtype=torch.bool).scatter_(1, kept, False)
+        rank = rank.masked_fill(out.repeat_interleave(c["E"] // c["groups"], 1), -math.inf)
+    return torch.sort(rank, dim=1, descending=True, stable=True)[1][:, :c["k"]]
+
+
+def _plain_gate(c, s):
+    x, idx = s["logits"], _chosen(c, s)
+    score = _scores(c, x)
+    kept = score.gather(1, idx)
+    total = kept.sum(1, keepdim=True) if c["renormalise"] else torch.ones_like(kept[:, :1])
+    w = c["scale"] * kept / total
+    out = [idx.int(), w]
+    if c["grad"]:
+        dw = s["dgates"] * c["scale"]
+        ds = (dw - (dw * kept).sum(1, keepdim=True) / total) / total if c["renormalise"] else dw
+        full = torch.zeros_like(x).scatter_(1, idx, ds)
+        out.append(score * (full - (full * score).sum(1, keepdim=True)) if c["score"] == "softmax" else full * score * (1 - score))
+    return out
+
+
+def _plain_norm(c, s):
+    x, w, dt = s["X"].float(), s["weight"].float(), s["X"].dtype
+    if c["residual"]:
+        x = x + s["R"].float()
+    rstd = torch.rsqrt((x * x).mean(1, keepdim=True) + 1e-6)
+    unit = x * rstd
+    y = unit * w
+    out = [x.to(dt)] if c["residual"] else []
+    out.append(y.to(dt))
+    if c["kind"] == "norm8":
+        out.append(_unpacked(*_packed(y)).to(torch.bfloat16))
+    if c["grad"]:
+        dy = s["dY"].float()
+        g = dy * w
+        dx = rstd * (g - unit * (g * unit).mean(1, keepdim=True))
+        out += [(dx + s["dS"].float() if c["residual"] else dx).to(dt), (dy * unit).sum(0, dtype=torch.float64).to(dt)]
+    return out
+
+
+def _plain_experts(c, s):
+    T, k, E = c["T"], c["k"], c["E"]
+    weight = lambda name: _unpacked(s[name].transpose(1, 2), s[name + "_e"]).transpose(1, 2).contiguous()
+    X = torch.cat([_unpacked(s["X"], s["X_e"]), torch.zeros(1, c["d_model"], device="cuda")])
+    x = X[s["slots"] // k]                                   # [E, most, d]; the slot that does not exist is a row of zeros
+    if c["kind"] == "linear":
+        y = torch.matmul(x, weight("W"))
+    else:
+        h = torch.matmul(x, weight("W1"))
+        if c["act"] == "swiglu":
+            gate, up = h.chunk(2, -1)
+            h = gate / (1 + torch.exp(-gate)) * up
+        else:
+            h = 0.5 * h * (1 + torch.erf(h * 0.5 ** 0.5))
+        y = torch.matmul(_unpacked(*_packed(h)), weight("W2"))
+    flat = torch.empty(T * k + 1, y.shape[2], device="cuda")
+    flat[s["slots"].flatten()] = y.flatten(0, 1)
+    flat = flat[:T * k]
+    if c.get("gates", True):
+        flat = (flat.view(T, k, -1) * s["gates"][..., None]).sum(1)
+    return flat.to(torch.bfloat16)
+
+
+def run(state):
+    s, c = state, state["case"]
+    if not own:
+        return _plain_gate(c, s) if c["kind"] == "gate" else _plain_norm(c, s) if "rows" in c else _plain_experts(c, s)
+    import paper_2403_08245_amd as smoe
+    if c["kind"] == "gate":
+        idx, gates = smoe.score_gate(s["logits"], c["k"], s["rule"], s["bias"])
+        return [idx, gates] + ([smoe.score_gate_bwd(s["logits"], idx, s["dgates"], s["rule"])] if c["grad"] else [])
+    if "rows" in c:
+        n = smoe.add_norm_fwd(s["X"], s["weight"], R=s["R"], eps=1e-6, packed=c["kind"] == "norm8")
+        out = [n.S, n.Y] if c["residual"] else [n.Y]
+        if c["kind"] == "norm8":
+            out.append(smoe.rows8_unpack(n.Y8))
+        if c["grad"]:
+            out += smoe.add_norm_bwd(s["dY"], n.S, s["weight"], n.rstd, dS=s["dS"])
+        return out
+    if c["kind"] == "linear":
+        return smoe.plinear8_fwd(s["rows"], s["W"], s["r"], c["k"], s["gates"] if c["gates"] else None)[0]
+    return smoe.mlp8_fwd(s["rows"], s["W1"], s["W2"], s["r"], c["k"], s["gates"], smoe.ACT_SWIGLU if c["act"] == "swiglu" else smoe.ACT_GELU)
+
+
+# ------------------------------------------------------------------------------------------------------- in 64 bits
+def _two(e):
+    """2^e for whole e, exactly: the exponent's bits."""
+    return ((e.long() + 1023) << 52).view(torch.float64)
+
+
+def _rounded64(x):
+    """The values that rows of x stand for once they are packed: the nearest e4m3 numbers, ties to even, times the block's power of two."""
+    x = x.reshape(*x.shape[:-1], -1, BLOCK)
+    amax = x.abs().amax(-1, keepdim=True)
+    e = torch.ceil(torch.log2(torch.where(amax > 0, amax, torch.ones_like(amax)) / 448.0) - 1e-12).clamp(min=-126)
+    y = x * _two(-e)
+    step = _two(torch.frexp(y.abs().clamp(min=2.0 ** -6))[1] - 4)                        # three bits behind the leading one
+    return torch.where(amax > 0, torch.round(y / step) * step * _two(e), torch.zeros_like(x)).flatten(-2)
+
+
+def _gate64(c, s):
+    x, k = s["logits"].double(), c["k"]
+    p = torch.exp(x - torch.logsumexp(x, 1, keepdim=True)) if c["score"] == "softmax" else 1 / (1 + torch.exp(-x))
+    rank = p if s["bias"] is None else p + s["bias"].double()
+    if c["groups"] > 1:
+        per = c["E"] // c["groups"]
+        group = torch.topk(rank.view(-1, c["groups"], per), min(c["best"], per), dim=2)[0].sum(2)
+        kept = torch.argsort(-group, dim=1, stable=True)[:, :c["kept"]]
+        allowed = (kept[:, None, :] == (torch.arange(c["E"], device="cuda") // per)[None, :, None]).any(2)
+        rank = torch.where(allowed, rank, torch.full_like(rank, -math.inf))
+    idx = torch.argsort(-rank, dim=1, stable=True)[:, :k]
+    q = p.gather(1, idx)
+    w = q / q.sum(1, keepdim=True) if c["renormalise"] else q
+    out = [idx.int(), w * c["scale"]]
+    if not c["grad"]:
+        return out
+    dw = s["dgates"].double() * c["scale"]
+    # d w / d log p, then d log p / d x
+    dl = w * (dw - (w * dw).sum(1, keepdim=True)) if c["renormalise"] else w * dw
+    dx = torch.zeros_like(x).scatter_add_(1, idx, dl if c["score"] == "softmax" else dl * (1 - q))
+    return out + [dx - p * dl.sum(1, keepdim=True) if c["score"] == "softmax" else dx]
+
+
+def _norm64(c, s):
+    x = s["X"].double() + (s["R"].double() if c["residual"] else 0)
+    w = s["weight"].double()
+    r = (x.square().mean(1, keepdim=True) + 1e-6).sqrt()
+    out = ([x] if c["residual"] else []) + [x / r * w]
+    if c["kind"] == "norm8":
+        out.append(_rounded64(out[-1]))
+    if c["grad"]:
+        dy = s["dY"].double()
+        dx = dy * w / r - x * ((dy * w * x).sum(1, keepdim=True) / (c["d"] * r ** 3))
+        out += [dx + s["dS"].double() if c["residual"] else dx, (dy * x / r).sum(0)]
+    return out
+
+
+def _experts64(c, s):
+    T, k, d = c["T"], c["k"], c["d_model"]
+    whole = lambda codes, e: (codes.double().view(*codes.shape[:-1], -1, BLOCK) * _two(e)[..., None]).flatten(-2)
+    X, flat = whole(s["X"], s["X_e"]), None
+    for e in range(c["E"]):
+        slot = (s["idx"].flatten() == e).nonzero()[:, 0]
+        if slot.numel() == 0:
+            continue
+        W = {n: whole(s[n][e].t(), s[n + "_e"][e]).t() for n in (("W",) if c["kind"] == "linear" else ("W1", "W2"))}
+        y = X[slot // k] @ W["W" if c["kind"] == "linear" else "W1"]
+        if c["kind"] == "experts":
+            if c["act"] == "swiglu":
+                y = y[:, :c["d_expert"]] * torch.sigmoid(y[:, :c["d_expert"]]) * y[:, c["d_expert"]:]
+            else:
+                y = y * 0.5 * torch.special.erfc(-y / math.sqrt(2))
+            y = _rounded64(y) @ W["W2"]
+        if flat is None:
+            flat = torch.zeros(T * k, y.shape[1], dtype=torch.float64, device="cuda")
+        flat[slot] = y
+    if c.get("gates", True):
+        flat = (flat.view(T, k, -1) * s["gates"].double()[..., None]).sum(1)
+    return flat
+
+
+def exact(case, seed):
+    s = prepare(case, seed)
+    return _gate64(case, s) if case["kind"] == "gate" else _norm64(case, s) if "rows" in case else _experts64(case, s)
