@@ -178,11 +178,13 @@ def _gate_rule(c):
 
 
 def _own_rows(codes, e):
-    """The package's rows of 8 bits: the exponents of a row stand in whole groups of four bytes."""
+    """The package's rows of 8 bits: as wide as whole 128s, padded as with zeros."""
     import paper_2403_08245_amd as smoe
-    exps = torch.full((*e.shape[:-1], -(-e.shape[-1] // 4) * 4), 127, dtype=torch.uint8, device="cuda")
-    exps[..., :e.shape[-1]] = (e + 127).to(torch.uint8)
-    return smoe.Rows8(codes.view(torch.uint8), exps)
+    d = codes.shape[-1]
+    pad = -d % 128
+    values = torch.nn.functional.pad(codes.view(torch.uint8), (0, pad))
+    exps = torch.nn.functional.pad((e + 127).to(torch.uint8), (0, pad // BLOCK), value=1)
+    return smoe.Rows8(values.contiguous(), exps.contiguous(), d)
 
 
 def prepare(case, seed):
@@ -228,7 +230,7 @@ def prepare(case, seed):
     for name, (d_in, d_out) in shapes.items():
         W = torch.empty(E, d_in, d_out, dtype=torch.bfloat16, device="cuda").normal_(0.0, d_in ** -0.5, generator=gen)
         if own:
-            s[name] = smoe.weights8(W)
+            s[name] = smoe.weights8(W, halves=2 if name == "W1" and c["act"] == "swiglu" else 1)
         else:                                                # blocks lie along the contraction
             parts = [_packed(w.t()) for w in W]
             s[name], s[name + "_e"] = torch.stack([p[0].t().contiguous() for p in parts]), torch.stack([p[1] for p in parts])
