@@ -7,3 +7,4 @@ slow, plainly-correct definition to compare the HIP kernels with.
 from .smoe_oracle import *  # noqa: F401,F403
 from .momha_oracle import *  # noqa: F401,F403
 from .cache_oracle import *  # noqa: F401,F403
+from .block_oracle import *  # noqa: F401,F403

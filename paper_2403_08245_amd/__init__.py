@@ -2,7 +2,8 @@
 
 Argument marshalling only: every function here checks tensor dtypes/contiguity, allocates
 outputs and scratch with torch, and calls the C entry point of the same name
-(smoe_<name>, declared in include/smoe.h, or include/smoe_cache.h for positions and serving) on torch's current HIP stream.  There is no
+(smoe_<name>, declared in include/smoe.h, in include/smoe_cache.h for positions and serving, or in include/smoe_block.h for the gate by
+scores, the norm and the products in 8 bits) on torch's current HIP stream.  There is no
 Python or PyTorch fallback: if libsmoe.so is missing, importing this package fails.
 """
 from __future__ import annotations
@@ -32,6 +33,11 @@ EXPORTS = [
 CACHE_EXPORTS = [
     "smoe_rotary_frequencies", "smoe_rotary_fwd", "smoe_rotary_bwd", "smoe_cache_append", "smoe_cache_read",
     "smoe_cached_attention_workspace_bytes", "smoe_cached_attention_fwd", "smoe_momha_decode_workspace_bytes", "smoe_momha_decode",
+]
+
+BLOCK_EXPORTS = [
+    "smoe_score_gate", "smoe_score_gate_bwd", "smoe_rows8_pack", "smoe_rows8_unpack", "smoe_weights8_bytes", "smoe_weights8_pack", "smoe_add_norm_fwd",
+    "smoe_add_norm_bwd_workspace_bytes", "smoe_add_norm_bwd", "smoe_plinear8_fwd", "smoe_mlp8_fwd_workspace_bytes", "smoe_mlp8_fwd",
 ]
 
 
@@ -123,6 +129,37 @@ lib.smoe_cached_attention_fwd.argtypes = [_vp, _vp, _i, _vp, _i, _i, _cp, _pp, _
 lib.smoe_momha_decode_workspace_bytes.argtypes = [_i] * 6
 lib.smoe_momha_decode_workspace_bytes.restype = _sz
 lib.smoe_momha_decode.argtypes = [_vp, _vp, _i, _vp, _i, _i, _vp, _vp, _vp, _vp, _rp, _i, _vp, _cp, _pp, _op, _vp, _vp, _sz]
+
+
+class smoe_gate_rule(ctypes.Structure):
+    _fields_ = [("score", ctypes.c_int32), ("groups", ctypes.c_int32), ("kept_groups", ctypes.c_int32), ("group_best", ctypes.c_int32),
+                ("renormalise", ctypes.c_int32), ("scale", ctypes.c_float)]
+
+
+class smoe_rows8(ctypes.Structure):
+    _fields_ = [("values", _vp), ("exps", _vp)]
+
+
+class smoe_weights8(ctypes.Structure):
+    _fields_ = [("values", _vp), ("exps", _vp), ("E", ctypes.c_int32), ("d_in", ctypes.c_int32), ("d_out", ctypes.c_int32), ("halves", ctypes.c_int32)]
+
+
+_gp, _r8, _w8 = ctypes.POINTER(smoe_gate_rule), ctypes.POINTER(smoe_rows8), ctypes.POINTER(smoe_weights8)
+lib.smoe_score_gate.argtypes = [_vp, _vp, _vp, _vp, _i, _i, _i, _gp, _vp, _vp]
+lib.smoe_score_gate_bwd.argtypes = [_vp, _vp, _vp, _vp, _vp, _i, _i, _i, _gp, _vp]
+lib.smoe_rows8_pack.argtypes = [_vp, _vp, _i, _vp, _i, _i, _r8]
+lib.smoe_rows8_unpack.argtypes = [_vp, _vp, _i, _r8, _i, _i, _vp]
+lib.smoe_weights8_bytes.argtypes = [_i] * 4
+lib.smoe_weights8_bytes.restype = _sz
+lib.smoe_weights8_pack.argtypes = [_vp, _vp, _i, _vp, _w8]
+lib.smoe_add_norm_fwd.argtypes = [_vp, _vp, _i, _vp, _vp, _vp, _i, _i, ctypes.c_float, _vp, _vp, _r8, _vp]
+lib.smoe_add_norm_bwd_workspace_bytes.argtypes = [_i] * 3
+lib.smoe_add_norm_bwd_workspace_bytes.restype = _sz
+lib.smoe_add_norm_bwd.argtypes = [_vp, _vp, _i, _vp, _vp, _vp, _vp, _vp, _i, _i, _vp, _vp, _vp, _sz]
+lib.smoe_plinear8_fwd.argtypes = [_vp, _vp, _r8, _i, _i, _w8, _i, _rp, _i, _vp, _i, _i, _i, _vp, _vp]
+lib.smoe_mlp8_fwd_workspace_bytes.argtypes = [_i] * 5
+lib.smoe_mlp8_fwd_workspace_bytes.restype = _sz
+lib.smoe_mlp8_fwd.argtypes = [_vp, _vp, _i, _r8, _i, _i, _i, _w8, _w8, _rp, _i, _vp, _vp, _vp, _sz]
 
 
 class SmoeError(RuntimeError):
@@ -748,3 +785,289 @@ def momha_decode(X, W_K, W_V, W_Q, W_O, r: Routing, k: int, gates, cache: KVCach
     _check(lib.smoe_momha_decode(c, stream, BF16, _p(X), N, d_model, _p(W_K), _p(W_V), _p(W_Q), _p(W_O), ctypes.byref(rc), k, _p(gates),
                                  cache._c, where, None if rotary is None else rotary._c, _p(O), _p(ws), ws.numel()), "smoe_momha_decode")
     return O
+
+
+# ---- the block around the experts (include/smoe_block.h) ------------------------------------------------------------------
+SCORES = {"softmax": 0, "sigmoid": 1}
+
+
+class GateRule(_Fixed):
+    """How a router's scores become a choice and weights (attributes fixed; see smoe_gate_rule)."""
+
+    def __init__(self, score: str, groups: int, kept_groups: int, group_best: int, renormalise: bool, scale: float):
+        if score not in SCORES:
+            raise ValueError(f"score {score!r}")
+        self.__dict__.update(score=score, groups=groups, kept_groups=kept_groups, group_best=group_best, renormalise=renormalise, scale=scale,
+                             _c=ctypes.byref(smoe_gate_rule(SCORES[score], groups, kept_groups, group_best, int(renormalise), scale)))
+
+
+def gate_rule(score: str = "softmax", groups: int = 1, kept_groups: int = 1, group_best: int = 1, renormalise: bool = True, scale: float = 1.0) -> GateRule:
+    """Scores "softmax" or "sigmoid"; of `groups` groups of experts the kept_groups whose group_best largest ranks sum to most; weights divided by
+    their sum with `renormalise`, times `scale`."""
+    return GateRule(score, groups, kept_groups, group_best, renormalise, scale)
+
+
+def score_gate(logits: torch.Tensor, k: int, rule: GateRule, bias: torch.Tensor | None = None):
+    """logits [T, E] fp32, bias [E] fp32 (moves the choice only) -> expert_idxs [T, k] int32, gates [T, k] fp32."""
+    dev = _device(logits)
+    _here(dev, torch.float32, logits)
+    if logits.dim() != 2:
+        raise ValueError("logits must be [T, E]")
+    T, E = logits.shape
+    if (T | E) > INT_MAX or not 0 < k <= E:
+        raise ValueError("more tokens or experts than 32 bits count, or k outside 1 .. E")
+    if bias is not None:
+        _here(dev, torch.float32, bias)
+        if bias.numel() != E:
+            raise ValueError("bias must be [E]")
+    idx, gates = _new(T, k, dtype=torch.int32, device=logits.device), _new(T, k, dtype=torch.float32, device=logits.device)
+    c, stream = _where(dev)
+    _check(lib.smoe_score_gate(c, stream, logits.data_ptr(), _p(bias), T, E, k, rule._c, idx.data_ptr(), gates.data_ptr()), "smoe_score_gate")
+    return idx, gates
+
+
+def score_gate_bwd(logits: torch.Tensor, expert_idxs: torch.Tensor, dgates: torch.Tensor, rule: GateRule) -> torch.Tensor:
+    """dlogits [T, E] from the gradient of score_gate's gates."""
+    dev = _device(logits)
+    _here(dev, torch.float32, logits, dgates)
+    _here(dev, torch.int32, expert_idxs)
+    if logits.dim() != 2 or expert_idxs.dim() != 2 or expert_idxs.shape[0] != logits.shape[0] or dgates.shape != expert_idxs.shape:
+        raise ValueError("logits must be [T, E], expert_idxs and dgates [T, k]")
+    (T, E), k = logits.shape, expert_idxs.shape[1]
+    if (T | E | k) > INT_MAX:
+        raise ValueError("more tokens or experts than 32 bits count")
+    dlogits = _new(T, E, dtype=torch.float32, device=logits.device)
+    c, stream = _where(dev)
+    _check(lib.smoe_score_gate_bwd(c, stream, logits.data_ptr(), expert_idxs.data_ptr(), dgates.data_ptr(), T, E, k, rule._c, dlogits.data_ptr()),
+           "smoe_score_gate_bwd")
+    return dlogits
+
+
+class Rows8(_Fixed):
+    """Rows of d elements in 8 bits: values [..., P] and exps [..., P / 32] uint8, P = 128 * ceil(d / 128) (see smoe_rows8).  The tensors stay
+    the caller's; which they are is fixed."""
+
+    def __init__(self, values: torch.Tensor, exps: torch.Tensor, d: int):
+        for t in (values, exps):
+            _chk(t, torch.uint8)
+        P = values.shape[-1]
+        if not 0 < d <= P or P != -(-d // 128) * 128 or exps.shape != (*values.shape[:-1], P // 32) or exps.device != values.device:
+            raise ValueError("rows in 8 bits must be values [..., 128 * ceil(d / 128)] and exps [..., 4 * ceil(d / 128)] on one device")
+        self.__dict__.update(values=values, exps=exps, d=d, rows=values.numel() // P, shape=(*values.shape[:-1], d), device=values.get_device(),
+                             _c=ctypes.byref(smoe_rows8(_p(values), _p(exps))))
+
+
+def _new_rows8(shape, device) -> Rows8:
+    P = -(-shape[-1] // 128) * 128
+    return Rows8(_new(*shape[:-1], P, dtype=torch.uint8, device=device), _new(*shape[:-1], P // 32, dtype=torch.uint8, device=device), shape[-1])
+
+
+def _rows_on(dev: int, *rows: Rows8):
+    for r in rows:
+        if r.device != dev:
+            raise ValueError(f"rows on device {r.device}, but the current device is {dev}")
+        if r.rows > INT_MAX:
+            raise ValueError("more rows than 32 bits count")
+
+
+def _row_sizes(X: torch.Tensor):
+    """Rows and width of X [..., d]."""
+    d = X.shape[-1] if X.dim() else 0
+    rows = X.numel() // d if d else 0
+    if X.dim() < 1 or d < 1 or (rows | d) > INT_MAX:
+        raise ValueError("rows must be [..., d], as many as 32 bits count")
+    return rows, d
+
+
+def rows8_pack(X: torch.Tensor, out: Rows8 | None = None) -> Rows8:
+    """X [..., d] (F32 or BF16) in 8 bits."""
+    dev = _device(X)
+    _here(dev, X.dtype, X)
+    rows, d = _row_sizes(X)
+    if out is None:
+        out = _new_rows8(X.shape, X.device)
+    _rows_on(dev, out)
+    if out.rows != rows or out.d != d:
+        raise ValueError("out must be rows like X")
+    c, stream = _where(dev)
+    _check(lib.smoe_rows8_pack(c, stream, _dt(X), X.data_ptr(), rows, d, out._c), "smoe_rows8_pack")
+    return out
+
+
+def rows8_unpack(rows: Rows8, dtype=torch.bfloat16) -> torch.Tensor:
+    """The values that rows in 8 bits stand for, [..., d]."""
+    dev = _device(rows.values)
+    _rows_on(dev, rows)
+    X = _new(*rows.shape, dtype=dtype, device=rows.values.device)
+    c, stream = _where(dev)
+    _check(lib.smoe_rows8_unpack(c, stream, _dt(X), rows._c, rows.rows, rows.d, X.data_ptr()), "smoe_rows8_unpack")
+    return X
+
+
+class Weights8(_Fixed):
+    """Weights of E experts [d_in, d_out] in 8 bits, as the products read them (made by weights8; see smoe_weights8)."""
+
+    def __init__(self, values: torch.Tensor, exps: torch.Tensor, E: int, d_in: int, d_out: int, halves: int):
+        for t in (values, exps):
+            _chk(t, torch.uint8)
+        nb = lib.smoe_weights8_bytes(E, d_in, d_out, halves)
+        if not nb or values.numel() != nb or exps.numel() * 32 != nb or exps.device != values.device:
+            raise ValueError("weights in 8 bits must be values of smoe_weights8_bytes and a 32nd as many exps, on one device")
+        self.__dict__.update(values=values, exps=exps, E=E, d_in=d_in, d_out=d_out, halves=halves, device=values.get_device(),
+                             _c=ctypes.byref(smoe_weights8(_p(values), _p(exps), E, d_in, d_out, halves)))
+
+
+def weights8(W: torch.Tensor, halves: int = 1) -> Weights8:
+    """W [E, d_in, d_out] (F32 or BF16) in 8 bits, laid out for the products; halves = 2 where the columns are SwiGLU's [gate | up].  Made once."""
+    dev = _device(W)
+    _here(dev, W.dtype, W)
+    if W.dim() != 3 or max(W.shape) > INT_MAX:
+        raise ValueError("weights must be [E, d_in, d_out]")
+    E, d_in, d_out = W.shape
+    nb = lib.smoe_weights8_bytes(E, d_in, d_out, halves)
+    if not nb:
+        raise ValueError(f"no layout for {E} experts of {d_in} x {d_out} in {halves} halves")
+    out = Weights8(_new(nb, dtype=torch.uint8, device=W.device), _new(nb // 32, dtype=torch.uint8, device=W.device), E, d_in, d_out, halves)
+    c, stream = _where(dev)
+    _check(lib.smoe_weights8_pack(c, stream, _dt(W), W.data_ptr(), out._c), "smoe_weights8_pack")
+    return out
+
+
+@dataclass
+class Norm:
+    """What add_norm_fwd leaves: the stream S that goes on (X itself where nothing was added), Y in its dtype, Y8 in 8 bits, rstd [rows] for the
+    backward pass; None for what was not asked for."""
+    S: torch.Tensor
+    Y: torch.Tensor | None
+    Y8: Rows8 | None
+    rstd: torch.Tensor
+
+
+def add_norm_fwd(X: torch.Tensor, weight: torch.Tensor, R: torch.Tensor | None = None, eps: float = 1e-6, plain: bool = True, packed: bool = False,
+                 out: Norm | None = None) -> Norm:
+    """The root-mean-square norm of X + R [..., d] (F32 or BF16, weight [d] in the same): Y with `plain`, Y8 with `packed`.  `out` reuses the
+    tensors of an earlier call; its S, where R is given, may be X or R itself."""
+    dev, dtype = _device(X), X.dtype
+    _here(dev, dtype, X, weight)
+    rows, d = _row_sizes(X)
+    if weight.numel() != d:
+        raise ValueError("weight must be [d]")
+    if not plain and not packed:
+        raise ValueError("ask for plain or packed rows, or both")
+    if R is not None:
+        _here(dev, dtype, R)
+        if R.shape != X.shape:
+            raise ValueError("R must be like X")
+    if out is None:
+        out = Norm(X if R is None else _like(X), _like(X) if plain else None, _new_rows8(X.shape, X.device) if packed else None,
+                   _new(rows, dtype=torch.float32, device=X.device))
+    else:
+        _here(dev, dtype, out.S)
+        _here(dev, torch.float32, out.rstd)
+        if out.S.shape != X.shape or out.rstd.numel() != rows or (out.Y is not None) != plain or (out.Y8 is not None) != packed:
+            raise ValueError("out must be what such a call leaves")
+        if plain:
+            _here(dev, dtype, out.Y)
+            if out.Y.shape != X.shape:
+                raise ValueError("out must be what such a call leaves")
+        if packed:
+            _rows_on(dev, out.Y8)
+            if out.Y8.rows != rows or out.Y8.d != d:
+                raise ValueError("out must be what such a call leaves")
+        if R is None and out.S is not X:
+            out = Norm(X, out.Y, out.Y8, out.rstd)
+    c, stream = _where(dev)
+    _check(lib.smoe_add_norm_fwd(c, stream, _dt(X), X.data_ptr(), _p(R), weight.data_ptr(), rows, d, eps, None if R is None else out.S.data_ptr(), _p(out.Y),
+                                 out.Y8._c if packed else None, out.rstd.data_ptr()), "smoe_add_norm_fwd")
+    return out
+
+
+def add_norm_bwd(dY: torch.Tensor, S: torch.Tensor, weight: torch.Tensor, rstd: torch.Tensor, dS: torch.Tensor | None = None, out=None, ws=None):
+    """(dX, dweight) of add_norm_fwd from the gradients of Y and, where the stream goes on, of S; that of R is dX.  out = (dX, dweight), whose dX
+    may be dY, S or dS itself."""
+    dev, dtype = _device(dY), dY.dtype
+    _here(dev, dtype, dY, S, weight)
+    _here(dev, torch.float32, rstd)
+    rows, d = _row_sizes(dY)
+    if S.shape != dY.shape or weight.numel() != d or rstd.numel() != rows:
+        raise ValueError("dY and S must be [..., d], weight [d] and rstd one for each row")
+    if dS is not None:
+        _here(dev, dtype, dS)
+        if dS.shape != dY.shape:
+            raise ValueError("dS must be like dY")
+    if out is None:
+        dX, dweight = _like(dY), _like(weight)
+    else:
+        dX, dweight = out
+        _here(dev, dtype, dX, dweight)
+        if dX.shape != dY.shape or dweight.numel() != d:
+            raise ValueError("out must be a tensor like dY and one like weight")
+    if ws is None:
+        ws = _ws(lib.smoe_add_norm_bwd_workspace_bytes(_dt(dY), rows, d), dY.device)
+    else:
+        _here(dev, torch.uint8, ws)
+    c, stream = _where(dev)
+    _check(lib.smoe_add_norm_bwd(c, stream, _dt(dY), dY.data_ptr(), _p(dS), S.data_ptr(), weight.data_ptr(), rstd.data_ptr(), rows, d, dX.data_ptr(),
+                                 dweight.data_ptr(), ws.data_ptr(), ws.numel()), "smoe_add_norm_bwd")
+    return dX, dweight
+
+
+def _experts8(dev: int, r: Routing, *weights: Weights8):
+    _here(dev, torch.int32, r.sorted_expert_idxs, r.sorted_scattered_idxs, r.expert_offsets)
+    for w in weights:
+        if w.device != dev:
+            raise ValueError(f"weights on device {w.device}, but the current device is {dev}")
+        if w.E != r.E:
+            raise ValueError("weights and routing must be of as many experts")
+    if r.sorted_scattered_idxs.numel() < r.Tk or r.expert_offsets.numel() < r.E + 1:
+        raise ValueError("routing arrays are too short")
+
+
+def plinear8_fwd(X: Rows8, W: Weights8, r: Routing, k: int, gates=None, grouped_in=False, grouped_out=False):
+    """Alg. 1 on rows and weights in 8 bits, bf16 out.  Returns (Y, Yhat); Y is Yhat when no gates are given."""
+    dev = _device(X.values)
+    _rows_on(dev, X)
+    _experts8(dev, r, W)
+    if X.d != W.d_in:
+        raise ValueError("rows and weights differ in d_in")
+    Y, gk = None, 0
+    Yhat = _new(r.Tk, W.d_out, dtype=torch.bfloat16, device=X.values.device)
+    if gates is not None:
+        _here(dev, torch.float32, gates)
+        gk = gates.shape[-1]
+        if gates.numel() != r.Tk:
+            raise ValueError("gates must hold one entry for each routed slot")
+        Y = _new(r.Tk // gk if gk else 0, W.d_out, dtype=torch.bfloat16, device=X.values.device)
+    rc = r.c()
+    c, stream = _where(dev)
+    _check(lib.smoe_plinear8_fwd(c, stream, X._c, X.rows, X.d, W._c, W.d_out, ctypes.byref(rc), k, _p(gates), gk, int(grouped_in), int(grouped_out),
+                                 Yhat.data_ptr(), _p(Y)), "smoe_plinear8_fwd")
+    return (Yhat if Y is None else Y), Yhat
+
+
+def mlp8_fwd(X: Rows8, W1: Weights8, W2: Weights8, r: Routing, k: int, gates, act: int, out=None, ws=None) -> torch.Tensor:
+    """Alg. 3's forward pass on rows and weights in 8 bits (W1 of two halves for SwiGLU).  Returns Y [..., d_model] bf16."""
+    dev = _device(X.values)
+    _rows_on(dev, X)
+    _experts8(dev, r, W1, W2)
+    _here(dev, torch.float32, gates)
+    T, d_model, d_expert = X.rows, X.d, W2.d_in
+    if W1.d_in != d_model or W2.d_out != d_model or W1.d_out != hidden_width(act, d_expert) or W1.halves != hidden_width(act, 1) or W2.halves != 1:
+        raise ValueError("weights do not fit the rows, one another or the activation")
+    if r.Tk != T * k or gates.numel() != T * k:
+        raise ValueError("gates and routing must hold k slots for each row")
+    if out is None:
+        out = _new(*X.shape, dtype=torch.bfloat16, device=X.values.device)
+    else:
+        _here(dev, torch.bfloat16, out)
+        if out.numel() != T * d_model or out.shape[-1] != d_model:
+            raise ValueError("out must be [..., d_model] like the rows")
+    if ws is None:
+        ws = _ws(lib.smoe_mlp8_fwd_workspace_bytes(act, T, k, d_model, d_expert), X.values.device)
+    else:
+        _here(dev, torch.uint8, ws)
+    rc = r.c()
+    c, stream = _where(dev)
+    _check(lib.smoe_mlp8_fwd(c, stream, act, X._c, T, d_model, d_expert, W1._c, W2._c, ctypes.byref(rc), k, gates.data_ptr(), out.data_ptr(), ws.data_ptr(),
+                             ws.numel()), "smoe_mlp8_fwd")
+    return out

@@ -1,0 +1,276 @@
+// The root-mean-square norm of the residual stream with the addition in front of it, its gradient, and its output in 8 bits.
+// Bound: HBM, each tensor read or written once; a row stays in registers between its sum and its output.
+#include "block.h"
+#include <type_traits>
+
+namespace {
+
+// V elements of a row as they are loaded and stored
+template <typename T, int V> struct Pack {
+  float v[V];
+  __device__ __forceinline__ void load(const T *p) {
+    if constexpr (V == 1) {
+      v[0] = to_f32<T>(*p);
+    } else {
+      constexpr int PER = 16 / sizeof(T);
+      typedef T vec __attribute__((ext_vector_type(PER)));
+#pragma unroll
+      for (int q = 0; q < V / PER; ++q) {
+        const vec x = reinterpret_cast<const vec *>(p)[q];
+#pragma unroll
+        for (int i = 0; i < PER; ++i) v[q * PER + i] = to_f32<T>(x[i]);
+      }
+    }
+  }
+  __device__ __forceinline__ void store(T *p) const {
+    if constexpr (V == 1) {
+      *p = from_f32<T>(v[0]);
+    } else {
+      constexpr int PER = 16 / sizeof(T);
+      typedef T vec __attribute__((ext_vector_type(PER)));
+#pragma unroll
+      for (int q = 0; q < V / PER; ++q) {
+        vec x;
+#pragma unroll
+        for (int i = 0; i < PER; ++i) x[i] = from_f32<T>(v[q * PER + i]);
+        reinterpret_cast<vec *>(p)[q] = x;
+      }
+    }
+  }
+};
+
+// sum over the TPR threads of a row, in all of them; `slot`: LDS of the row's wavefronts
+template <int TPR> __device__ __forceinline__ float row_sum(float v, float *slot) {
+#pragma unroll
+  for (int d = 32; d > 0; d >>= 1) v += __shfl_xor(v, d, 64);
+  if constexpr (TPR > 64) {
+    const int wave = threadIdx.x >> 6;
+    __syncthreads();                                   // the last sum has been read
+    if ((threadIdx.x & 63) == 0) slot[wave] = v;
+    __syncthreads();
+    v = 0.f;
+#pragma unroll
+    for (int w = 0; w < TPR / 64; ++w) v += slot[w];
+  }
+  return v;
+}
+
+// V elements of a block of 32 per lane, 32 / V lanes a block
+template <int V> __device__ __forceinline__ void store8(const float (&y)[V], uint8_t *values, uint8_t *exps, int col) {
+  float amax = 0.f;
+#pragma unroll
+  for (int i = 0; i < V; ++i) amax = fmaxf(amax, finite_abs(y[i]));
+#pragma unroll
+  for (int d = 1; d < BLOCK8 / V; d <<= 1) amax = fmaxf(amax, __shfl_xor(amax, d, 64));
+  const unsigned int byte = e4m3_byte(amax);
+  if constexpr (V == 8) {
+    uint2 q;
+    q.x = e4m3_four(y[0], y[1], y[2], y[3], byte);
+    q.y = e4m3_four(y[4], y[5], y[6], y[7], byte);
+    *reinterpret_cast<uint2 *>(values + col) = q;
+  } else {
+    values[col] = (uint8_t)(e4m3_four(y[0], 0.f, 0.f, 0.f, byte) & 0xffu);
+  }
+  if (col % BLOCK8 == 0) exps[col / BLOCK8] = (uint8_t)byte;
+}
+
+// TPR threads a row, NV packs of V elements each; rows wider than that are another instantiation's.
+template <typename T, int V, int TPR, int NV>
+__global__ void __launch_bounds__(TPR > 256 ? TPR : 256) norm_kernel(NormArgs a, int pitch) {
+  constexpr int ROWS = TPR > 256 ? 1 : 256 / TPR;
+  __shared__ float s_sum[16];
+  const int t = threadIdx.x % TPR;
+  const long long row = (long long)blockIdx.x * ROWS + threadIdx.x / TPR;
+  if (row >= a.rows) return;                           // with several rows a block each is one wavefront's
+  const size_t at = (size_t)row * a.d;
+  Pack<T, V> x[NV], w[NV];
+  float sum = 0.f;
+#pragma unroll
+  for (int i = 0; i < NV; ++i) {
+    const int c = (i * TPR + t) * V;
+#pragma unroll
+    for (int q = 0; q < V; ++q) x[i].v[q] = w[i].v[q] = 0.f;
+    if (c < a.d) {
+      x[i].load((const T *)a.X + at + c);
+      w[i].load((const T *)a.weight + c);
+      if (a.R) {
+        Pack<T, V> r;
+        r.load((const T *)a.R + at + c);
+#pragma unroll
+        for (int q = 0; q < V; ++q) x[i].v[q] += r.v[q];
+      }
+    }
+#pragma unroll
+    for (int q = 0; q < V; ++q) sum = fmaf(x[i].v[q], x[i].v[q], sum);
+  }
+  sum = row_sum<TPR>(sum, s_sum);
+  float rstd = 1.0f / sqrtf(sum / (float)a.d + a.eps);
+  if (!(sum < INFINITY)) {                             // squares past fp32's range: the same of values 2^-70 as large
+    sum = 0.f;
+#pragma unroll
+    for (int i = 0; i < NV; ++i)
+#pragma unroll
+      for (int q = 0; q < V; ++q) {
+        const float y = x[i].v[q] * 0x1p-70f;
+        sum = fmaf(y, y, sum);
+      }
+    sum = row_sum<TPR>(sum, s_sum);
+    rstd = 0x1p-70f / sqrtf(sum / (float)a.d);
+  }
+  if (a.rstd && t == 0) a.rstd[row] = rstd;
+#pragma unroll
+  for (int i = 0; i < NV; ++i) {
+    const int c = (i * TPR + t) * V;
+    if (c < a.d) {
+      if (a.S) x[i].store((T *)a.S + at + c);
+#pragma unroll
+      for (int q = 0; q < V; ++q) x[i].v[q] = x[i].v[q] * rstd * w[i].v[q];
+      if (a.Y) x[i].store((T *)a.Y + at + c);
+    }
+    if (a.Y8.values && c < pitch) store8<V>(x[i].v, a.Y8.values + (size_t)row * pitch, a.Y8.exps + (size_t)row * (pitch / BLOCK8), c);
+  }
+}
+
+// Gradient: block b takes rows b, b + gridDim.x, ... (ROWS of them at a time) and leaves its sum of dweight.
+template <typename T, int V, int TPR, int NV>
+__global__ void __launch_bounds__(TPR > 256 ? TPR : 256) norm_bwd_kernel(NormBwdArgs a) {
+  constexpr int ROWS = TPR > 256 ? 1 : 256 / TPR;
+  __shared__ float s_sum[16];
+  const int t = threadIdx.x % TPR, mine = threadIdx.x / TPR;
+  Pack<T, V> w[NV];
+  float dw[NV][V];
+#pragma unroll
+  for (int i = 0; i < NV; ++i) {
+    const int c = (i * TPR + t) * V;
+#pragma unroll
+    for (int q = 0; q < V; ++q) dw[i][q] = w[i].v[q] = 0.f;
+    if (c < a.d) w[i].load((const T *)a.weight + c);
+  }
+  for (long long row = (long long)blockIdx.x * ROWS + mine; row < a.rows; row += (long long)gridDim.x * ROWS) {
+    const size_t at = (size_t)row * a.d;
+    const float rstd = a.rstd[row];
+    Pack<T, V> u[NV], g[NV];
+    float dot = 0.f;
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      const int c = (i * TPR + t) * V;
+#pragma unroll
+      for (int q = 0; q < V; ++q) u[i].v[q] = g[i].v[q] = 0.f;
+      if (c < a.d) {
+        u[i].load((const T *)a.S + at + c);
+        g[i].load((const T *)a.dY + at + c);
+      }
+#pragma unroll
+      for (int q = 0; q < V; ++q) {
+        u[i].v[q] *= rstd;
+        dw[i][q] = fmaf(g[i].v[q], u[i].v[q], dw[i][q]);
+        g[i].v[q] *= w[i].v[q];
+        dot = fmaf(g[i].v[q], u[i].v[q], dot);
+      }
+    }
+    const float mean = row_sum<TPR>(dot, s_sum) / (float)a.d;
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      const int c = (i * TPR + t) * V;
+      if (c < a.d) {
+        Pack<T, V> o;
+#pragma unroll
+        for (int q = 0; q < V; ++q) o.v[q] = rstd * (g[i].v[q] - u[i].v[q] * mean);
+        if (a.dS) {
+          Pack<T, V> up;
+          up.load((const T *)a.dS + at + c);
+#pragma unroll
+          for (int q = 0; q < V; ++q) o.v[q] += up.v[q];
+        }
+        o.store((T *)a.dX + at + c);
+      }
+    }
+  }
+  float *part = a.part + ((size_t)blockIdx.x * ROWS + mine) * a.d;
+#pragma unroll
+  for (int i = 0; i < NV; ++i) {
+    const int c = (i * TPR + t) * V;
+    if (c < a.d) {
+#pragma unroll
+      for (int q = 0; q < V; ++q) part[c + q] = dw[i][q];
+    }
+  }
+}
+
+// dweight = the sum of the parts, in their order within 16 shares of them: 64 columns a block
+template <typename T> __global__ void __launch_bounds__(1024) norm_dweight_kernel(const float *__restrict__ part, int parts, int d, T *__restrict__ dweight) {
+  __shared__ float s_part[16][64];
+  const int c = blockIdx.x * 64 + (threadIdx.x & 63), share = threadIdx.x >> 6;
+  float sum = 0.f;
+  if (c < d) {
+#pragma unroll 8
+    for (int p = share; p < parts; p += 16) sum += part[(size_t)p * d + c];
+  }
+  s_part[share][threadIdx.x & 63] = sum;
+  __syncthreads();
+  if (share == 0 && c < d) {
+#pragma unroll
+    for (int q = 1; q < 16; ++q) sum += s_part[q][threadIdx.x];
+    dweight[c] = from_f32<T>(sum);
+  }
+}
+
+// The shape for rows of d elements: eight at a time where rows start on 16-byte lines, else one.
+template <typename T, typename F> void by_shape(int d, F f) {
+  using std::integral_constant;
+  auto go = [&](auto v, auto tpr, auto nv) { f(v, tpr, nv); };
+  if (d % 8 == 0) {
+    integral_constant<int, 8> v;
+    const int packs = ceil_div(pitch8(d), 8);
+    if (packs <= 64) go(v, integral_constant<int, 64>{}, integral_constant<int, 1>{});
+    else if (packs <= 128) go(v, integral_constant<int, 64>{}, integral_constant<int, 2>{});
+    else if (packs <= 256) go(v, integral_constant<int, 256>{}, integral_constant<int, 1>{});
+    else if (packs <= 512) go(v, integral_constant<int, 256>{}, integral_constant<int, 2>{});
+    else if (packs <= 1024) go(v, integral_constant<int, 256>{}, integral_constant<int, 4>{});
+    else go(v, integral_constant<int, 1024>{}, integral_constant<int, 4>{});
+  } else {
+    integral_constant<int, 1> v;
+    const int n = pitch8(d);
+    if (n <= 256) go(v, integral_constant<int, 64>{}, integral_constant<int, 4>{});
+    else if (n <= 1024) go(v, integral_constant<int, 256>{}, integral_constant<int, 4>{});
+    else if (n <= 4096) go(v, integral_constant<int, 256>{}, integral_constant<int, 16>{});
+    else go(v, integral_constant<int, 1024>{}, integral_constant<int, 32>{});
+  }
+}
+constexpr int BWD_BLOCKS = 512;
+
+template <typename T> int launch_norm_as(hipStream_t s, const NormArgs &a) {
+  by_shape<T>(a.d, [&](auto v, auto tpr, auto nv) {
+    constexpr int TPR = decltype(tpr)::value, ROWS = TPR > 256 ? 1 : 256 / TPR;
+    hipLaunchKernelGGL((norm_kernel<T, decltype(v)::value, TPR, decltype(nv)::value>), dim3(ceil_div(a.rows, ROWS)), dim3(TPR > 256 ? TPR : 256), 0, s, a,
+                       pitch8(a.d));
+  });
+  SMOE_LAUNCH_CHECK();
+  return SMOE_OK;
+}
+template <typename T> int launch_norm_bwd_as(hipStream_t s, const NormBwdArgs &a) {
+  const int parts = norm_bwd_parts(SMOE_BF16, a.rows, a.d);
+  if (a.rows > 0) {
+    by_shape<T>(a.d, [&](auto v, auto tpr, auto nv) {
+      constexpr int TPR = decltype(tpr)::value, ROWS = TPR > 256 ? 1 : 256 / TPR;
+      hipLaunchKernelGGL((norm_bwd_kernel<T, decltype(v)::value, TPR, decltype(nv)::value>), dim3(parts / ROWS), dim3(TPR > 256 ? TPR : 256), 0, s, a);
+    });
+    SMOE_LAUNCH_CHECK();
+  }
+  hipLaunchKernelGGL((norm_dweight_kernel<T>), dim3(ceil_div(a.d, 64)), dim3(1024), 0, s, a.part, a.rows > 0 ? parts : 0, a.d, (T *)a.dweight);
+  SMOE_LAUNCH_CHECK();
+  return SMOE_OK;
+}
+
+}  // namespace
+
+int launch_norm(hipStream_t s, smoe_dtype dt, const NormArgs &a) { return dt == SMOE_BF16 ? launch_norm_as<bf16_t>(s, a) : launch_norm_as<float>(s, a); }
+int norm_bwd_parts(smoe_dtype, int rows, int d) {
+  int per = 1;                   // rows a block has at a time
+  by_shape<float>(d, [&](auto, auto tpr, auto) { per = decltype(tpr)::value > 256 ? 1 : 256 / decltype(tpr)::value; });
+  const int blocks = ceil_div(rows, per);
+  return (blocks < BWD_BLOCKS ? blocks : BWD_BLOCKS) * per;
+}
+int launch_norm_bwd(hipStream_t s, smoe_dtype dt, const NormBwdArgs &a) {
+  return dt == SMOE_BF16 ? launch_norm_bwd_as<bf16_t>(s, a) : launch_norm_bwd_as<float>(s, a);
+}
