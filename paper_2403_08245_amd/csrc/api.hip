@@ -1,6 +1,7 @@
 // C ABI of libsmoe: argument checks, workspace layout and the order of kernel launches for
 // ParallelLinear (Alg. 1, Alg. 2) and the SMoE MLP (Alg. 3).  No entry point allocates,
 // synchronises or touches the host copy of any tensor.
+#include "block.h"
 #include "cache.h"
 #include <new>
 
@@ -110,6 +111,7 @@ int smoe_create(smoe_ctx **out, int device) {
   int rc = SMOE_ERR_HIP;
   if (hipGetDevice(&prev) == hipSuccess && hipSetDevice(device) == hipSuccess) {
     rc = init_stream_kernels();
+    if (rc == SMOE_OK) rc = init_stream8_kernels();
     if (rc == SMOE_OK) rc = init_mfma_kernels();
     if (rc == SMOE_OK) rc = init_route_kernels();
     if (rc == SMOE_OK) rc = route_scratch_address(&c->route_scratch);

@@ -53,7 +53,10 @@ size_t weights8_size(int E, int d_in, int d_out, int halves) { return (size_t)E 
 
 int product8(smoe_ctx *ctx, hipStream_t s, S2S8Args a) {
   a.grid = ctx->stream_grid;
-  return launch_s2s8_decode(s, a);
+  a.group_m = ctx->group_m;
+  a.tile_shape = ctx->tile_shape;
+  const bool few = (long long)a.Tk <= 32LL * a.W.E && !a.tile_shape;
+  return few || ctx->kernel_mode || !s2s8_stream_supported(a) ? launch_s2s8_decode(s, a) : launch_s2s8_stream(s, a);
 }
 
 // Workspace of the MLP: hidden rows and their exponents, and the second product's rows [Tk, d_model] bf16 or fp32.

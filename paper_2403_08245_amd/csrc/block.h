@@ -51,8 +51,12 @@ struct S2S8Args {
   smoe_rows8 H{nullptr, nullptr};  // in C's place: expert-sorted
   int act = SMOE_ACT_NONE;
   size_t call_weights = 0;         // bytes of all the weights that the call may read: past the last-level cache they are read past it
-  int grid = 256;
+  int grid = 256, group_m = 4;     // of the persistent kernels (smoe_ctx)
+  int tile_shape = 0;              // 0 chosen by size, 1 128 x 256 only, 2 256 x 256 only (smoe_ctx)
 };
+bool s2s8_stream_supported(const S2S8Args &a);
+int launch_s2s8_stream(hipStream_t s, const S2S8Args &a);
+int init_stream8_kernels();        // with the context's device current
 int launch_s2s8_decode(hipStream_t s, const S2S8Args &a);
 
 #if defined(__HIPCC__)

@@ -1,0 +1,543 @@
+// The products in 8 bits for many rows: persistent blocks, one per compute unit, four wavefronts 2 x 2 over a 256 x 256 (or 128 x 256) tile,
+// v_mfma_scale_f32_32x32x64_f8f6f4 with the weights as the first operand, so that a lane holds four consecutive columns of a row.
+// Bound: the matrix cores at twice the rate of bf16; an instruction reads as many bytes of operands in as many cycles, so the loop is the
+// one of the bf16 kernels (gemm_stream.hip) with stages of 128 elements instead of 64: the same 128 bytes a row.
+//
+// A stage is 128 elements of the contraction.  Rows come as whole 128-byte lines, 16-byte chunks permuted by the row; weights lie in memory as
+// they are read from LDS (smoe_weights8), 2 KB for 16 columns; both go to LDS directly, and so do the powers of two: four bytes for a row or column and
+// stage.  Two slots.  The first half of a stage multiplies what is in registers and reads the second half's operands; then the slot is
+// free, and the second half issues the loads of the stage after next, waits for the next stage and reads its first half.
+// The loader walks the block's list of tiles ahead of the multiplying side, so a tile's first stages land while the one before it is written out.
+//
+// Operands of an instruction: lane (r, h) = (lane % 32, lane / 32) holds elements 16 h .. 16 h + 15 and 32 + 16 h .. of row or column r, and the power
+// of two of its elements 32 h .. 32 h + 31.
+#include "block.h"
+#include "gemm_epilogue.h"
+#include <type_traits>
+
+namespace {
+
+typedef int i32x8 __attribute__((ext_vector_type(8)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+constexpr int B8_BYTES = TB * ROW8;                     // weights of a stage, 256 columns
+constexpr int MAX_E8 = 256;
+
+template <int FM_> struct Shape8 {
+  static constexpr int FM = FM_;                        // 32-row fragments per wavefront
+  static constexpr int TM = FM * 64;                    // tile rows; columns are TB = 256
+  static constexpr int A_BYTES = TM * ROW8;
+  static constexpr int NLA = A_BYTES / 4096, NLB = B8_BYTES / 4096;   // load instructions per wavefront and stage
+  static constexpr int NL = NLA + NLB + 2;              // and the powers of two of the rows and the columns
+  // LDS: rows of two slots, weights of two, then powers of two of rows and columns, then each wavefront's patch
+  static constexpr int OFF_B = 2 * A_BYTES, OFF_EA = OFF_B + 2 * B8_BYTES, OFF_EB = OFF_EA + 2 * TM * 4, OFF_PATCH = OFF_EB + 2 * TB * 4;
+  static constexpr int LDS_BYTES = OFF_PATCH + 4 * EPI_WAVE_BYTES;
+};
+using Big8 = Shape8<4>;
+using Half8 = Shape8<2>;
+
+enum { OUT_BF16, OUT_F32, OUT_SWIGLU, OUT_GELU };
+// store instructions that a wavefront issues per tile
+template <int FM, int OUT> constexpr int Stores8 = FM * (OUT == OUT_BF16 ? 8 : OUT == OUT_F32 ? 16 : OUT == OUT_SWIGLU ? 3 : 5);
+
+// first[e] = M-tiles of the experts before e, by every wavefront for itself (all write the same); returns first[E]
+template <int TM> __device__ __forceinline__ int number_tiles8(const int32_t *offsets, int E, int *first, int lane) {
+  int base = 0;
+  if (lane == 0) first[0] = 0;
+  for (int c0 = 0; c0 < E; c0 += 64) {
+    const int x = c0 + lane;
+    int n = x < E ? (offsets[x + 1] - offsets[x] + TM - 1) / TM : 0;
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+      const int up = __shfl_up(n, d, 64);
+      if (lane >= d) n += up;
+    }
+    if (x < E) first[x + 1] = base + n;
+    base += __builtin_amdgcn_readlane(n, 63);
+  }
+  return base;
+}
+template <int TM>
+__device__ __forceinline__ void find_tile8(const int32_t *offsets, const int *first, int E, int tile, int lane, int &e, int &row0, int &row_end) {
+  e = E - 1;
+  for (int c0 = 0; c0 < E; c0 += 64) {
+    const unsigned long long owns = __ballot(first[min(c0 + lane, E - 1) + 1] > tile);
+    if (!owns) continue;
+    e = c0 + __ffsll((long long)owns) - 1;
+    break;
+  }
+  row0 = __builtin_amdgcn_readfirstlane(offsets[e]) + (tile - __builtin_amdgcn_readfirstlane(first[e])) * TM;
+  row_end = __builtin_amdgcn_readfirstlane(offsets[e + 1]);
+}
+
+// Sources of the loader's current tile: range-checked windows and per-lane byte offsets at step 0.
+template <typename S> struct Loader8 {
+  int32x4 win_a, win_ea, win_b, win_eb;
+  uint32_t oa[S::NLA], oea, ob, oeb;
+  uint32_t group_bytes;              // of a group of 16 columns: steps * 2048
+  int step, uwave;
+  __device__ __forceinline__ void load(int I, uint32_t lds0, int slot) const {
+    if (I < S::NLA) {
+      load16_to_lds_checked(win_a, oa[I] + (uint32_t)step * ROW8, lds0 + slot * S::A_BYTES + uwave * (S::NLA * 1024), I * 1024);
+    } else if (I < S::NLA + S::NLB) {
+      const int J = I - S::NLA;
+      load16_to_lds_checked(win_b, ob + ((uint32_t)(J >> 1) * group_bytes + (uint32_t)step * 2048u + (uint32_t)(J & 1) * 1024u),
+                            lds0 + S::OFF_B + slot * B8_BYTES + uwave * (S::NLB * 1024), J * 1024);
+    } else if (I == S::NLA + S::NLB) {
+      load4_to_lds_checked(win_ea, oea + (uint32_t)step * 4u, lds0 + S::OFF_EA + slot * (S::TM * 4) + (uwave & (S::TM / 64 - 1)) * 256);
+    } else {
+      load4_to_lds_checked(win_eb, oeb + (uint32_t)step * 64u, lds0 + S::OFF_EB + slot * (TB * 4) + uwave * 256);
+    }
+  }
+};
+
+// a wavefront's operands of 64 elements
+template <int FM> struct Frags8 {
+  i32x8 a[FM], b[FR];
+};
+template <int FM> struct Exps8 {
+  int a[FM], b[FR];
+};
+// Where the lane reads in a slot.
+struct Reader8 {
+  uint32_t fa[4], fb;                // chunk kk of the rows' fragments; of the columns': further chunks lie 512 bytes on
+  uint32_t ea, eb;
+  int shift;                         // of the power of two in its four bytes
+  // part `i` of half s: fragment b0 a0 b1 b2 b3 a1 .., 16 bytes of each, twice
+  template <typename S> __device__ __forceinline__ void read(Frags8<S::FM> &f, int i, const char *smem, int slot, int s) const {
+    const int frag = i >> 1, t = i & 1, kk = 2 * s + t;
+    const char *a = smem + slot * S::A_BYTES, *b = smem + S::OFF_B + slot * B8_BYTES;
+    const bool rows = frag == 1 || frag > FR;
+    const int n = frag == 0 ? 0 : frag == 1 ? 0 : frag <= FR ? frag - 1 : frag - FR;
+    const i32x4 v = rows ? *reinterpret_cast<const i32x4 *>(a + fa[kk] + n * 4096) : *reinterpret_cast<const i32x4 *>(b + fb + kk * 512 + n * 4096);
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      if (rows) f.a[n][4 * t + q] = v[q];
+      else f.b[n][4 * t + q] = v[q];
+    }
+  }
+  template <typename S> __device__ __forceinline__ void read_exps(Exps8<S::FM> &x, const char *smem, int slot) const {
+#pragma unroll
+    for (int n = 0; n < S::FM; ++n) x.a[n] = *reinterpret_cast<const int *>(smem + S::OFF_EA + slot * (S::TM * 4) + ea + n * 128);
+#pragma unroll
+    for (int n = 0; n < FR; ++n) x.b[n] = *reinterpret_cast<const int *>(smem + S::OFF_EB + slot * (TB * 4) + eb + n * 128);
+  }
+  template <int FM> __device__ __forceinline__ void shift_exps(Exps8<FM> &x) const {
+#pragma unroll
+    for (int n = 0; n < FM; ++n) x.a[n] = (int)((unsigned)x.a[n] >> shift);
+#pragma unroll
+    for (int n = 0; n < FR; ++n) x.b[n] = (int)((unsigned)x.b[n] >> shift);
+  }
+};
+
+// The products of one half of a stage; behind(m) issues what goes behind fragment row m.
+template <bool FIRST, int HALF_, int FM, typename Behind>
+__device__ __forceinline__ void multiply8(const Frags8<FM> &f, const Exps8<FM> &x, f32x16 (&acc)[FM][FR], Behind behind) {
+  f32x16 zero;
+#pragma unroll
+  for (int q = 0; q < 16; ++q) zero[q] = 0.f;
+  sched_fence();
+#pragma unroll
+  for (int m = 0; m < FM; ++m) {
+#pragma unroll
+    for (int n = 0; n < FR; ++n)
+      acc[m][n] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(f.b[n], f.a[m], FIRST ? zero : acc[m][n], 0, 0, 2 * HALF_, x.b[n], 2 * HALF_, x.a[m]);
+    behind(m);
+    sched_fence();
+  }
+}
+
+// One stage in slot `cur`, the next in `nxt`.  f[0] and x hold its first half and its powers of two on entry, the next stage's on exit.
+// STORES: at least that many stores were issued after the next stage's loads.
+template <bool FIRST, int STORES, typename S, typename Slot, typename Next>
+__device__ __forceinline__ void stage8(const Loader8<S> &ld, const Reader8 &rd, Frags8<S::FM> (&f)[2], Exps8<S::FM> &x, f32x16 (&acc)[S::FM][FR], const char *smem,
+                                       uint32_t lds0, Slot cur, Next nxt) {
+  constexpr int FM = S::FM, PARTS = 2 * (FM + FR);
+  multiply8<FIRST, 0>(f[0], x, acc, [&](int m) {
+#pragma unroll
+    for (int i = 0; i < PARTS; ++i)
+      if (i >= m * PARTS / FM && i < (m + 1) * PARTS / FM) rd.template read<S>(f[1], i, smem, (int)cur, 1);
+  });
+  __syncthreads();      // every wavefront holds the stage: its slot is free
+  constexpr int EARLY = S::NL / FM;
+  Exps8<FM> y;
+  multiply8<false, 1>(f[1], x, acc, [&](int m) {
+#pragma unroll
+    for (int i = 0; i < S::NL; ++i)
+      if (i >= m * S::NL / FM && i < (m + 1) * S::NL / FM) ld.load(i, lds0, (int)cur);
+    if (m == 0) {       // the next stage has landed
+      wait_loads<(EARLY + STORES < 63 ? EARLY + STORES : 63)>();
+      __syncthreads();
+      rd.template read_exps<S>(y, smem, (int)nxt);
+    }
+    if (m > 0 || FM == 1) {
+#pragma unroll
+      for (int i = 0; i < PARTS; ++i)
+        if (i >= (m - 1) * PARTS / (FM - 1) && i < m * PARTS / (FM - 1)) rd.template read<S>(f[0], i, smem, (int)nxt, 0);
+    }
+  });
+  rd.shift_exps(y);
+  x = y;
+}
+
+// 32 rows of fp32 through the patch, 32 columns at a time
+template <int FM, typename DestFn> __device__ __forceinline__ void store_wave_tile_f32(const f32x16 (&acc)[FM][FR], char *patch, DestFn dest, int lane) {
+  acc_settle();
+  RowStore<decltype(dest(0, 0))> pend;
+#pragma unroll
+  for (int fm = 0; fm < FM; ++fm)
+#pragma unroll
+    for (int fn = 0; fn < FR; ++fn)
+      pipe_block(pend, patch, lane, [&] {
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+          f32x4 v;
+#pragma unroll
+          for (int q = 0; q < 4; ++q) v[q] = acc_read(acc[fm][fn][g * 4 + q]);
+          *reinterpret_cast<f32x4 *>(patch_slot(patch, lane & 31, 2 * g + (lane >> 5))) = v;
+        }
+      }, dest(fm, fn));
+  sched_fence();
+  issue_row_store(pend);
+}
+
+// Sixteen values of a row's block of 32 (its other lane has the rest): their codes, four to a word, and the block's byte.
+__device__ __forceinline__ unsigned int pack_block(float (&h)[16], unsigned int (&code)[4]) {
+  float amax = 0.f;
+#pragma unroll
+  for (int i = 0; i < 16; ++i) amax = fmaxf(amax, fabsf(h[i]));       // NaN is passed over, and comes out of the conversion as NaN
+  amax = fmaxf(amax, __shfl_xor(amax, 32, 64));
+  unsigned int byte = e4m3_byte(amax);
+  if (__any(byte > 246u)) {                                            // infinities, and values next to fp32's end: as e4m3_scaled has them
+    amax = 0.f;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) amax = fmaxf(amax, finite_abs(h[i]));
+    amax = fmaxf(amax, __shfl_xor(amax, 32, 64));
+    byte = e4m3_byte(amax);
+#pragma unroll
+    for (int g = 0; g < 4; ++g) code[g] = e4m3_four(h[4 * g], h[4 * g + 1], h[4 * g + 2], h[4 * g + 3], byte);
+    return byte;
+  }
+  const float inv = __uint_as_float((254u - byte) << 23);
+#pragma unroll
+  for (int g = 0; g < 4; ++g) {
+    const int lo = __builtin_amdgcn_cvt_pk_fp8_f32(h[4 * g] * inv, h[4 * g + 1] * inv, 0, false);
+    code[g] = (unsigned int)__builtin_amdgcn_cvt_pk_fp8_f32(h[4 * g + 2] * inv, h[4 * g + 3] * inv, lo, true);
+  }
+  return byte;
+}
+
+// EVEN: an even number of stages, so that every tile starts in slot 0 and slots are constants.
+template <typename S, int OUT, bool SCATTER, bool EVEN>
+__global__ void __launch_bounds__(NTHREADS, 1) s2s8_stream_kernel(S2S8Args a, int tiles_n, int group_m, uint32_t magic_a) {
+  constexpr bool HIDDEN = OUT == OUT_SWIGLU || OUT == OUT_GELU;
+  constexpr int STORES = Stores8<S::FM, OUT>;
+  extern __shared__ __attribute__((aligned(1024))) char smem[];
+  __shared__ int s_off[MAX_E8 + 1], s_first[MAX_E8 + 1];
+  // order indices of the rows of up to four open tiles, and the tiles: the loader has opened tile n + 2 and requested the rows of n + 3 while
+  // tile n is written out (contractions have two stages at least).
+  __shared__ int s_idx[4][S::TM];
+  __shared__ __attribute__((aligned(16))) int s_tile[4][4];
+
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+  const int uwave = __builtin_amdgcn_readfirstlane(wave);
+  const int uwm = uwave >> 1, uwn = uwave & 1;
+  const int G = gridDim.x;
+  const int pos = ((int)blockIdx.x & 7) * (G >> 3) + ((int)blockIdx.x >> 3);   // blocks b, b + 8, ... share an XCD and get consecutive tiles
+  const int steps = (a.W.d_in + ROW8 - 1) / ROW8;
+  const int ns = steps;
+  for (int i = threadIdx.x; i <= a.W.E; i += NTHREADS) s_off[i] = a.offsets[i];
+  __syncthreads();
+  const int m_tiles = number_tiles8<S::TM>(s_off, a.W.E, s_first, lane);
+  const long long total = (long long)m_tiles * tiles_n;
+  const int tiles = (int)((total - pos + G - 1) / G);   // of this block: pos, pos + G, ..
+  auto args = [&]() {                                   // read again where they are used, once a tile
+    auto p = (const __attribute__((address_space(4))) S2S8Args *)__builtin_amdgcn_kernarg_segment_ptr();
+    __asm__ volatile("" : "+s"(p));
+    return p;
+  };
+  struct Tile {
+    int seq;                        // position in this block's list (-1 before the first)
+    int e, row0, row_end, n0;       // n0: first column, or hidden unit
+  };
+  auto next_tile = [&](Tile &t) -> bool {
+    const int seq = t.seq + 1;
+    if (seq >= tiles) return false;
+    int mt, nt;
+    tile_coords(seq * G + pos, m_tiles, tiles_n, group_m, mt, nt);
+    t.seq = seq;
+    find_tile8<S::TM>(s_off, s_first, args()->W.E, mt, lane, t.e, t.row0, t.row_end);
+    t.n0 = nt * (OUT == OUT_SWIGLU ? TB / 2 : TB);
+    *reinterpret_cast<int4 *>(s_tile[seq & 3]) = make_int4(t.e, t.row0, t.row_end, t.n0);
+    return true;
+  };
+  auto follow = [&](Tile &t) -> bool {
+    if (t.seq + 1 >= tiles) return false;
+    ++t.seq;
+    const int4 v = *reinterpret_cast<const int4 *>(s_tile[t.seq & 3]);
+    t.e = __builtin_amdgcn_readfirstlane(v.x);
+    t.row0 = __builtin_amdgcn_readfirstlane(v.y);
+    t.row_end = __builtin_amdgcn_readfirstlane(v.z);
+    t.n0 = __builtin_amdgcn_readfirstlane(v.w);
+    return true;
+  };
+  // order indices of a tile's rows (rows past the segment repeat its last one's)
+  auto fetch_rows = [&](const Tile &t) {
+    const auto p = args();
+    const int32_t *o = p->a_map.o ? p->a_map.o : p->c_map.o;
+    if (!o) return;
+    const int part = wave & (S::TM / 64 - 1);
+    const int i = min(t.row0 + part * 64 + lane, t.row_end - 1);
+    load4_to_lds(o + i, __builtin_amdgcn_readfirstlane(lds_address((const char *)&s_idx[t.seq & 3][0])) + (uwave & (S::TM / 64 - 1)) * 256);
+  };
+
+  Loader8<S> ld;
+  ld.uwave = uwave;
+  ld.group_bytes = (uint32_t)steps * 2048u;
+  Reader8 rd;
+#pragma unroll
+  for (int kk = 0; kk < 4; ++kk) rd.fa[kk] = line_frag_offset((wave >> 1) * (S::TM / 2), kk, lane);
+  rd.fb = (uint32_t)((wave & 1) * 16384 + ((lane >> 4) & 1) * 2048 + (lane >> 5) * 256 + (lane & 15) * 16);
+  rd.ea = (uint32_t)((wave >> 1) * (S::TM / 2) + (lane & 31)) * 4u;
+  rd.eb = (uint32_t)((wave & 1) * (TB / 2) + (lane & 31)) * 4u;
+  rd.shift = (lane >> 5) * 8;
+  uint32_t chunk[2];                 // source chunk of the lane's 16 bytes in a row, even and odd load instructions
+#pragma unroll
+  for (int p = 0; p < 2; ++p) chunk[p] = (uint32_t)((lane & 7) ^ line_swz(p * 8 + (lane >> 3))) * 16u;
+  const uint32_t whole = magic_a ? 0u : ~0u;
+  auto source_row = [&](uint32_t slot) { return __umulhi(slot, magic_a) + (slot & whole); };
+  auto setup_sources = [&](const Tile &t) {
+    const auto p = args();
+    const uint32_t pitch = (uint32_t)steps * ROW8;
+    const bool gathered = p->a_map.o != nullptr;
+    const uint32_t rows = gathered ? source_row((uint32_t)p->Tk) : (uint32_t)min(S::TM, t.row_end - t.row0);
+    const size_t first = gathered ? 0 : (size_t)t.row0;
+    ld.win_a = buffer_window(p->X.values + first * pitch, rows * pitch);
+    ld.win_ea = buffer_window(p->X.exps + first * (pitch / BLOCK8), rows * (pitch / BLOCK8));
+    const uint32_t per_expert = (uint32_t)(p->W.halves * 2 * ((p->W.d_out / p->W.halves + 31) / 32)) * ld.group_bytes;
+    ld.win_b = buffer_window(p->W.values + (size_t)t.e * per_expert, per_expert);
+    ld.win_eb = buffer_window(p->W.exps + (size_t)t.e * (per_expert / BLOCK8), per_expert / BLOCK8);
+    const int *idx = &s_idx[t.seq & 3][0];
+    // rows past the segment read zeros: an offset outside the window at every stage
+    const uint32_t past = 0x80000000u;
+#pragma unroll
+    for (int I = 0; I < S::NLA; ++I) {
+      const int r = (wave * S::NLA + I) * 8 + (lane >> 3);
+      const uint32_t src = gathered ? source_row((uint32_t)idx[r]) : (uint32_t)r;
+      ld.oa[I] = r < t.row_end - t.row0 ? src * pitch + chunk[I & 1] : past;
+    }
+    const int r = (wave & (S::TM / 64 - 1)) * 64 + lane;
+    const uint32_t src = gathered ? source_row((uint32_t)idx[r]) : (uint32_t)r;
+    ld.oea = r < t.row_end - t.row0 ? src * (pitch / BLOCK8) : past;
+    // The wavefront loads four groups of 16 columns.  SwiGLU: a wavefront's 128 columns of the tile are 64 gates and their 64 ups.
+    const int half_groups = (p->W.d_out / 2 + 31) / 32 * 2;
+    const uint32_t group = OUT == OUT_SWIGLU ? (uint32_t)(t.n0 / 16 + (wave >> 1) * 4 + (wave & 1) * half_groups) : (uint32_t)(t.n0 / 16 + wave * 4);
+    ld.ob = group * ld.group_bytes + lane * 16u;
+    ld.oeb = group * (ld.group_bytes / BLOCK8) + (uint32_t)(lane >> 4) * (ld.group_bytes / BLOCK8) + (uint32_t)(lane & 15) * 4u;
+  };
+
+  // ---- open the first two tiles
+  Tile lt{-1, 0, 0, 0, 0};
+  if (!next_tile(lt)) return;
+  Tile ct = lt, upcoming = lt;
+  bool have_upcoming = next_tile(upcoming);
+  fetch_rows(lt);
+  if (have_upcoming) fetch_rows(upcoming);
+  wait_loads<0>();
+  __syncthreads();
+  setup_sources(lt);
+  ld.step = 0;
+  bool loader_live = true;
+  auto advance_loader = [&]() {
+    if (!loader_live) return;
+    if (++ld.step < ns) return;
+    if (!have_upcoming) {
+      loader_live = false;
+      --ld.step;                    // stages past the end repeat the last one's addresses
+      return;
+    }
+    lt = upcoming;
+    ld.step = 0;
+    have_upcoming = next_tile(upcoming);
+    if (have_upcoming) fetch_rows(upcoming);
+    setup_sources(lt);
+  };
+  const uint32_t lds0 = __builtin_amdgcn_readfirstlane(lds_address(smem));
+#pragma unroll 1
+  for (int st = 0; st < 2; ++st) {
+#pragma unroll
+    for (int I = 0; I < S::NL; ++I) ld.load(I, lds0, st);
+    advance_loader();
+  }
+  wait_loads<0>();
+  __syncthreads();
+  f32x16 acc[S::FM][FR];
+  Frags8<S::FM> f[2];
+  Exps8<S::FM> x;
+#pragma unroll
+  for (int i = 0; i < 2 * (S::FM + FR); ++i) rd.template read<S>(f[0], i, smem, 0, 0);
+  rd.template read_exps<S>(x, smem, 0);
+  rd.shift_exps(x);
+
+  int cur = 0;
+  using I0 = std::integral_constant<int, 0>;
+  using I1 = std::integral_constant<int, 1>;
+  for (;;) {                        // one tile per trip
+    if constexpr (EVEN) {
+      if (ct.seq > 0) stage8<true, STORES, S>(ld, rd, f, x, acc, smem, lds0, I0{}, I1{});
+      else stage8<true, 0, S>(ld, rd, f, x, acc, smem, lds0, I0{}, I1{});
+      advance_loader();
+      stage8<false, 0, S>(ld, rd, f, x, acc, smem, lds0, I1{}, I0{});
+      advance_loader();
+      for (int h = 2; h < ns; h += 2) {
+        stage8<false, 0, S>(ld, rd, f, x, acc, smem, lds0, I0{}, I1{});
+        advance_loader();
+        stage8<false, 0, S>(ld, rd, f, x, acc, smem, lds0, I1{}, I0{});
+        advance_loader();
+      }
+    } else {
+      if (ct.seq > 0) stage8<true, STORES, S>(ld, rd, f, x, acc, smem, lds0, cur, cur ^ 1);
+      else stage8<true, 0, S>(ld, rd, f, x, acc, smem, lds0, cur, cur ^ 1);
+      advance_loader();
+      cur ^= 1;
+      for (int h = 1; h < ns; ++h) {
+        stage8<false, 0, S>(ld, rd, f, x, acc, smem, lds0, cur, cur ^ 1);
+        advance_loader();
+        cur ^= 1;
+      }
+    }
+    const int lane = lane_here(threadIdx.x & 63);
+    char *patch = smem + S::OFF_PATCH + uwave * EPI_WAVE_BYTES;
+    const auto p = args();
+    const int N = p->W.d_out;
+    const int rbase = ct.row0 + uwm * (S::TM / 2);            // the wavefront's first row
+    const int left = max(min(S::TM / 2, ct.row_end - rbase), 0);
+    const int *idx = &s_idx[ct.seq & 3][uwm * (S::TM / 2)];
+    if constexpr (!HIDDEN) {
+      constexpr int ES = OUT == OUT_F32 ? 4 : 2, PER = 16 / ES;      // bytes of an element, elements of a 16-byte chunk
+      const int wcol = ct.n0 + uwn * (TB / 2);
+      const window_t win = SCATTER ? make_window(p->C, (uint32_t)p->Tk * (uint32_t)N * ES)
+                                   : make_window((const char *)p->C + (size_t)rbase * N * ES, (uint32_t)left * (uint32_t)N * ES);
+      auto dest = [&](int fm, int block) {                           // 128 bytes of 32 rows
+        BlockDest d{win, {}};
+        const int col = wcol + (block * 8 + (lane & 7)) * PER;
+#pragma unroll
+        for (int it = 0; it < 4; ++it) {
+          const int r = fm * 32 + it * 8 + (lane >> 3);
+          const uint32_t row = SCATTER ? (uint32_t)idx[r] : (uint32_t)r;
+          d.off[it] = r < left && col < N ? (row * (uint32_t)N + (uint32_t)col) * ES : ~0u;
+        }
+        return d;
+      };
+      if constexpr (OUT == OUT_F32) store_wave_tile_f32(acc, patch, dest, lane);
+      else store_wave_tile(acc, patch, dest, lane);
+    } else {
+      // hidden rows: 64 (SwiGLU) or 128 units of the wavefront, blocks of 32
+      constexpr int BLOCKS = OUT == OUT_SWIGLU ? 2 : 4, UNITS = BLOCKS * 32;
+      const int half = N / p->W.halves, pitch = (half + ROW8 - 1) / ROW8 * ROW8, padded = (half + 31) / 32 * 32;
+      const int unit0 = ct.n0 + uwn * UNITS;
+      const window_t win = make_window(p->H.values + (size_t)rbase * pitch, (uint32_t)left * (uint32_t)pitch);
+      const window_t win_e = make_window(p->H.exps + (size_t)rbase * (pitch / BLOCK8), (uint32_t)left * (uint32_t)(pitch / BLOCK8));
+      acc_settle();
+#pragma unroll
+      for (int fm = 0; fm < S::FM; ++fm) {
+        sched_fence();
+        unsigned int bytes = 0;
+#pragma unroll
+        for (int b = 0; b < BLOCKS; ++b) {
+          float h[16];
+          unsigned int code[4];
+          const bool exists = unit0 + b * 32 < padded;               // whole blocks; a half's padding has weights of zero
+#pragma unroll
+          for (int i = 0; i < 16; ++i) {
+            const float v = acc_read(acc[fm][b][i]);
+            if constexpr (OUT == OUT_SWIGLU) {
+              const float up = acc_read(acc[fm][2 + b][i]);
+              h[i] = v * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-1.4426950408889634f * v)) * up;
+            } else {
+              h[i] = gelu_f(v);
+            }
+            if (!exists) h[i] = 0.f;
+          }
+          bytes |= pack_block(h, code) << (8 * b);
+          // patch: rows of UNITS bytes, 16-byte chunks permuted by the row
+#pragma unroll
+          for (int g = 0; g < 4; ++g) {
+            const int c = b * 2 + (g >> 1);                          // the chunk of units 8 g + 4 (lane / 32) .. of the block
+            const int row = lane & 31;
+            const int at = OUT == OUT_SWIGLU ? row * 64 + ((c ^ ((row >> 1) & 3)) << 4) : row * 128 + ((c ^ (row & 7)) << 4);
+            *reinterpret_cast<unsigned int *>(patch + at + (g & 1) * 8 + (lane >> 5) * 4) = code[g];
+          }
+        }
+        sched_fence();
+        constexpr int PER_ROW = UNITS / 16, ROWS = 64 / PER_ROW;     // lanes of a row, rows at a time
+#pragma unroll
+        for (int it = 0; it < 32 / ROWS; ++it) {
+          const int row = it * ROWS + lane / PER_ROW, c = lane % PER_ROW;
+          const int at = OUT == OUT_SWIGLU ? row * 64 + ((c ^ ((row >> 1) & 3)) << 4) : row * 128 + ((c ^ (row & 7)) << 4);
+          const i32x4 v = *reinterpret_cast<const i32x4 *>(patch + at);
+          const int col = unit0 + c * 16;
+          const uint32_t off = fm * 32 + row < left && col < pitch ? (uint32_t)(fm * 32 + row) * (uint32_t)pitch + (uint32_t)col : ~0u;
+          __builtin_amdgcn_raw_buffer_store_b128(v, win, (int)off, 0, 0);
+        }
+        const uint32_t off = lane < 32 && fm * 32 + lane < left && unit0 < pitch ? (uint32_t)(fm * 32 + lane) * (uint32_t)(pitch / BLOCK8) + (uint32_t)(unit0 / BLOCK8) : ~0u;
+        if constexpr (OUT == OUT_SWIGLU) __builtin_amdgcn_raw_buffer_store_b16((short)bytes, win_e, (int)off, 0, 0);
+        else __builtin_amdgcn_raw_buffer_store_b32((int)bytes, win_e, (int)off, 0, 0);
+      }
+    }
+    if (!follow(ct)) break;
+  }
+  wait_loads<0>();
+}
+
+template <typename S, int OUT, bool SCATTER> int launch_as(hipStream_t s, const S2S8Args &a) {
+  const int steps = ceil_div(a.W.d_in, ROW8), hidden = pitch8(a.W.d_out / a.W.halves);
+  const int tiles_n = OUT == OUT_SWIGLU ? ceil_div(hidden, TB / 2) : OUT == OUT_GELU ? ceil_div(hidden, TB) : ceil_div(a.W.d_out, TB);
+  const uint32_t magic = a.a_map.o ? division_magic(a.a_map.fan) : 0u;
+  const dim3 grid(a.grid), block(NTHREADS);
+  if (steps % 2 == 0) hipLaunchKernelGGL((s2s8_stream_kernel<S, OUT, SCATTER, true>), grid, block, S::LDS_BYTES, s, a, tiles_n, a.group_m, magic);
+  else hipLaunchKernelGGL((s2s8_stream_kernel<S, OUT, SCATTER, false>), grid, block, S::LDS_BYTES, s, a, tiles_n, a.group_m, magic);
+  SMOE_LAUNCH_CHECK();
+  return SMOE_OK;
+}
+template <typename S> int launch(hipStream_t s, const S2S8Args &a) {
+  if (a.act == SMOE_ACT_SWIGLU) return launch_as<S, OUT_SWIGLU, false>(s, a);
+  if (a.act == SMOE_ACT_GELU) return launch_as<S, OUT_GELU, false>(s, a);
+  if (a.wide) return launch_as<S, OUT_F32, true>(s, a);
+  return a.c_map.o ? launch_as<S, OUT_BF16, true>(s, a) : launch_as<S, OUT_BF16, false>(s, a);
+}
+template <typename S, int OUT, bool SCATTER> int init_as() {
+  int rc = set_lds_limit(s2s8_stream_kernel<S, OUT, SCATTER, true>, S::LDS_BYTES);
+  return rc == SMOE_OK ? set_lds_limit(s2s8_stream_kernel<S, OUT, SCATTER, false>, S::LDS_BYTES) : rc;
+}
+template <typename S> int init() {
+  int rc = init_as<S, OUT_SWIGLU, false>();
+  if (rc == SMOE_OK) rc = init_as<S, OUT_GELU, false>();
+  if (rc == SMOE_OK) rc = init_as<S, OUT_F32, true>();
+  if (rc == SMOE_OK) rc = init_as<S, OUT_BF16, true>();
+  if (rc == SMOE_OK) rc = init_as<S, OUT_BF16, false>();
+  return rc;
+}
+
+}  // namespace
+
+int init_stream8_kernels() {
+  const int rc = init<Big8>();
+  return rc == SMOE_OK ? init<Half8>() : rc;
+}
+
+// 32-bit offsets into the rows, an expert's weights and a scattered output; the fan-out's division.
+bool s2s8_stream_supported(const S2S8Args &a) {
+  if (a.Tk < 1 || a.W.E > MAX_E8 || a.grid < 8 || a.W.d_in <= ROW8) return false;      // two stages at least
+  if (a.wide && !a.c_map.o) return false;
+  const unsigned long long pitch = pitch8(a.W.d_in), rows = a.a_map.o ? a.Tk / a.a_map.fan : 256;
+  if (rows * pitch > 0x7fff0000ULL || (unsigned long long)groups8(a.W.d_out, a.W.halves) * 16 * pitch + 32 * pitch * 16 > 0x7fff0000ULL) return false;
+  if (!a.H.values && a.c_map.o && (unsigned long long)a.Tk * a.W.d_out * (a.wide ? 4 : 2) > 0xfffffff0ULL) return false;
+  if (256ULL * a.W.d_out * 2 > 0x7fff0000ULL) return false;
+  if (a.a_map.o && (unsigned long long)a.Tk * a.a_map.fan >= 0x100000000ULL) return false;
+  const long long m_tiles = (long long)a.Tk / 128 + a.W.E, n_tiles = ceil_div(a.W.d_out, 128);
+  return m_tiles * n_tiles <= 0x7fffffffLL;
+}
+int launch_s2s8_stream(hipStream_t s, const S2S8Args &a) {
+  if (!s2s8_stream_supported(a)) return SMOE_ERR_UNSUPPORTED;
+  return a.tile_shape == 1 ? launch<Half8>(s, a) : launch<Big8>(s, a);
+}

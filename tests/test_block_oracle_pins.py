@@ -85,6 +85,24 @@ def test_packed_rows_by_hand():
     assert (codes[0, 40:] == 0).all()
 
 
+def test_packed_rows_are_the_caches_block_by_block():
+    """e4m3 with a power of two, as the oracle of the cache searches it out one value at a time."""
+    g = np.random.default_rng(5)
+    x = g.normal(size=(40, 64)) * np.exp(g.normal(size=(40, 1)) * 20)
+    x[0] = 0
+    x[1, 3], x[2, 4], x[3] = math.nan, -math.inf, math.inf
+    x[4] *= 2.0 ** -150
+    x[5] = np.sign(x[5]) * 1.96 * 2.0 ** 127
+    x[6, 0], x[6, 1:] = 448.0, 2.0 ** -10 * np.arange(63)
+    x[7, 0], x[7, 1:] = 448.0, 16 + 0.5 * np.arange(63)
+    x[8] = -0.0
+    codes, exps = oracle.pack8(x)
+    for i in range(40):
+        for b in range(2):
+            want, e = oracle.e4m3_encode(x[i, 32 * b:32 * b + 32])
+            assert np.array_equal(codes[i, 32 * b:32 * b + 32], want) and exps[i, b] == e + 127, (i, b)
+
+
 def test_packed_products_are_the_plain_ones_on_exact_values():
     """Small whole numbers are exact in 8 bits, also as hidden rows of an activation that keeps them (GELU far from 0 is the identity)."""
     g = np.random.default_rng(3)
