@@ -56,7 +56,9 @@ GATES = [  # T, E, k, score, bias, groups, kept, best, renormalise, scale
     (7, 60, 6, "sigmoid", True, 5, 2, 2, True, 16.0), (130, 256, 8, "sigmoid", True, 8, 4, 2, True, 2.5), (9, 256, 8, "sigmoid", False, 8, 3, 1, False, 1.0),
     (6, 96, 5, "softmax", False, 8, 2, 2, False, 1.0), (4, 1000, 16, "sigmoid", True, 4, 1, 2, True, 1.0), (3, 1024, 64, "softmax", False, 1, 1, 1, False, 3.0),
     (5, 512, 12, "softmax", True, 16, 5, 1, True, 1.0), (8, 64, 64, "sigmoid", True, 64, 64, 1, True, 1.0), (11, 160, 7, "sigmoid", True, 5, 1, 2, False, 0.5),
-    (4, 3, 3, "sigmoid", False, 3, 3, 2, True, 1.0), (2, 2, 1, "sigmoid", True, 2, 1, 2, True, 1.0), (6, 65, 3, "softmax", True, 13, 4, 2, True, -1.0),
+    (2500, 256, 8, "sigmoid", True, 8, 4, 2, True, 2.5), (1501, 64, 6, "softmax", True, 1, 1, 1, False, 1.0), (999, 128, 16, "sigmoid", False, 16, 5, 2, True, 1.0), (700, 160, 5, "softmax", True, 5, 3, 1, True, 1.0),
+    (800, 512, 8, "sigmoid", True, 8, 4, 2, True, 2.5), (300, 60, 6, "softmax", True, 5, 2, 2, True, 1.0), (200, 120, 4, "sigmoid", True, 3, 2, 2, True, 1.0), (200, 48, 3, "sigmoid", False, 4, 3, 2, False, 1.0),
+    (150, 384, 12, "sigmoid", True, 4, 2, 1, True, 1.0), (4, 3, 3, "sigmoid", False, 3, 3, 2, True, 1.0), (2, 2, 1, "sigmoid", True, 2, 1, 2, True, 1.0), (6, 65, 3, "softmax", True, 13, 4, 2, True, -1.0),
 ]
 
 
@@ -83,7 +85,7 @@ def test_gate_and_its_gradient(smoe, T, E, k, score, bias, groups, kept, best, r
 @pytest.mark.parametrize("score", ["softmax", "sigmoid"])
 @pytest.mark.parametrize("renormalise", [False, True])
 @pytest.mark.parametrize("bias", [False, True])
-@pytest.mark.parametrize("E,groups,kept,best", [(8, 1, 1, 1), (12, 4, 2, 2), (64, 8, 4, 2), (256, 8, 3, 1)])
+@pytest.mark.parametrize("E,groups,kept,best", [(8, 1, 1, 1), (12, 4, 2, 2), (60, 5, 3, 2), (64, 8, 4, 2), (256, 8, 3, 1), (480, 5, 2, 2)])
 def test_gate_of_masked_infinite_and_equal_logits(smoe, score, renormalise, bias, E, groups, kept, best):
     _log(f"gate edges {score} {renormalise} {bias} {E}")
     inf, nan, k = float("inf"), float("nan"), 3
@@ -141,6 +143,20 @@ def test_gate_gradient_of_repeated_and_foreign_experts(smoe):
             got = smoe.score_gate_bwd(x.cuda(), idx.cuda(), dw.cuda(), smoe.gate_rule(score, renormalise=renormalise))
             want = oracle.score_gate_bwd(_f64(x), idx.numpy(), _f64(dw), score, renormalise)
             _near(got, want, 100 * EPS32 * np.abs(_f64(dw)).sum(1, keepdims=True), f"{score} {renormalise}")
+
+
+@pytest.mark.parametrize("T,E,k", [(13, 64, 8), (6, 256, 4), (5, 300, 20), (9, 7, 3)])
+def test_gate_gradient_over_the_logits(smoe, T, E, k):
+    """dlogits may be the logits themselves (the C entry point)."""
+    import ctypes
+    for score in ("softmax", "sigmoid"):
+        for renormalise in (False, True):
+            x, dw = _normal((T, E), 12, torch.float32).cuda(), _normal((T, k), 13, torch.float32).cuda()
+            rule = smoe.gate_rule(score, renormalise=renormalise)
+            idx, _ = smoe.score_gate(x, k, rule)
+            want = smoe.score_gate_bwd(x, idx, dw, rule)
+            rc = smoe.lib.smoe_score_gate_bwd(smoe.ctx(), torch.cuda.current_stream().cuda_stream, x.data_ptr(), idx.data_ptr(), dw.data_ptr(), T, E, k, rule._c, x.data_ptr())
+            assert rc == 0 and torch.equal(x, want)
 
 
 # --------------------------------------------------------------------------------------------------------------- norm
