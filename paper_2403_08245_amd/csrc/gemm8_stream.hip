@@ -129,7 +129,8 @@ struct Reader8 {
   }
 };
 
-// The products of one half of a stage; behind(m) issues what goes behind fragment row m.
+// The products of one half of a stage; behind(i) issues what goes behind product i.  LDS reads and loads are spread one or two behind a product: in
+// bursts they queue up in front of the next product.
 template <bool FIRST, int HALF_, int FM, typename Behind>
 __device__ __forceinline__ void multiply8(const Frags8<FM> &f, const Exps8<FM> &x, f32x16 (&acc)[FM][FR], Behind behind) {
   f32x16 zero;
@@ -139,41 +140,59 @@ __device__ __forceinline__ void multiply8(const Frags8<FM> &f, const Exps8<FM> &
 #pragma unroll
   for (int m = 0; m < FM; ++m) {
 #pragma unroll
-    for (int n = 0; n < FR; ++n)
+    for (int n = 0; n < FR; ++n) {
       acc[m][n] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(f.b[n], f.a[m], FIRST ? zero : acc[m][n], 0, 0, 2 * HALF_, x.b[n], 2 * HALF_, x.a[m]);
-    behind(m);
-    sched_fence();
+      sched_fence();
+      behind(m * FR + n);
+      sched_fence();
+    }
   }
 }
+// part `i` of n things spread over the products from .. to: does it go behind product p?
+__device__ constexpr bool goes_behind(int i, int n, int p, int from, int to) {
+  const int at = from + i * (to - from) / n;
+  return at == p;
+}
 
-// One stage in slot `cur`, the next in `nxt`.  f[0] and x hold its first half and its powers of two on entry, the next stage's on exit.
+// One stage in slot `cur`, the next in `nxt`.  f[0] holds the columns and the first rows of its first half, x its powers of two on entry, and the next
+// stage's on exit.
 // STORES: at least that many stores were issued after the next stage's loads.
 template <bool FIRST, int STORES, typename S, typename Slot, typename Next>
 __device__ __forceinline__ void stage8(const Loader8<S> &ld, const Reader8 &rd, Frags8<S::FM> (&f)[2], Exps8<S::FM> &x, f32x16 (&acc)[S::FM][FR], const char *smem,
                                        uint32_t lds0, Slot cur, Next nxt) {
-  constexpr int FM = S::FM, PARTS = 2 * (FM + FR);
-  multiply8<FIRST, 0>(f[0], x, acc, [&](int m) {
-#pragma unroll
-    for (int i = 0; i < PARTS; ++i)
-      if (i >= m * PARTS / FM && i < (m + 1) * PARTS / FM) rd.template read<S>(f[1], i, smem, (int)cur, 1);
-  });
-  __syncthreads();      // every wavefront holds the stage: its slot is free
-  constexpr int EARLY = S::NL / FM;
-  Exps8<FM> y;
-  multiply8<false, 1>(f[1], x, acc, [&](int m) {
+  constexpr int FM = S::FM, P = FM * FR, PARTS = 2 * (FM + FR), HEAD = 2 * (FR + 1);
+  // Products 0 .. P - 1 are the first half's, P .. 2 P - 1 the second's.  The first half's further rows are read by TAIL (they are needed from product 4 on),
+  // the second half by FREE, behind which the slot is free; loads go behind the products to LOADED; the next stage is waited for behind
+  // LANDED.  8192 x 8192 x 8192, us, by FREE, LOADED, LANDED (of 16 + 16): 12, 29, 24 485; 11, 32, 26 488; 13, 28, 28 490; 15, 30, 22 496; 16, 28, 26 500 to 508.
+  constexpr int TAIL = P == 16 ? 3 : 2, FREE = P * 3 / 4, LOADED = P + P * 13 / 16, LANDED = P + P / 2;
+  auto load_at = [](int i) { return FREE + i * (LOADED - FREE) / S::NL; };
+  constexpr int EARLY = [] { int n = 0; for (int i = 0; i < S::NL; ++i) n += FREE + i * (LOADED - FREE) / S::NL <= LANDED; return n; }();
+  auto loads = [&](int p) {
 #pragma unroll
     for (int i = 0; i < S::NL; ++i)
-      if (i >= m * S::NL / FM && i < (m + 1) * S::NL / FM) ld.load(i, lds0, (int)cur);
-    if (m == 0) {       // the next stage has landed
+      if (load_at(i) == p) ld.load(i, lds0, (int)cur);
+  };
+  multiply8<FIRST, 0>(f[0], x, acc, [&](int p) {
+#pragma unroll
+    for (int i = HEAD; i < PARTS; ++i)
+      if (goes_behind(i - HEAD, PARTS - HEAD, p, 0, TAIL)) rd.template read<S>(f[0], i, smem, (int)cur, 0);
+#pragma unroll
+    for (int i = 0; i < PARTS; ++i)
+      if (goes_behind(i, PARTS, p, TAIL, FREE)) rd.template read<S>(f[1], i, smem, (int)cur, 1);
+    if (p == FREE) __syncthreads();      // every wavefront holds the stage: its slot is free
+    loads(p);
+  });
+  Exps8<FM> y;
+  multiply8<false, 1>(f[1], x, acc, [&](int p) {
+    loads(P + p);
+    if (P + p == LANDED) {
       wait_loads<(EARLY + STORES < 63 ? EARLY + STORES : 63)>();
       __syncthreads();
       rd.template read_exps<S>(y, smem, (int)nxt);
     }
-    if (m > 0 || FM == 1) {
 #pragma unroll
-      for (int i = 0; i < PARTS; ++i)
-        if (i >= (m - 1) * PARTS / (FM - 1) && i < m * PARTS / (FM - 1)) rd.template read<S>(f[0], i, smem, (int)nxt, 0);
-    }
+    for (int i = 0; i < HEAD; ++i)
+      if (goes_behind(i, HEAD, P + p, LANDED, 2 * P)) rd.template read<S>(f[0], i, smem, (int)nxt, 0);
   });
   rd.shift_exps(y);
   x = y;
@@ -374,7 +393,7 @@ __global__ void __launch_bounds__(NTHREADS, 1) s2s8_stream_kernel(S2S8Args a, in
   Frags8<S::FM> f[2];
   Exps8<S::FM> x;
 #pragma unroll
-  for (int i = 0; i < 2 * (S::FM + FR); ++i) rd.template read<S>(f[0], i, smem, 0, 0);
+  for (int i = 0; i < 2 * (FR + 1); ++i) rd.template read<S>(f[0], i, smem, 0, 0);
   rd.template read_exps<S>(x, smem, 0);
   rd.shift_exps(x);
 
