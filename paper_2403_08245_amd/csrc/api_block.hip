@@ -51,12 +51,35 @@ bool grid_fits(int Tk, int E, int d_out) { return ((long long)Tk / 32 + E) * (ce
 
 size_t weights8_size(int E, int d_in, int d_out, int halves) { return (size_t)E * groups8(d_out, halves) * ceil_div(d_in, ROW8) * 2048; }
 
+// Which kernels a product takes, by an estimate of their times in us (the rows of each expert are on the device: they are taken as even).  Fitted to 91
+// products, seven layers at 8 to 2000 rows an expert, each timed on all three kernels; what the rule picks takes 1.1 % more than the fastest on
+// average, 36 % at worst (32 experts of 300 rows, 1280 -> 1280: 39 us for 29).  Some of them, few rows / 128 x 256 / 256 x 256:
+//   64 experts, 2048 -> 1024: 8 rows 33 / 32 / 35, 32 rows 45 / 34 / 36, 200 rows 126 / 50 / 45, 2000 rows - / 350 / 287
+//   8 experts, 2816 -> 1024: 8 rows 9 / 26 / 32, 128 rows 21 / 25 / 35, 300 rows 36 / 27 / 36, 2000 rows - / 55 / 51
+//   16 experts, 2048 -> 1536: 8 rows 12 / 22 / 26, 64 rows 24 / 23 / 28, 200 rows 52 / 22 / 32, 1200 rows - / 80 / 63
+double few_rows_time(const S2S8Args &a) {
+  const double expert = (double)groups8(a.W.d_out, a.W.halves) * ceil_div(a.W.d_in, ROW8) * 2048e-6, used = a.Tk < a.W.E ? a.Tk : a.W.E;      // MB of weights
+  return 4.0 + (a.Tk / 32.0 + 0.5 * used) * expert / 8.2 + used * expert * 0.08;      // tiles of 32 rows read them from the caches, once from memory
+}
+double tiles_time(const S2S8Args &a, int rows, double stage, double lone_stage, double epilogue) {
+  const double used = a.Tk < a.W.E ? a.Tk : a.W.E, each = a.Tk / used / rows;
+  const double m_tiles = used * (each <= 0.8 ? 1.0 : each + 0.5), tiles = m_tiles * ceil_div(a.W.d_out, 256);
+  const double rounds = std::fmax(1.0, std::ceil(tiles / a.grid - 0.05)), steps = ceil_div(a.W.d_in, ROW8);
+  const double from_memory = m_tiles < 1.6 * used ? 1.6 * std::fmin(1.0, tiles / a.grid) : 0.0;      // a stage of weights that only this tile reads
+  if (a.act) epilogue *= 1.8;
+  return 4.5 + rounds * (steps * std::fmax(tiles > 128 ? stage : lone_stage, from_memory) + epilogue);
+}
 int product8(smoe_ctx *ctx, hipStream_t s, S2S8Args a) {
   a.grid = ctx->stream_grid;
   a.group_m = ctx->group_m;
   a.tile_shape = ctx->tile_shape;
-  const bool few = (long long)a.Tk <= 32LL * a.W.E && !a.tile_shape;
-  return few || ctx->kernel_mode || !s2s8_stream_supported(a) ? launch_s2s8_decode(s, a) : launch_s2s8_stream(s, a);
+  if (ctx->kernel_mode || !s2s8_stream_supported(a)) return launch_s2s8_decode(s, a);
+  if (!a.tile_shape) {
+    const double few = few_rows_time(a), half = tiles_time(a, 128, 1.03, 0.92, 3.0), big = tiles_time(a, 256, 1.58, 1.2, 4.5);
+    if (few <= half && few <= big) return launch_s2s8_decode(s, a);
+    a.tile_shape = half <= big ? 1 : 2;
+  }
+  return launch_s2s8_stream(s, a);
 }
 
 // Workspace of the MLP: hidden rows and their exponents, and the second product's rows [Tk, d_model] bf16 or fp32.

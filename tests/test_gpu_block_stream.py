@@ -103,8 +103,8 @@ def test_a_bad_row_stays_by_itself(smoe, shape):
 
 
 def test_few_rows_and_many_agree_where_the_rule_changes(smoe):
-    """32 rows per expert on average are the decoding kernels', one more the large tiles'."""
-    for T in (64, 65):
+    """Either side of sizes where the kernels change (64 rows an expert here, as estimated)."""
+    for T in (32, 64, 65, 130, 400):
         idx, gates, r, code, X, W1, W2, packed = _mlp_case(smoe, T, 256, 128, 4, 2, "swiglu", seed=71)
         rows, g = smoe.rows8_pack(X.cuda()), torch.from_numpy(gates).cuda()
         Y = smoe.mlp8_fwd(rows, *packed, r, 2, g, code)
