@@ -39,6 +39,25 @@ template <typename T, int V> struct Pack {
   }
 };
 
+// the same, kept as they come
+template <typename T, int V> struct Raw {
+  static constexpr int PER = V == 1 ? 1 : 16 / sizeof(T);
+  typedef T vec __attribute__((ext_vector_type(PER)));
+  vec v[V / PER];
+  __device__ __forceinline__ void load(const T *p) {
+#pragma unroll
+    for (int q = 0; q < V / PER; ++q) {
+      if constexpr (V == 1) v[q][0] = *p;
+      else v[q] = reinterpret_cast<const vec *>(p)[q];
+    }
+  }
+  __device__ __forceinline__ void clear() {
+#pragma unroll
+    for (int q = 0; q < V; ++q) v[q / PER][q % PER] = from_f32<T>(0.f);
+  }
+  __device__ __forceinline__ float get(int i) const { return to_f32<T>(v[i / PER][i % PER]); }
+};
+
 // sum over the TPR threads of a row, in all of them; `slot`: LDS of the row's wavefronts
 template <int TPR> __device__ __forceinline__ float row_sum(float v, float *slot) {
 #pragma unroll
@@ -131,11 +150,15 @@ __global__ void __launch_bounds__(TPR > 256 ? TPR : 256) norm_kernel(NormArgs a,
   }
 }
 
-// Gradient: block b takes rows b, b + gridDim.x, ... (ROWS of them at a time) and leaves its sum of dweight.
+// Gradient.  A block's rows (ROWS at a time, TPR threads each) lie gridDim.x * ROWS apart; the next ones are requested before the present ones' sum is
+// taken, so that HBM does not wait for it.  Up to 2048 elements a wavefront has a row to itself and no barrier stands in the loop (8192 rows of
+// 2048 in bf16, with the sum of the parts: 256 threads a row, nothing requested ahead, 45 us; so 30, 134 MB at 4.9 TB/s in the larger kernel).  A block leaves its sum of dweight.
 template <typename T, int V, int TPR, int NV>
 __global__ void __launch_bounds__(TPR > 256 ? TPR : 256) norm_bwd_kernel(NormBwdArgs a) {
   constexpr int ROWS = TPR > 256 ? 1 : 256 / TPR;
+  constexpr bool LEAN = TPR > 256;       // 128 registers a thread: neither the next row nor the weights are held
   __shared__ float s_sum[16];
+  __shared__ float s_dw[ROWS > 1 ? NV * TPR * V : 1];
   const int t = threadIdx.x % TPR, mine = threadIdx.x / TPR;
   Pack<T, V> w[NV];
   float dw[NV][V];
@@ -144,49 +167,95 @@ __global__ void __launch_bounds__(TPR > 256 ? TPR : 256) norm_bwd_kernel(NormBwd
     const int c = (i * TPR + t) * V;
 #pragma unroll
     for (int q = 0; q < V; ++q) dw[i][q] = w[i].v[q] = 0.f;
-    if (c < a.d) w[i].load((const T *)a.weight + c);
+    if (c < a.d && !LEAN) w[i].load((const T *)a.weight + c);
   }
-  for (long long row = (long long)blockIdx.x * ROWS + mine; row < a.rows; row += (long long)gridDim.x * ROWS) {
+  struct Row {
+    Raw<T, V> s[NV], dy[NV], ds[NV];
+    float rstd;
+  };
+  auto request = [&](long long row) {
+    Row r;
     const size_t at = (size_t)row * a.d;
-    const float rstd = a.rstd[row];
-    Pack<T, V> u[NV], g[NV];
-    float dot = 0.f;
+    r.rstd = a.rstd[row];
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
       const int c = (i * TPR + t) * V;
-#pragma unroll
-      for (int q = 0; q < V; ++q) u[i].v[q] = g[i].v[q] = 0.f;
       if (c < a.d) {
-        u[i].load((const T *)a.S + at + c);
-        g[i].load((const T *)a.dY + at + c);
-      }
-#pragma unroll
-      for (int q = 0; q < V; ++q) {
-        u[i].v[q] *= rstd;
-        dw[i][q] = fmaf(g[i].v[q], u[i].v[q], dw[i][q]);
-        g[i].v[q] *= w[i].v[q];
-        dot = fmaf(g[i].v[q], u[i].v[q], dot);
+        r.s[i].load((const T *)a.S + at + c);
+        r.dy[i].load((const T *)a.dY + at + c);
+        if (a.dS && !LEAN) r.ds[i].load((const T *)a.dS + at + c);
+      } else {
+        r.s[i].clear();
+        r.dy[i].clear();
       }
     }
-    const float mean = row_sum<TPR>(dot, s_sum) / (float)a.d;
+    return r;
+  };
+  const long long step = (long long)gridDim.x * ROWS;
+  long long row = (long long)blockIdx.x * ROWS + mine;
+  if (row < a.rows) {
+    Row now = request(row);
+    for (; row < a.rows; row += step) {
+      // dX may be dS, S or dY: the next row is another one, and each element is read before it is written by the thread that reads it
+      Row next;
+      if constexpr (!LEAN) next = request(row + step < a.rows ? row + step : row);
+      float u[NV][V], g[NV][V], dot = 0.f;
 #pragma unroll
-    for (int i = 0; i < NV; ++i) {
-      const int c = (i * TPR + t) * V;
-      if (c < a.d) {
-        Pack<T, V> o;
+      for (int i = 0; i < NV; ++i)
 #pragma unroll
-        for (int q = 0; q < V; ++q) o.v[q] = rstd * (g[i].v[q] - u[i].v[q] * mean);
-        if (a.dS) {
-          Pack<T, V> up;
-          up.load((const T *)a.dS + at + c);
-#pragma unroll
-          for (int q = 0; q < V; ++q) o.v[q] += up.v[q];
+        for (int q = 0; q < V; ++q) {
+          u[i][q] = now.s[i].get(q) * now.rstd;
+          g[i][q] = now.dy[i].get(q);
+          dw[i][q] = fmaf(g[i][q], u[i][q], dw[i][q]);
         }
-        o.store((T *)a.dX + at + c);
+#pragma unroll
+      for (int i = 0; i < NV; ++i) {
+        const int c = (i * TPR + t) * V;
+        if (LEAN && c < a.d) w[i].load((const T *)a.weight + c);
+#pragma unroll
+        for (int q = 0; q < V; ++q) {
+          g[i][q] *= w[i].v[q];
+          dot = fmaf(g[i][q], u[i][q], dot);
+        }
       }
+      const float mean = row_sum<TPR>(dot, s_sum) / (float)a.d;
+#pragma unroll
+      for (int i = 0; i < NV; ++i) {
+        const int c = (i * TPR + t) * V;
+        if (c < a.d) {
+          Pack<T, V> o;
+          if (LEAN && a.dS) now.ds[i].load((const T *)a.dS + (size_t)row * a.d + c);
+#pragma unroll
+          for (int q = 0; q < V; ++q) o.v[q] = now.rstd * (g[i][q] - u[i][q] * mean) + (a.dS ? now.ds[i].get(q) : 0.f);
+          o.store((T *)a.dX + (size_t)row * a.d + c);
+        }
+      }
+      if constexpr (!LEAN) now = next;
+      else if (row + step < a.rows) now = request(row + step);
     }
   }
-  float *part = a.part + ((size_t)blockIdx.x * ROWS + mine) * a.d;
+  // the block's sum, in the order of its wavefronts
+  if constexpr (ROWS > 1) {
+#pragma unroll
+    for (int m = 0; m < ROWS - 1; ++m) {
+      if (mine == m) {
+#pragma unroll
+        for (int i = 0; i < NV; ++i)
+#pragma unroll
+          for (int q = 0; q < V; ++q) s_dw[(i * V + q) * TPR + t] = dw[i][q];
+      }
+      __syncthreads();
+      if (mine == m + 1) {
+#pragma unroll
+        for (int i = 0; i < NV; ++i)
+#pragma unroll
+          for (int q = 0; q < V; ++q) dw[i][q] += s_dw[(i * V + q) * TPR + t];
+      }
+      __syncthreads();
+    }
+    if (mine != ROWS - 1) return;
+  }
+  float *part = a.part + (size_t)blockIdx.x * a.d;
 #pragma unroll
   for (int i = 0; i < NV; ++i) {
     const int c = (i * TPR + t) * V;
@@ -197,22 +266,24 @@ __global__ void __launch_bounds__(TPR > 256 ? TPR : 256) norm_bwd_kernel(NormBwd
   }
 }
 
-// dweight = the sum of the parts, in their order within 16 shares of them: 64 columns a block
+// dweight = the sum of the parts: 16 columns a block, each in 64 shares that are added in a fixed order
 template <typename T> __global__ void __launch_bounds__(1024) norm_dweight_kernel(const float *__restrict__ part, int parts, int d, T *__restrict__ dweight) {
-  __shared__ float s_part[16][64];
-  const int c = blockIdx.x * 64 + (threadIdx.x & 63), share = threadIdx.x >> 6;
+  __shared__ float s_part[64][16];
+  const int c = blockIdx.x * 16 + (threadIdx.x & 15), share = threadIdx.x >> 4;
   float sum = 0.f;
   if (c < d) {
 #pragma unroll 8
-    for (int p = share; p < parts; p += 16) sum += part[(size_t)p * d + c];
+    for (int p = share; p < parts; p += 64) sum += part[(size_t)p * d + c];
   }
-  s_part[share][threadIdx.x & 63] = sum;
+  s_part[share][threadIdx.x & 15] = sum;
   __syncthreads();
-  if (share == 0 && c < d) {
+  if (threadIdx.x >= 64) return;
+  sum = 0.f;
 #pragma unroll
-    for (int q = 1; q < 16; ++q) sum += s_part[q][threadIdx.x];
-    dweight[c] = from_f32<T>(sum);
-  }
+  for (int q = 0; q < 16; ++q) sum += s_part[(threadIdx.x >> 4) * 16 + q][threadIdx.x & 15];
+  sum += __shfl_xor(sum, 16, 64);
+  sum += __shfl_xor(sum, 32, 64);
+  if (threadIdx.x < 16 && c < d) dweight[c] = from_f32<T>(sum);
 }
 
 // The shape for rows of d elements: eight at a time where rows start on 16-byte lines, else one.
@@ -227,6 +298,7 @@ template <typename T, typename F> void by_shape(int d, F f) {
     else if (packs <= 256) go(v, integral_constant<int, 256>{}, integral_constant<int, 1>{});
     else if (packs <= 512) go(v, integral_constant<int, 256>{}, integral_constant<int, 2>{});
     else if (packs <= 1024) go(v, integral_constant<int, 256>{}, integral_constant<int, 4>{});
+    else if (packs <= 2048) go(v, integral_constant<int, 1024>{}, integral_constant<int, 2>{});
     else go(v, integral_constant<int, 1024>{}, integral_constant<int, 4>{});
   } else {
     integral_constant<int, 1> v;
@@ -234,7 +306,28 @@ template <typename T, typename F> void by_shape(int d, F f) {
     if (n <= 256) go(v, integral_constant<int, 64>{}, integral_constant<int, 4>{});
     else if (n <= 1024) go(v, integral_constant<int, 256>{}, integral_constant<int, 4>{});
     else if (n <= 4096) go(v, integral_constant<int, 256>{}, integral_constant<int, 16>{});
+    else if (n <= 8192) go(v, integral_constant<int, 1024>{}, integral_constant<int, 8>{});
+    else if (n <= 16384) go(v, integral_constant<int, 1024>{}, integral_constant<int, 16>{});
     else go(v, integral_constant<int, 1024>{}, integral_constant<int, 32>{});
+  }
+}
+// Of the gradient, whose registers hold two rows and the sums: a wavefront a row up to 2048 elements (1024 in ones).
+template <typename T, typename F> void by_bwd_shape(int d, F f) {
+  using std::integral_constant;
+  const int packs = ceil_div(pitch8(d), 8);
+  if (d % 8 == 0 && packs <= 256) {
+    integral_constant<int, 8> v;
+    integral_constant<int, 64> wave;
+    if (packs <= 64) f(v, wave, integral_constant<int, 1>{});
+    else if (packs <= 128) f(v, wave, integral_constant<int, 2>{});
+    else f(v, wave, integral_constant<int, 4>{});
+  } else if (d % 8 && d <= 1024) {
+    integral_constant<int, 1> v;
+    integral_constant<int, 64> wave;
+    if (d <= 256) f(v, wave, integral_constant<int, 4>{});
+    else f(v, wave, integral_constant<int, 16>{});
+  } else {
+    by_shape<T>(d, f);
   }
 }
 constexpr int BWD_BLOCKS = 512;
@@ -251,13 +344,13 @@ template <typename T> int launch_norm_as(hipStream_t s, const NormArgs &a) {
 template <typename T> int launch_norm_bwd_as(hipStream_t s, const NormBwdArgs &a) {
   const int parts = norm_bwd_parts(SMOE_BF16, a.rows, a.d);
   if (a.rows > 0) {
-    by_shape<T>(a.d, [&](auto v, auto tpr, auto nv) {
-      constexpr int TPR = decltype(tpr)::value, ROWS = TPR > 256 ? 1 : 256 / TPR;
-      hipLaunchKernelGGL((norm_bwd_kernel<T, decltype(v)::value, TPR, decltype(nv)::value>), dim3(parts / ROWS), dim3(TPR > 256 ? TPR : 256), 0, s, a);
+    by_bwd_shape<T>(a.d, [&](auto v, auto tpr, auto nv) {
+      constexpr int TPR = decltype(tpr)::value;
+      hipLaunchKernelGGL((norm_bwd_kernel<T, decltype(v)::value, TPR, decltype(nv)::value>), dim3(parts), dim3(TPR > 256 ? TPR : 256), 0, s, a);
     });
     SMOE_LAUNCH_CHECK();
   }
-  hipLaunchKernelGGL((norm_dweight_kernel<T>), dim3(ceil_div(a.d, 64)), dim3(1024), 0, s, a.part, a.rows > 0 ? parts : 0, a.d, (T *)a.dweight);
+  hipLaunchKernelGGL((norm_dweight_kernel<T>), dim3(ceil_div(a.d, 16)), dim3(1024), 0, s, a.part, a.rows > 0 ? parts : 0, a.d, (T *)a.dweight);
   SMOE_LAUNCH_CHECK();
   return SMOE_OK;
 }
@@ -267,9 +360,9 @@ template <typename T> int launch_norm_bwd_as(hipStream_t s, const NormBwdArgs &a
 int launch_norm(hipStream_t s, smoe_dtype dt, const NormArgs &a) { return dt == SMOE_BF16 ? launch_norm_as<bf16_t>(s, a) : launch_norm_as<float>(s, a); }
 int norm_bwd_parts(smoe_dtype, int rows, int d) {
   int per = 1;                   // rows a block has at a time
-  by_shape<float>(d, [&](auto, auto tpr, auto) { per = decltype(tpr)::value > 256 ? 1 : 256 / decltype(tpr)::value; });
+  by_bwd_shape<float>(d, [&](auto, auto tpr, auto) { per = decltype(tpr)::value > 256 ? 1 : 256 / decltype(tpr)::value; });
   const int blocks = ceil_div(rows, per);
-  return (blocks < BWD_BLOCKS ? blocks : BWD_BLOCKS) * per;
+  return blocks < BWD_BLOCKS ? blocks : BWD_BLOCKS;
 }
 int launch_norm_bwd(hipStream_t s, smoe_dtype dt, const NormBwdArgs &a) {
   return dt == SMOE_BF16 ? launch_norm_bwd_as<bf16_t>(s, a) : launch_norm_bwd_as<float>(s, a);

@@ -163,7 +163,7 @@ def test_gate_gradient_over_the_logits(smoe, T, E, k):
 # fp32 on the way: the sum of squares in a thread's up to 32 terms, 6 lane steps and up to 16 wavefronts (54 additions at most, half of which reach rstd, the sums
 # being of one sign), root, division and the products: 40 units.
 NORM_UNITS = 40 * EPS32
-NORMS = [(1, 1), (3, 7), (2, 128), (5, 512), (4, 520), (3, 999), (2, 1024), (7, 2048), (3, 4096), (2, 4100), (2, 8192), (1, 16384), (1, 32768), (2, 5001), (70, 40), (600, 264), (1030, 8)]
+NORMS = [(1, 1), (3, 7), (2, 128), (5, 512), (4, 520), (3, 999), (2, 1024), (7, 2048), (3, 4096), (2, 4100), (2, 8192), (1, 16384), (1, 32768), (2, 5001), (2, 10001), (1, 32767), (3, 20000), (70, 40), (600, 264), (1030, 8)]
 
 
 @pytest.mark.parametrize("rows,d", NORMS)
@@ -219,7 +219,7 @@ def _near_packed(smoe, rows, y, tol):
 
 
 def test_norm_in_place_of_its_inputs(smoe):
-    for rows, d, dtype in ((5, 264, torch.bfloat16), (3, 4096, torch.float32), (4, 77, torch.bfloat16), (2, 20000, torch.bfloat16)):
+    for rows, d, dtype in ((5, 9000, torch.float32), (5, 264, torch.bfloat16), (3, 4096, torch.float32), (4, 77, torch.bfloat16), (2, 20000, torch.bfloat16)):
         X, R, w = _normal((rows, d), 1, dtype).cuda(), _normal((rows, d), 2, dtype).cuda(), _normal((d,), 3, dtype).cuda()
         dY, dS = _normal((rows, d), 4, dtype).cuda(), _normal((rows, d), 5, dtype).cuda()
         want = smoe.add_norm_fwd(X, w, R)
