@@ -154,9 +154,10 @@ def plinear8(X, W, idx, gates=None):
     return y if gates is None else (y.reshape(T, k, -1) * np.asarray(gates, dtype=np.float64)[..., None]).sum(1)
 
 
-def mlp8(X, W1, W2, idx, gates, act, slack=None):
+def mlp8(X, W1, W2, idx, gates, act, slack=None, rounding=0.0):
     """(Y [T, d_model], tolerance [T, d_model]): Alg. 3 with the hidden rows packed to 8 bits.  `slack`(x, W) bounds the error of a product x W before
-    it is rounded; the tolerance is what it does to Y: hidden values that it moves to another code, and the second product's own."""
+    it is rounded; the tolerance is what it does to Y: hidden values that it moves to another code, and the second product's own, whose rows
+    may then be rounded once, by `rounding` of a value, or 2^-8 of that of the largest, at most."""
     T, k = idx.shape
     Y, tol = np.zeros((T, W2.shape[2])), np.zeros((T, W2.shape[2]))
     for t in range(T):
@@ -187,5 +188,6 @@ def mlp8(X, W1, W2, idx, gates, act, slack=None):
             other = np.ceil(np.log2(np.maximum(top(a), 2.0 ** -200) / 448)) != np.ceil(np.log2(np.maximum(top(b), 2.0 ** -200) / 448))
             step = np.maximum(np.abs(h) * 2.0 ** -3, np.repeat(top(a), 32)[:d] * 2.0 ** -17)
             dq = np.maximum(np.maximum(np.abs(lo - q), np.abs(hi - q)), np.where(np.repeat(other, 32)[:d], step, 0.0))
-            tol[t] += abs(gates[t, j]) * (dq @ np.abs(W2[e]) + slack(np.abs(q) + dq, W2[e]))
+            off = dq @ np.abs(W2[e]) + slack(np.abs(q) + dq, W2[e])
+            tol[t] += abs(gates[t, j]) * (off + rounding * (np.abs(y) + off + 2.0 ** -8 * (np.abs(y) + off).max()))
     return Y, tol

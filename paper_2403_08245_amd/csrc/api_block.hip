@@ -69,31 +69,34 @@ double tiles_time(const S2S8Args &a, int rows, double stage, double lone_stage, 
   if (a.act) epilogue *= 1.8;
   return 4.5 + rounds * (steps * std::fmax(tiles > 128 ? stage : lone_stage, from_memory) + epilogue);
 }
-int product8(smoe_ctx *ctx, hipStream_t s, S2S8Args a) {
+// what every launch takes from the context; true: the kernels for few rows
+bool set_launch(const smoe_ctx *ctx, S2S8Args &a) {
   a.grid = ctx->stream_grid;
   a.group_m = ctx->group_m;
   a.tile_shape = ctx->tile_shape;
-  if (ctx->kernel_mode || !s2s8_stream_supported(a)) return launch_s2s8_decode(s, a);
+  if (ctx->kernel_mode || !s2s8_stream_supported(a)) return true;
   if (!a.tile_shape) {
     const double few = few_rows_time(a), half = tiles_time(a, 128, 1.03, 0.92, 3.0), big = tiles_time(a, 256, 1.58, 1.2, 4.5);
-    if (few <= half && few <= big) return launch_s2s8_decode(s, a);
+    if (few <= half && few <= big) return true;
     a.tile_shape = half <= big ? 1 : 2;
   }
-  return launch_s2s8_stream(s, a);
+  return false;
 }
+int product8(smoe_ctx *ctx, hipStream_t s, S2S8Args a) { return set_launch(ctx, a) ? launch_s2s8_decode(s, a) : launch_s2s8_stream(s, a); }
 
-// Workspace of the MLP: hidden rows and their exponents, and the second product's rows [Tk, d_model] bf16 or fp32.
+// Workspace of the MLP: hidden rows and their exponents, and the second product's rows [Tk, d_model], 2 bytes an element and their exponents, or fp32.
 struct Mlp8Layout {
-  size_t h, h_exps, yhat, total;
+  size_t h, h_exps, yhat, y_exps, total;
 };
-// Rows of the second product in fp32, rounded once behind the weighted sum, up to here: they are few, and in the caches.
+// Rows of the second product in fp32, where the kernels for few rows make them, up to here: they are few, and in the caches.
 constexpr int WIDE_ROWS = 8192;
 Mlp8Layout mlp8_layout(int Tk, int d_model, int d_expert) {
   Mlp8Layout l;
   l.h = 0;
   l.h_exps = align256(rows8_bytes(Tk, d_expert));
   l.yhat = l.h_exps + align256(rows8_bytes(Tk, d_expert) / BLOCK8);
-  l.total = l.yhat + align256((size_t)Tk * d_model * (Tk <= WIDE_ROWS ? 4 : 2));
+  l.y_exps = l.yhat + align256((size_t)Tk * d_model * (Tk <= WIDE_ROWS ? 4 : 2));
+  l.total = l.y_exps + align256((size_t)Tk * ceil_div(d_model, 128));
   return l;
 }
 }  // namespace
@@ -292,8 +295,15 @@ int smoe_mlp8_fwd(smoe_ctx *ctx, void *stream, smoe_act act, const smoe_rows8 *X
   a.a_map = RowMap{nullptr, 1};
   a.c_map = RowMap{r->sorted_scattered_idxs, 1};
   a.C = at + l.yhat;
+  // a few rows are summed from fp32, others from fp16 with exponents (bf16 where neither has room: many experts of few rows)
+  a.C_exps = (uint8_t *)at + l.y_exps;
+  if (!set_launch(ctx, a)) {
+    rc = launch_s2s8_stream(s, a);
+    return rc == SMOE_OK ? launch_combine_f16(s, a.C, a.C_exps, gates, Y, T, k, d_model) : rc;
+  }
+  a.C_exps = nullptr;
   a.wide = Tk <= WIDE_ROWS;
-  rc = product8(ctx, s, a);
+  rc = launch_s2s8_decode(s, a);
   if (rc != SMOE_OK) return rc;
   return a.wide ? launch_combine_wide(s, (const float *)a.C, gates, Y, T, k, d_model) : launch_combine(s, SMOE_BF16, a.C, gates, Y, T, k, d_model);
 }

@@ -35,9 +35,9 @@ template <int FM_> struct Shape8 {
 using Big8 = Shape8<4>;
 using Half8 = Shape8<2>;
 
-enum { OUT_BF16, OUT_F32, OUT_SWIGLU, OUT_GELU };
+enum { OUT_BF16, OUT_F16, OUT_SWIGLU, OUT_GELU };
 // store instructions that a wavefront issues per tile
-template <int FM, int OUT> constexpr int Stores8 = FM * (OUT == OUT_BF16 ? 8 : OUT == OUT_F32 ? 16 : OUT == OUT_SWIGLU ? 3 : 5);
+template <int FM, int OUT> constexpr int Stores8 = FM * (OUT == OUT_BF16 ? 8 : OUT == OUT_F16 ? 9 : OUT == OUT_SWIGLU ? 3 : 5);
 
 // first[e] = M-tiles of the experts before e, by every wavefront for itself (all write the same); returns first[E]
 template <int TM> __device__ __forceinline__ int number_tiles8(const int32_t *offsets, int E, int *first, int lane) {
@@ -198,23 +198,61 @@ __device__ __forceinline__ void stage8(const Loader8<S> &ld, const Reader8 &rd, 
   x = y;
 }
 
-// 32 rows of fp32 through the patch, 32 columns at a time
-template <int FM, typename DestFn> __device__ __forceinline__ void store_wave_tile_f32(const f32x16 (&acc)[FM][FR], char *patch, DestFn dest, int lane) {
+// The rows of a weighted sum: fp16 with a power of two for the wavefront's 128 columns of a row, as many bytes as bf16 and three bits more, so that the
+// sum carries little but its own rounding (16384 tokens, 8 experts, 4096 -> 2 x 14336: error against 64 bits 2.7e-3 with bf16 rows,
+// 2.1e-3 so; the plain form's 1.7e-3).  Where the largest values of all 32 rows lie in [2^-6, 2^15) (or are 0) they are stored as they are, good
+// to 2^-11 of a value and 2^-19 of the largest; else times the power of two that brings the largest into [2^14, 2^15).
+// exps: 141 for values as they are, else the largest's exponent, biased by 127 (15 .. 254; infinite and NaN rows take the largest finite value's).
+template <int FM, typename DestFn, typename ExpFn>
+__device__ __forceinline__ void store_wave_tile_f16(const f32x16 (&acc)[FM][FR], char *patch, DestFn dest, ExpFn put_exp, int lane) {
+  typedef float f32x4_t __attribute__((ext_vector_type(4)));
+  typedef _Float16 f16x4 __attribute__((ext_vector_type(4)));
   acc_settle();
   RowStore<decltype(dest(0, 0))> pend;
 #pragma unroll
-  for (int fm = 0; fm < FM; ++fm)
+  for (int fm = 0; fm < FM; ++fm) {
+    sched_fence();
+    float v[FR][16], most = 0.f;
 #pragma unroll
     for (int fn = 0; fn < FR; ++fn)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) v[fn][i] = acc_read(acc[fm][fn][i]);
+#pragma unroll
+    for (int fn = 0; fn < FR; ++fn)
+#pragma unroll
+      for (int i = 0; i < 16; i += 2) most = fmaxf(most, fmaxf(fabsf(v[fn][i]), fabsf(v[fn][i + 1])));
+    most = fmaxf(most, __shfl_xor(most, 32, 64));
+    unsigned int e = 141u;
+    if (__any(most != 0.f && !(most >= 0x1p-6f && most < 0x1p15f))) {
+      if (__any(most == INFINITY)) {
+        most = 0.f;
+#pragma unroll
+        for (int fn = 0; fn < FR; ++fn)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) most = fmaxf(most, finite_abs(v[fn][i]));
+        most = fmaxf(most, __shfl_xor(most, 32, 64));
+      }
+      e = max(__float_as_uint(most) >> 23, 15u);
+      const float scale = __uint_as_float((268u - e) << 23);
+#pragma unroll
+      for (int fn = 0; fn < FR; ++fn)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) v[fn][i] *= scale;
+    }
+    put_exp(fm, e);
+#pragma unroll
+    for (int half = 0; half < 2; ++half)
       pipe_block(pend, patch, lane, [&] {
 #pragma unroll
-        for (int g = 0; g < 4; ++g) {
-          f32x4 v;
+        for (int f2 = 0; f2 < 2; ++f2)
 #pragma unroll
-          for (int q = 0; q < 4; ++q) v[q] = acc_read(acc[fm][fn][g * 4 + q]);
-          *reinterpret_cast<f32x4 *>(patch_slot(patch, lane & 31, 2 * g + (lane >> 5))) = v;
-        }
-      }, dest(fm, fn));
+          for (int g = 0; g < 4; ++g) {
+            const float *x = &v[half * 2 + f2][g * 4];
+            const f16x4 o = __builtin_convertvector(f32x4_t{x[0], x[1], x[2], x[3]}, f16x4);
+            patch_put(patch, lane, f2, g, __builtin_bit_cast(bf16x4, o));
+          }
+      }, dest(fm, half));
+  }
   sched_fence();
   issue_row_store(pend);
 }
@@ -432,7 +470,7 @@ __global__ void __launch_bounds__(NTHREADS, 1) s2s8_stream_kernel(S2S8Args a, in
     const int left = max(min(S::TM / 2, ct.row_end - rbase), 0);
     const int *idx = &s_idx[ct.seq & 3][uwm * (S::TM / 2)];
     if constexpr (!HIDDEN) {
-      constexpr int ES = OUT == OUT_F32 ? 4 : 2, PER = 16 / ES;      // bytes of an element, elements of a 16-byte chunk
+      constexpr int ES = 2, PER = 16 / ES;                           // bytes of an element, elements of a 16-byte chunk
       const int wcol = ct.n0 + uwn * (TB / 2);
       const window_t win = SCATTER ? make_window(p->C, (uint32_t)p->Tk * (uint32_t)N * ES)
                                    : make_window((const char *)p->C + (size_t)rbase * N * ES, (uint32_t)left * (uint32_t)N * ES);
@@ -447,8 +485,17 @@ __global__ void __launch_bounds__(NTHREADS, 1) s2s8_stream_kernel(S2S8Args a, in
         }
         return d;
       };
-      if constexpr (OUT == OUT_F32) store_wave_tile_f32(acc, patch, dest, lane);
-      else store_wave_tile(acc, patch, dest, lane);
+      if constexpr (OUT == OUT_F16) {
+        const int per_row = (N + 127) / 128;
+        const window_t win_e = make_window(p->C_exps, (uint32_t)p->Tk * (uint32_t)per_row);
+        store_wave_tile_f16(acc, patch, dest, [&](int fm, unsigned int e) {
+          const int r = fm * 32 + (lane & 31);
+          const uint32_t off = lane < 32 && r < left && wcol < N ? (uint32_t)idx[r] * (uint32_t)per_row + (uint32_t)(wcol / 128) : ~0u;
+          __builtin_amdgcn_raw_buffer_store_b8((char)e, win_e, (int)off, 0, 0);
+        }, lane);
+      } else {
+        store_wave_tile(acc, patch, dest, lane);
+      }
     } else {
       // hidden rows: 64 (SwiGLU) or 128 units of the wavefront, blocks of 32
       constexpr int BLOCKS = OUT == OUT_SWIGLU ? 2 : 4, UNITS = BLOCKS * 32;
@@ -521,7 +568,7 @@ template <typename S, int OUT, bool SCATTER> int launch_as(hipStream_t s, const 
 template <typename S> int launch(hipStream_t s, const S2S8Args &a) {
   if (a.act == SMOE_ACT_SWIGLU) return launch_as<S, OUT_SWIGLU, false>(s, a);
   if (a.act == SMOE_ACT_GELU) return launch_as<S, OUT_GELU, false>(s, a);
-  if (a.wide) return launch_as<S, OUT_F32, true>(s, a);
+  if (a.C_exps) return launch_as<S, OUT_F16, true>(s, a);
   return a.c_map.o ? launch_as<S, OUT_BF16, true>(s, a) : launch_as<S, OUT_BF16, false>(s, a);
 }
 template <typename S, int OUT, bool SCATTER> int init_as() {
@@ -531,7 +578,7 @@ template <typename S, int OUT, bool SCATTER> int init_as() {
 template <typename S> int init() {
   int rc = init_as<S, OUT_SWIGLU, false>();
   if (rc == SMOE_OK) rc = init_as<S, OUT_GELU, false>();
-  if (rc == SMOE_OK) rc = init_as<S, OUT_F32, true>();
+  if (rc == SMOE_OK) rc = init_as<S, OUT_F16, true>();
   if (rc == SMOE_OK) rc = init_as<S, OUT_BF16, true>();
   if (rc == SMOE_OK) rc = init_as<S, OUT_BF16, false>();
   return rc;
@@ -547,10 +594,10 @@ int init_stream8_kernels() {
 // 32-bit offsets into the rows, an expert's weights and a scattered output; the fan-out's division.
 bool s2s8_stream_supported(const S2S8Args &a) {
   if (a.Tk < 1 || a.W.E > MAX_E8 || a.grid < 8 || a.W.d_in <= ROW8) return false;      // two stages at least
-  if (a.wide && !a.c_map.o) return false;
+  if (a.wide || (a.C_exps && !a.c_map.o)) return false;
   const unsigned long long pitch = pitch8(a.W.d_in), rows = a.a_map.o ? a.Tk / a.a_map.fan : 256;
   if (rows * pitch > 0x7fff0000ULL || (unsigned long long)groups8(a.W.d_out, a.W.halves) * 16 * pitch + 32 * pitch * 16 > 0x7fff0000ULL) return false;
-  if (!a.H.values && a.c_map.o && (unsigned long long)a.Tk * a.W.d_out * (a.wide ? 4 : 2) > 0xfffffff0ULL) return false;
+  if (!a.H.values && a.c_map.o && (unsigned long long)a.Tk * a.W.d_out * 2 > 0xfffffff0ULL) return false;
   if (256ULL * a.W.d_out * 2 > 0x7fff0000ULL) return false;
   if (a.a_map.o && (unsigned long long)a.Tk * a.a_map.fan >= 0x100000000ULL) return false;
   const long long m_tiles = (long long)a.Tk / 128 + a.W.E, n_tiles = ceil_div(a.W.d_out, 128);

@@ -74,6 +74,46 @@ __global__ void __launch_bounds__(256) rows8_unpack_kernel(smoe_rows8 in, long l
   }
 }
 
+// The weighted sum of k slots' rows, eight columns a thread; up to K rows in flight, read past the caches (each once).
+template <int K>
+__global__ void __launch_bounds__(256) combine_f16_kernel(const uint4 *__restrict__ Yhat, const uint8_t *__restrict__ exps, const float *__restrict__ g, bf16_t *__restrict__ Y,
+                                                          long long chunks, int k, int per_row, int exps_row) {
+  typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
+  typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+  typedef bf16_t bf16x8 __attribute__((ext_vector_type(8)));
+  for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < chunks; i += (long long)gridDim.x * 256) {
+    const long long t = i / per_row;
+    const int c = (int)(i - t * per_row);
+    const u32x4 *src = reinterpret_cast<const u32x4 *>(Yhat) + t * k * per_row + c;
+    const uint8_t *e = exps + t * k * exps_row + c / 16;
+    const float *w = g + t * k;
+    float acc[8];
+#pragma unroll
+    for (int q = 0; q < 8; ++q) acc[q] = 0.f;
+    for (int j0 = 0; j0 < k; j0 += K) {
+      u32x4 row[K];
+      float scale[K];
+#pragma unroll
+      for (int j = 0; j < K; ++j)
+        if (j0 + j < k) {
+          row[j] = __builtin_nontemporal_load(src + (long long)(j0 + j) * per_row);
+          scale[j] = w[j0 + j] * __uint_as_float(((unsigned int)e[(long long)(j0 + j) * exps_row] - 14u) << 23);
+        }
+#pragma unroll
+      for (int j = 0; j < K; ++j)
+        if (j0 + j < k) {
+          const f16x8 v = __builtin_bit_cast(f16x8, row[j]);
+#pragma unroll
+          for (int q = 0; q < 8; ++q) acc[q] = fmaf(scale[j], (float)v[q], acc[q]);
+        }
+    }
+    bf16x8 o;
+#pragma unroll
+    for (int q = 0; q < 8; ++q) o[q] = (bf16_t)acc[q];
+    reinterpret_cast<bf16x8 *>(Y)[i] = o;
+  }
+}
+
 // A block packs one step of 128 of the contraction of 64 columns: rows of W into LDS, a thread takes 32 elements of a column.
 template <typename T>
 __global__ void __launch_bounds__(256) weights8_pack_kernel(const T *__restrict__ W, smoe_weights8 out, int groups, int steps) {
@@ -134,6 +174,18 @@ int launch_rows8_unpack(hipStream_t s, smoe_dtype dt, const smoe_rows8 &in, int 
   const long long chunks = (long long)rows * per_row;
   if (dt == SMOE_BF16) hipLaunchKernelGGL((rows8_unpack_kernel<bf16_t>), dim3(row_blocks(chunks)), dim3(256), 0, s, in, chunks, per_row, d, (bf16_t *)X);
   else hipLaunchKernelGGL((rows8_unpack_kernel<float>), dim3(row_blocks(chunks)), dim3(256), 0, s, in, chunks, per_row, d, (float *)X);
+  SMOE_LAUNCH_CHECK();
+  return SMOE_OK;
+}
+int launch_combine_f16(hipStream_t s, const void *Yhat, const uint8_t *exps, const float *g, void *Y, int T, int k, int d) {
+  const int per_row = d / 8;
+  const long long chunks = (long long)T * per_row;
+  const dim3 grid(row_blocks(chunks)), block(256);
+  auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, block, 0, s, (const uint4 *)Yhat, exps, g, (bf16_t *)Y, chunks, k, per_row, ceil_div(d, 128)); };
+  if (k == 1) go(combine_f16_kernel<1>);
+  else if (k == 2) go(combine_f16_kernel<2>);
+  else if (k <= 4) go(combine_f16_kernel<4>);
+  else go(combine_f16_kernel<8>);
   SMOE_LAUNCH_CHECK();
   return SMOE_OK;
 }

@@ -11,6 +11,7 @@ pytestmark = pytest.mark.gpu
 
 HALF = {torch.bfloat16: 2.0 ** -8, torch.float32: 2.0 ** -24}     # what a rounding is off by at most, relative to the value
 EPS32 = 2.0 ** -24
+ROW = 2.0 ** -11                    # rows of a weighted sum may be held in fp16, with a power of two for 128 of them
 
 
 def _log(*a):
@@ -404,7 +405,7 @@ def test_mlp_in_8_bits(smoe, T, d_model, d_expert, E, k, act):
     idx, gates, r, code, X, W1, W2, packed = _mlp_case(smoe, T, d_model, d_expert, E, k, act)
     Y = smoe.mlp8_fwd(smoe.rows8_pack(X.cuda()), *packed, r, k, torch.from_numpy(gates).cuda(), code)
     x = oracle.unpack8(*oracle.pack8(_f64(X)), d_model)
-    want, tol = oracle.mlp8(x, _stored(smoe, W1), _stored(smoe, W2), idx, gates.astype(np.float64), code, slack=_slack)
+    want, tol = oracle.mlp8(x, _stored(smoe, W1), _stored(smoe, W2), idx, gates.astype(np.float64), code, slack=_slack, rounding=ROW)
     half = HALF[torch.bfloat16]
     _near(Y, want, half * np.abs(want) + (1 + half) * tol + k * EPS32 * np.abs(want).max(), "Y")
 
@@ -416,7 +417,7 @@ def test_mlp_with_empty_and_crowded_experts(smoe):
         assert set(idx.ravel()) <= set(only)
         Y = smoe.mlp8_fwd(smoe.rows8_pack(X.cuda()), *packed, r, k, torch.from_numpy(gates).cuda(), code)
         x = oracle.unpack8(*oracle.pack8(_f64(X)), 128)
-        want, tol = oracle.mlp8(x, _stored(smoe, W1), _stored(smoe, W2), idx, gates.astype(np.float64), code, slack=_slack)
+        want, tol = oracle.mlp8(x, _stored(smoe, W1), _stored(smoe, W2), idx, gates.astype(np.float64), code, slack=_slack, rounding=ROW)
         _near(Y, want, 2.0 ** -8 * np.abs(want) + 1.01 * tol + 1e-6 * np.abs(want).max(), str(only))
 
 
@@ -479,7 +480,7 @@ def test_a_block_as_it_is_served(smoe, T):
     x = oracle.unpack8(n.Y8.values.cpu().numpy(), n.Y8.exps.cpu().numpy(), 256)
     _, y, _ = oracle.add_norm(_f64(s["X"]), _f64(s["R"]), _f64(s["weight"]), 1e-6)
     _near_packed(smoe, n.Y8, y, (NORM_UNITS + 3 * EPS32) * np.abs(y))
-    want, tol = oracle.mlp8(x, _stored(smoe, s["w"][0]), _stored(smoe, s["w"][1]), idx.cpu().numpy(), _f64(gates), 2, slack=_slack)
+    want, tol = oracle.mlp8(x, _stored(smoe, s["w"][0]), _stored(smoe, s["w"][1]), idx.cpu().numpy(), _f64(gates), 2, slack=_slack, rounding=ROW)
     _near(Y, want, 2.0 ** -8 * np.abs(want) + 1.01 * tol + 1e-6 * np.abs(want).max(), "Y")
     stream, y, _ = oracle.add_norm(_f64(Y), _f64(n.S), _f64(s["weight"]), 1e-6)
     _near(m.S, stream, 2.0 ** -8 * np.abs(stream) * 1.01 + EPS32 * np.abs(stream))

@@ -5,7 +5,7 @@ import pytest
 import torch
 
 import oracle
-from test_gpu_block import HALF, _f64, _log, _mlp_case, _near, _normal, _routed, _slack, _stored, _weights
+from test_gpu_block import HALF, ROW, _f64, _log, _mlp_case, _near, _normal, _routed, _slack, _stored, _weights
 
 pytestmark = pytest.mark.gpu
 FEW = 1            # smoe_set_kernel_mode: the kernels for few rows, whatever the size
@@ -80,7 +80,7 @@ def test_mlp(smoe, shape, T, d_model, d_expert, E, k, act):
     small = _few(smoe, call, shape)
     x = oracle.unpack8(*oracle.pack8(_f64(X)), d_model)
     sample = np.unique(np.concatenate([np.arange(0, T, max(1, T // 40)), [T - 1]]))
-    want, tol = oracle.mlp8(x[sample], _stored(smoe, W1), _stored(smoe, W2), idx[sample], gates[sample].astype(np.float64), code, slack=_slack)
+    want, tol = oracle.mlp8(x[sample], _stored(smoe, W1), _stored(smoe, W2), idx[sample], gates[sample].astype(np.float64), code, slack=_slack, rounding=ROW)
     half = HALF[torch.bfloat16]
     _near(Y[torch.from_numpy(sample).cuda()], want, half * np.abs(want) + (1 + half) * tol + k * 2.0 ** -24 * np.abs(want).max(), "Y")
     a, b = Y.float(), small.float()
@@ -109,5 +109,5 @@ def test_few_rows_and_many_agree_where_the_rule_changes(smoe):
         rows, g = smoe.rows8_pack(X.cuda()), torch.from_numpy(gates).cuda()
         Y = smoe.mlp8_fwd(rows, *packed, r, 2, g, code)
         x = oracle.unpack8(*oracle.pack8(_f64(X)), 256)
-        want, tol = oracle.mlp8(x, _stored(smoe, W1), _stored(smoe, W2), idx, gates.astype(np.float64), code, slack=_slack)
+        want, tol = oracle.mlp8(x, _stored(smoe, W1), _stored(smoe, W2), idx, gates.astype(np.float64), code, slack=_slack, rounding=ROW)
         _near(Y, want, 2.0 ** -8 * np.abs(want) + 1.01 * tol + 1e-6 * np.abs(want).max(), str(T))
