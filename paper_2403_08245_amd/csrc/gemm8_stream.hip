@@ -22,8 +22,9 @@ typedef float f32x4 __attribute__((ext_vector_type(4)));
 constexpr int B8_BYTES = TB * ROW8;                     // weights of a stage, 256 columns
 constexpr int MAX_E8 = 256;
 
-template <int FM_> struct Shape8 {
+template <int FM_, bool ONCE_ = false> struct Shape8 {
   static constexpr int FM = FM_;                        // 32-row fragments per wavefront
+  static constexpr bool ONCE = ONCE_;                   // weights that no further tile reads pass the caches
   static constexpr int TM = FM * 64;                    // tile rows; columns are TB = 256
   static constexpr int A_BYTES = TM * ROW8;
   static constexpr int NLA = A_BYTES / 4096, NLB = B8_BYTES / 4096;   // load instructions per wavefront and stage
@@ -34,6 +35,7 @@ template <int FM_> struct Shape8 {
 };
 using Big8 = Shape8<4>;
 using Half8 = Shape8<2>;
+using Half8Once = Shape8<2, true>;
 
 enum { OUT_BF16, OUT_F16, OUT_SWIGLU, OUT_GELU };
 // store instructions that a wavefront issues per tile
@@ -75,13 +77,16 @@ template <typename S> struct Loader8 {
   uint32_t oa[S::NLA], oea, ob, oeb;
   uint32_t group_bytes;              // of a group of 16 columns: steps * 2048
   int step, uwave;
+  int again;                         // S::ONCE: above 0 where the expert has further tiles
   __device__ __forceinline__ void load(int I, uint32_t lds0, int slot) const {
     if (I < S::NLA) {
       load16_to_lds_checked(win_a, oa[I] + (uint32_t)step * ROW8, lds0 + slot * S::A_BYTES + uwave * (S::NLA * 1024), I * 1024);
     } else if (I < S::NLA + S::NLB) {
       const int J = I - S::NLA;
-      load16_to_lds_checked(win_b, ob + ((uint32_t)(J >> 1) * group_bytes + (uint32_t)step * 2048u + (uint32_t)(J & 1) * 1024u),
-                            lds0 + S::OFF_B + slot * B8_BYTES + uwave * (S::NLB * 1024), J * 1024);
+      const uint32_t off = ob + ((uint32_t)(J >> 1) * group_bytes + (uint32_t)step * 2048u + (uint32_t)(J & 1) * 1024u);
+      const uint32_t lds = lds0 + S::OFF_B + slot * B8_BYTES + uwave * (S::NLB * 1024);
+      if (S::ONCE) load16_to_lds_checked_or_once(win_b, off, lds + J * 1024, again);
+      else load16_to_lds_checked(win_b, off, lds, J * 1024);
     } else if (I == S::NLA + S::NLB) {
       load4_to_lds_checked(win_ea, oea + (uint32_t)step * 4u, lds0 + S::OFF_EA + slot * (S::TM * 4) + (uwave & (S::TM / 64 - 1)) * 256);
     } else {
@@ -373,6 +378,7 @@ __global__ void __launch_bounds__(NTHREADS, 1) s2s8_stream_kernel(S2S8Args a, in
     const uint32_t per_expert = (uint32_t)(p->W.halves * 2 * ((p->W.d_out / p->W.halves + 31) / 32)) * ld.group_bytes;
     ld.win_b = buffer_window(p->W.values + (size_t)t.e * per_expert, per_expert);
     ld.win_eb = buffer_window(p->W.exps + (size_t)t.e * (per_expert / BLOCK8), per_expert / BLOCK8);
+    if (S::ONCE) ld.again = t.row_end - __builtin_amdgcn_readfirstlane(s_off[t.e]) - S::TM;
     const int *idx = &s_idx[t.seq & 3][0];
     // rows past the segment read zeros: an offset outside the window at every stage
     const uint32_t past = 0x80000000u;
@@ -588,7 +594,9 @@ template <typename S> int init() {
 
 int init_stream8_kernels() {
   const int rc = init<Big8>();
-  return rc == SMOE_OK ? init<Half8>() : rc;
+  if (rc != SMOE_OK) return rc;
+  const int half = init<Half8>();
+  return half == SMOE_OK ? init<Half8Once>() : half;
 }
 
 // 32-bit offsets into the rows, an expert's weights and a scattered output; the fan-out's division.
@@ -605,5 +613,8 @@ bool s2s8_stream_supported(const S2S8Args &a) {
 }
 int launch_s2s8_stream(hipStream_t s, const S2S8Args &a) {
   if (!s2s8_stream_supported(a)) return SMOE_ERR_UNSUPPORTED;
-  return a.tile_shape == 1 ? launch<Half8>(s, a) : launch<Big8>(s, a);
+  if (a.tile_shape != 1) return launch<Big8>(s, a);
+  // see launch_as in gemm8_decode.hip; with a tile an expert on average the weights are read about once
+  const bool once = a.call_weights > LAST_LEVEL_CACHE / 2 && (long long)a.Tk <= 128LL * a.W.E;
+  return once ? launch<Half8Once>(s, a) : launch<Half8>(s, a);
 }

@@ -111,3 +111,43 @@ def test_few_rows_and_many_agree_where_the_rule_changes(smoe):
         x = oracle.unpack8(*oracle.pack8(_f64(X)), 256)
         want, tol = oracle.mlp8(x, _stored(smoe, W1), _stored(smoe, W2), idx, gates.astype(np.float64), code, slack=_slack, rounding=ROW)
         _near(Y, want, 2.0 ** -8 * np.abs(want) + 1.01 * tol + 1e-6 * np.abs(want).max(), str(T))
+
+
+@pytest.mark.parametrize("act", ["swiglu", "gelu"])
+def test_rows_of_all_sizes(smoe, shape, act):
+    """Rows from 2^-60 to 2^30: hidden rows and rows of the weighted sum far from 1, in one tile."""
+    T, k = 300, 2
+    idx, gates, r, code, X, W1, W2, packed = _mlp_case(smoe, T, 256, 320, 3, k, act, seed=81)
+    X = (X.float() * 2.0 ** torch.linspace(-60, 30, T).round()[:, None]).to(torch.bfloat16)
+    Y = smoe.mlp8_fwd(smoe.rows8_pack(X.cuda()), *packed, r, k, torch.from_numpy(gates).cuda(), code)
+    x = oracle.unpack8(*oracle.pack8(_f64(X)), 256)
+    with np.errstate(over="ignore"):
+        want, tol = oracle.mlp8(x, _stored(smoe, W1), _stored(smoe, W2), idx, gates.astype(np.float64), code, slack=_slack, rounding=ROW)
+    half = HALF[torch.bfloat16]
+    _near(Y, want, half * np.abs(want) + (1 + half) * tol + k * 2.0 ** -24 * np.abs(want).max(1, keepdims=True) * 2, "Y")
+
+
+def test_weights_past_the_caches(smoe):
+    """Weights over half of the last-level cache (128 MB) are read past it by tiles that are their expert's only one: experts with one tile, with several and with none."""
+    E, d, N, k = 66, 1024, 2048, 1
+    logits = torch.zeros(3000, E)
+    pick = torch.cat([torch.zeros(400), torch.ones(128), torch.full((129,), 2), torch.randint(3, 60, (2343,), generator=torch.Generator().manual_seed(1)).float()]).long()
+    logits[torch.arange(3000), pick] = 5.0
+    idx, _ = oracle.score_gate(_f64(logits), k)
+    r = smoe.route(torch.from_numpy(idx).cuda(), E)
+    X, W = _normal((3000, d), 2), _weights((E, d, N), 3)
+    packed = smoe.weights8(W.cuda())
+    assert packed.values.numel() > 128 << 20
+    rows = smoe.rows8_pack(X.cuda())
+    smoe.set_kernel_mode(3)
+    try:
+        Y = smoe.plinear8_fwd(rows, packed, r, k)[0]
+    finally:
+        smoe.set_kernel_mode(0)
+    x = oracle.unpack8(*oracle.pack8(_f64(X)), d)
+    for t in (0, 5, 399, 400, 527, 528, 656, 657, 1500, 2999):
+        w = oracle.unpack8(*oracle.pack8(_f64(W[idx[t, 0]]).T), d).T
+        want = x[t] @ w
+        _near(Y[t], want, 2.0 ** -8 * np.abs(want) + 1.01 * _slack(x[t], w), str(t))
+    few = _few(smoe, lambda: smoe.plinear8_fwd(rows, packed, r, k)[0], 0).float()
+    assert ((Y.float() - few).abs() <= 2.0 ** -6 * few.abs() + 0.05).all()
