@@ -64,7 +64,7 @@ double few_rows_time(const S2S8Args &a) {
 double tiles_time(const S2S8Args &a, int rows, double stage, double lone_stage, double epilogue) {
   const double used = a.Tk < a.W.E ? a.Tk : a.W.E, each = a.Tk / used / rows;
   const double m_tiles = used * (each <= 0.8 ? 1.0 : each + 0.5), tiles = m_tiles * ceil_div(a.W.d_out, 256);
-  const double rounds = std::fmax(1.0, std::ceil(tiles / a.grid - 0.05)), steps = ceil_div(a.W.d_in, ROW8);
+  const double rounds = std::fmax(1.0, std::ceil(tiles / a.grid - 0.05)), steps = a.W.d_in <= ROW8 ? 2 : ceil_div(a.W.d_in, ROW8);
   const double from_memory = m_tiles < 1.6 * used ? 1.6 * std::fmin(1.0, tiles / a.grid) : 0.0;      // a stage of weights that only this tile reads
   if (a.act) epilogue *= 1.8;
   return 4.5 + rounds * (steps * std::fmax(tiles > 128 ? stage : lone_stage, from_memory) + epilogue);

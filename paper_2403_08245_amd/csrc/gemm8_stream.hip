@@ -76,21 +76,22 @@ template <typename S> struct Loader8 {
   int32x4 win_a, win_ea, win_b, win_eb;
   uint32_t oa[S::NLA], oea, ob, oeb;
   uint32_t group_bytes;              // of a group of 16 columns: steps * 2048
+  uint32_t row_step, group_step, row_exps_step, group_exps_step;      // bytes a source moves per stage
   int step, uwave;
   int again;                         // S::ONCE: above 0 where the expert has further tiles
   __device__ __forceinline__ void load(int I, uint32_t lds0, int slot) const {
     if (I < S::NLA) {
-      load16_to_lds_checked(win_a, oa[I] + (uint32_t)step * ROW8, lds0 + slot * S::A_BYTES + uwave * (S::NLA * 1024), I * 1024);
+      load16_to_lds_checked(win_a, oa[I] + (uint32_t)step * row_step, lds0 + slot * S::A_BYTES + uwave * (S::NLA * 1024), I * 1024);
     } else if (I < S::NLA + S::NLB) {
       const int J = I - S::NLA;
-      const uint32_t off = ob + ((uint32_t)(J >> 1) * group_bytes + (uint32_t)step * 2048u + (uint32_t)(J & 1) * 1024u);
+      const uint32_t off = ob + ((uint32_t)(J >> 1) * group_bytes + (uint32_t)step * group_step + (uint32_t)(J & 1) * 1024u);
       const uint32_t lds = lds0 + S::OFF_B + slot * B8_BYTES + uwave * (S::NLB * 1024);
       if (S::ONCE) load16_to_lds_checked_or_once(win_b, off, lds + J * 1024, again);
       else load16_to_lds_checked(win_b, off, lds, J * 1024);
     } else if (I == S::NLA + S::NLB) {
-      load4_to_lds_checked(win_ea, oea + (uint32_t)step * 4u, lds0 + S::OFF_EA + slot * (S::TM * 4) + (uwave & (S::TM / 64 - 1)) * 256);
+      load4_to_lds_checked(win_ea, oea + (uint32_t)step * row_exps_step, lds0 + S::OFF_EA + slot * (S::TM * 4) + (uwave & (S::TM / 64 - 1)) * 256);
     } else {
-      load4_to_lds_checked(win_eb, oeb + (uint32_t)step * 64u, lds0 + S::OFF_EB + slot * (TB * 4) + uwave * 256);
+      load4_to_lds_checked(win_eb, oeb + (uint32_t)step * group_exps_step, lds0 + S::OFF_EB + slot * (TB * 4) + uwave * 256);
     }
   }
 };
@@ -296,7 +297,7 @@ __global__ void __launch_bounds__(NTHREADS, 1) s2s8_stream_kernel(S2S8Args a, in
   extern __shared__ __attribute__((aligned(1024))) char smem[];
   __shared__ int s_off[MAX_E8 + 1], s_first[MAX_E8 + 1];
   // order indices of the rows of up to four open tiles, and the tiles: the loader has opened tile n + 2 and requested the rows of n + 3 while
-  // tile n is written out (contractions have two stages at least).
+  // tile n is written out (a tile has two stages at least).
   __shared__ int s_idx[4][S::TM];
   __shared__ __attribute__((aligned(16))) int s_tile[4][4];
 
@@ -306,7 +307,7 @@ __global__ void __launch_bounds__(NTHREADS, 1) s2s8_stream_kernel(S2S8Args a, in
   const int G = gridDim.x;
   const int pos = ((int)blockIdx.x & 7) * (G >> 3) + ((int)blockIdx.x >> 3);   // blocks b, b + 8, ... share an XCD and get consecutive tiles
   const int steps = (a.W.d_in + ROW8 - 1) / ROW8;
-  const int ns = steps;
+  const int ns = max(steps, 2);                         // a contraction of one stage has a second one of zeros
   for (int i = threadIdx.x; i <= a.W.E; i += NTHREADS) s_off[i] = a.offsets[i];
   __syncthreads();
   const int m_tiles = number_tiles8<S::TM>(s_off, a.W.E, s_first, lane);
@@ -355,6 +356,11 @@ __global__ void __launch_bounds__(NTHREADS, 1) s2s8_stream_kernel(S2S8Args a, in
   Loader8<S> ld;
   ld.uwave = uwave;
   ld.group_bytes = (uint32_t)steps * 2048u;
+  const uint32_t outside = steps == 1 ? 0x80000000u : 0u;     // where it lies
+  ld.row_step = ROW8 + outside;
+  ld.group_step = 2048u + outside;
+  ld.row_exps_step = 4u + outside;
+  ld.group_exps_step = 64u + outside;
   Reader8 rd;
 #pragma unroll
   for (int kk = 0; kk < 4; ++kk) rd.fa[kk] = line_frag_offset((wave >> 1) * (S::TM / 2), kk, lane);
@@ -380,7 +386,8 @@ __global__ void __launch_bounds__(NTHREADS, 1) s2s8_stream_kernel(S2S8Args a, in
     ld.win_eb = buffer_window(p->W.exps + (size_t)t.e * (per_expert / BLOCK8), per_expert / BLOCK8);
     if (S::ONCE) ld.again = t.row_end - __builtin_amdgcn_readfirstlane(s_off[t.e]) - S::TM;
     const int *idx = &s_idx[t.seq & 3][0];
-    // rows past the segment read zeros: an offset outside the window at every stage
+    // rows past the segment read zeros: an offset outside the window at every stage (in a second stage of zeros it wraps into the window, where the
+    // weights are the zeros)
     const uint32_t past = 0x80000000u;
 #pragma unroll
     for (int I = 0; I < S::NLA; ++I) {
@@ -566,7 +573,7 @@ template <typename S, int OUT, bool SCATTER> int launch_as(hipStream_t s, const 
   const int tiles_n = OUT == OUT_SWIGLU ? ceil_div(hidden, TB / 2) : OUT == OUT_GELU ? ceil_div(hidden, TB) : ceil_div(a.W.d_out, TB);
   const uint32_t magic = a.a_map.o ? division_magic(a.a_map.fan) : 0u;
   const dim3 grid(a.grid), block(NTHREADS);
-  if (steps % 2 == 0) hipLaunchKernelGGL((s2s8_stream_kernel<S, OUT, SCATTER, true>), grid, block, S::LDS_BYTES, s, a, tiles_n, a.group_m, magic);
+  if (steps % 2 == 0 || steps == 1) hipLaunchKernelGGL((s2s8_stream_kernel<S, OUT, SCATTER, true>), grid, block, S::LDS_BYTES, s, a, tiles_n, a.group_m, magic);
   else hipLaunchKernelGGL((s2s8_stream_kernel<S, OUT, SCATTER, false>), grid, block, S::LDS_BYTES, s, a, tiles_n, a.group_m, magic);
   SMOE_LAUNCH_CHECK();
   return SMOE_OK;
@@ -601,7 +608,7 @@ int init_stream8_kernels() {
 
 // 32-bit offsets into the rows, an expert's weights and a scattered output; the fan-out's division.
 bool s2s8_stream_supported(const S2S8Args &a) {
-  if (a.Tk < 1 || a.W.E > MAX_E8 || a.grid < 8 || a.W.d_in <= ROW8) return false;      // two stages at least
+  if (a.Tk < 1 || a.W.E > MAX_E8 || a.grid < 8) return false;
   if (a.wide || (a.C_exps && !a.c_map.o)) return false;
   const unsigned long long pitch = pitch8(a.W.d_in), rows = a.a_map.o ? a.Tk / a.a_map.fan : 256;
   if (rows * pitch > 0x7fff0000ULL || (unsigned long long)groups8(a.W.d_out, a.W.halves) * 16 * pitch + 32 * pitch * 16 > 0x7fff0000ULL) return false;

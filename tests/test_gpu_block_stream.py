@@ -33,7 +33,7 @@ def _few(smoe, call, mode):
 
 
 LINEARS = [  # T, d_in, d_out, E, k: even, odd, many and few stages; one column tile and several; more tiles than compute units
-    (150, 256, 136, 2, 2), (300, 384, 520, 3, 1), (90, 2048, 72, 1, 2), (5, 640, 8, 4, 2), (700, 500, 264, 5, 3), (5000, 256, 2056, 3, 2), (4000, 384, 1032, 40, 4), (2600, 130, 768, 200, 5),
+    (150, 256, 136, 2, 2), (300, 384, 520, 3, 1), (90, 2048, 72, 1, 2), (5, 640, 8, 4, 2), (700, 500, 264, 5, 3), (5000, 256, 2056, 3, 2), (4000, 384, 1032, 40, 4), (2600, 130, 768, 200, 5), (400, 128, 264, 3, 2), (333, 40, 1000, 2, 1), (3000, 100, 1536, 30, 4),
 ]
 
 
@@ -66,7 +66,7 @@ def test_linear(smoe, shape, T, d_in, d_out, E, k, form):
 
 MLPS = [  # T, d_model, d_expert, E, k, act
     (300, 256, 264, 4, 2, "swiglu"), (257, 304, 200, 2, 2, "gelu"), (520, 384, 1000, 3, 2, "swiglu"), (130, 256, 130, 1, 1, "gelu"), (1500, 512, 224, 64, 8, "swiglu"), (2000, 264, 161, 6, 3, "swiglu"),
-    (900, 640, 320, 5, 2, "gelu"),
+    (900, 640, 320, 5, 2, "gelu"), (700, 120, 128, 4, 2, "swiglu"), (500, 384, 60, 6, 2, "gelu"),
 ]
 
 
