@@ -52,14 +52,15 @@ bool grid_fits(int Tk, int E, int d_out) { return ((long long)Tk / 32 + E) * (ce
 size_t weights8_size(int E, int d_in, int d_out, int halves) { return (size_t)E * groups8(d_out, halves) * ceil_div(d_in, ROW8) * 2048; }
 
 // Which kernels a product takes, by an estimate of their times in us (the rows of each expert are on the device: they are taken as even).  Fitted to 91
-// products, seven layers at 8 to 2000 rows an expert, each timed on all three kernels; what the rule picks takes 1.1 % more than the fastest on
+// products, seven layers at 8 to 2000 rows an expert, each timed on all three kernels; what the rule picks takes 0.6 % more than the fastest on
 // average, 36 % at worst (32 experts of 300 rows, 1280 -> 1280: 39 us for 29).  Some of them, few rows / 128 x 256 / 256 x 256:
 //   64 experts, 2048 -> 1024: 8 rows 33 / 32 / 35, 32 rows 45 / 34 / 36, 200 rows 126 / 50 / 45, 2000 rows - / 350 / 287
 //   8 experts, 2816 -> 1024: 8 rows 9 / 26 / 32, 128 rows 21 / 25 / 35, 300 rows 36 / 27 / 36, 2000 rows - / 55 / 51
 //   16 experts, 2048 -> 1536: 8 rows 12 / 22 / 26, 64 rows 24 / 23 / 28, 200 rows 52 / 22 / 32, 1200 rows - / 80 / 63
 double few_rows_time(const S2S8Args &a) {
   const double expert = (double)groups8(a.W.d_out, a.W.halves) * ceil_div(a.W.d_in, ROW8) * 2048e-6, used = a.Tk < a.W.E ? a.Tk : a.W.E;      // MB of weights
-  return 4.0 + (a.Tk / 32.0 + 0.5 * used) * expert / 8.2 + used * expert * 0.08;      // tiles of 32 rows read them from the caches, once from memory
+  // tiles of 32 rows read them from the caches, once from memory, and write rows in pieces of 32 bytes (14756 rows on 48 experts, 128 -> 3712: 90 us)
+  return 4.0 + (a.Tk / 32.0 + 0.5 * used) * expert / 8.2 + used * expert * 0.08 + (a.act ? 0.0 : (double)a.Tk * a.W.d_out * 1e-6);
 }
 double tiles_time(const S2S8Args &a, int rows, double stage, double lone_stage, double epilogue) {
   const double used = a.Tk < a.W.E ? a.Tk : a.W.E, each = a.Tk / used / rows;
