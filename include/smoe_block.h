@@ -37,12 +37,13 @@ typedef struct {
 } smoe_gate_rule;
 
 /* logits [T,E] fp32, bias [E] fp32 or NULL (in); expert_idxs [T*k] int32, gates [T*k] fp32 (out).  E <= 1024 and k <= 64, else
- * SMOE_ERR_UNSUPPORTED.  T = 0 is a no-op. */
+ * SMOE_ERR_UNSUPPORTED, as are more than 2^26 - 64 tokens.  T = 0 is a no-op. */
 int smoe_score_gate(smoe_ctx *ctx, void *stream, const float *logits, const float *bias, int T, int E, int k, const smoe_gate_rule *rule,
                     int32_t *expert_idxs, float *gates);
 /* Gradient of the gates with respect to the logits (the choice is piecewise constant, the bias has none):
  *   dlogits [T,E] fp32 (out, every entry written) from logits, expert_idxs and dgates [T*k].  An expert named by several slots of a token
- * gets the sum of their gradients; slots that name none in [0,E) have gate 0 and get none.  Masked experts have gradient 0. */
+ * gets the sum of their gradients; slots that name none in [0,E) have gate 0 and get none.  Masked experts have gradient 0.  dlogits may be the
+ * logits themselves. */
 int smoe_score_gate_bwd(smoe_ctx *ctx, void *stream, const float *logits, const int32_t *expert_idxs, const float *dgates, int T, int E, int k,
                         const smoe_gate_rule *rule, float *dlogits);
 
@@ -93,12 +94,14 @@ int smoe_add_norm_bwd(smoe_ctx *ctx, void *stream, smoe_dtype dtype, const void 
 /* ---- the experts' products in 8 bits ---------------------------------------------------------------------------------------------
  * smoe_plinear_fwd on rows and weights in 8 bits, bf16 out: X [x_rows, d_in] and W (halves = 1) as packed, the other arguments as there;
  * d_out a multiple of 8.  No workspace.  Products are summed in fp32 over the contraction; the matrix instructions add each 64 or 128 of
- * them with an error of about 2^-13 of the largest (1.5e-5 of the sum for normal values), under the output's rounding. */
+ * them with an error of about 2^-12 of the largest (1.5e-5 of the sum for normal values), under the output's rounding.  Kernel modes 1 and 2 of
+ * smoe_set_kernel_mode force the kernels for few rows, 3 and 4 the 128 x 256 / 256 x 256 tiles. */
 int smoe_plinear8_fwd(smoe_ctx *ctx, void *stream, const smoe_rows8 *X, int x_rows, int d_in, const smoe_weights8 *W, int d_out, const smoe_routing *r,
                       int k, const float *gates, int gates_k, int grouped_in, int grouped_out, void *Yhat, void *Y);
 /* The SMoE MLP (Alg. 3) forward: X [T, d_model] rows, W1 (halves = 2 for SWIGLU, else 1) and W2 (halves = 1) packed, gates [T*k] fp32,
- * Y [T, d_model] bf16 (out).  The hidden rows are packed to 8 bits from fp32 in the first product's epilogue.  d_model a multiple of 8,
- * d_expert any. */
+ * Y [T, d_model] bf16 (out).  The hidden rows are packed to 8 bits from fp32 in the first product's epilogue (a hidden value within the product's error of
+ * a border between two codes may take either); the second product's rows are summed from fp32 or fp16 with a power of two for 128 columns
+ * (bf16 for more than 8192 routed rows on the kernels for few rows).  d_model a multiple of 8, d_expert any. */
 size_t smoe_mlp8_fwd_workspace_bytes(smoe_act act, int T, int k, int d_model, int d_expert);
 int smoe_mlp8_fwd(smoe_ctx *ctx, void *stream, smoe_act act, const smoe_rows8 *X, int T, int d_model, int d_expert, const smoe_weights8 *W1,
                   const smoe_weights8 *W2, const smoe_routing *r, int k, const float *gates, void *Y, void *ws, size_t ws_bytes);

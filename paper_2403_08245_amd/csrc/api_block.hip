@@ -26,7 +26,7 @@ int gate_args_ok(smoe_ctx *ctx, int T, int E, int k, const smoe_gate_rule *rule)
   if (!ctx || T < 0 || E < 1 || k < 1 || k > E) return SMOE_ERR_INVALID_ARG;
   int rc = rule_ok(rule, E, k);
   if (rc != SMOE_OK) return rc;
-  return (long long)T * k > 0x7fffffffLL ? SMOE_ERR_UNSUPPORTED : SMOE_OK;
+  return T > GATE_MAX_T || (long long)T * k > 0x7fffffffLL ? SMOE_ERR_UNSUPPORTED : SMOE_OK;
 }
 
 bool routing_ok(const smoe_routing *r) {
@@ -164,7 +164,7 @@ int smoe_weights8_pack(smoe_ctx *ctx, void *stream, smoe_dtype dtype, const void
 
 static int norm_sizes_ok(smoe_ctx *ctx, smoe_dtype dtype, int rows, int d) {
   if (!ctx || !dtype_ok(dtype) || rows < 0 || d < 1) return SMOE_ERR_INVALID_ARG;
-  return d > NORM_MAX_D ? SMOE_ERR_UNSUPPORTED : SMOE_OK;
+  return d > NORM_MAX_D || rows > NORM_MAX_ROWS ? SMOE_ERR_UNSUPPORTED : SMOE_OK;
 }
 
 int smoe_add_norm_fwd(smoe_ctx *ctx, void *stream, smoe_dtype dtype, const void *X, const void *R, const void *weight, int rows, int d, float eps,
@@ -189,7 +189,7 @@ int smoe_add_norm_fwd(smoe_ctx *ctx, void *stream, smoe_dtype dtype, const void 
 }
 
 size_t smoe_add_norm_bwd_workspace_bytes(smoe_dtype dtype, int rows, int d) {
-  if (!dtype_ok(dtype) || rows < 0 || d < 1 || d > NORM_MAX_D) return 0;
+  if (!dtype_ok(dtype) || rows < 0 || rows > NORM_MAX_ROWS || d < 1 || d > NORM_MAX_D) return 0;
   return align256((size_t)norm_bwd_parts(dtype, rows, d) * d * sizeof(float));
 }
 
@@ -227,7 +227,8 @@ int smoe_plinear8_fwd(smoe_ctx *ctx, void *stream, const smoe_rows8 *X, int x_ro
   if (!X->values || !X->exps || !Yhat) return SMOE_ERR_INVALID_ARG;
   if (!aligned(X->values, X->exps, gates, Yhat, Y)) return SMOE_ERR_UNSUPPORTED;
   const size_t stored = weights8_size(r->E, d_in, d_out, 1), rows = rows8_bytes(x_rows, d_in);
-  const Span ins[] = {{X->values, rows}, {X->exps, rows / BLOCK8}, {W->values, stored}, {W->exps, stored / BLOCK8}, {gates, (size_t)Tk * 4}};
+  const Span ins[] = {{X->values, rows}, {X->exps, rows / BLOCK8}, {W->values, stored}, {W->exps, stored / BLOCK8}, {gates, (size_t)Tk * 4},
+                      {r->sorted_scattered_idxs, (size_t)Tk * 4}, {r->expert_offsets, ((size_t)r->E + 1) * 4}};
   const Span outs[] = {{Yhat, (size_t)Tk * d_out * 2}, {Y, gates ? (size_t)(Tk / gates_k) * d_out * 2 : 0}};
   for (const Span &o : outs)
     for (const Span &i : ins)
@@ -271,7 +272,7 @@ int smoe_mlp8_fwd(smoe_ctx *ctx, void *stream, smoe_act act, const smoe_rows8 *X
   if (!ws || ((uintptr_t)ws & 255) || ws_bytes < l.total) return SMOE_ERR_WORKSPACE;
   const size_t first = weights8_size(r->E, d_model, d_expert * halves, halves), second = weights8_size(r->E, d_expert, d_model, 1), rows = rows8_bytes(T, d_model);
   const Span ins[] = {{X->values, rows}, {X->exps, rows / BLOCK8}, {W1->values, first}, {W1->exps, first / BLOCK8}, {W2->values, second}, {W2->exps, second / BLOCK8},
-                      {gates, (size_t)Tk * 4}};
+                      {gates, (size_t)Tk * 4}, {r->sorted_scattered_idxs, (size_t)Tk * 4}, {r->expert_offsets, ((size_t)r->E + 1) * 4}};
   const Span outs[] = {{Y, (size_t)T * d_model * 2}, {ws, l.total}};
   for (const Span &o : outs)
     for (const Span &i : ins)

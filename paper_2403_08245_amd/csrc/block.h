@@ -4,12 +4,13 @@
 #include "smoe_block.h"
 
 // ---- gate.hip
+constexpr int GATE_MAX_T = (1 << 26) - 64;      // a wavefront a token, in one launch
 int launch_score_gate(hipStream_t s, const float *logits, const float *bias, int T, int E, int k, const smoe_gate_rule &rule, int32_t *idx, float *gates);
 int launch_score_gate_bwd(hipStream_t s, const float *logits, const int32_t *idx, const float *dgates, int T, int E, int k, const smoe_gate_rule &rule,
                           float *dlogits);
 
 // ---- norm.hip
-constexpr int NORM_MAX_D = 32768;
+constexpr int NORM_MAX_D = 32768, NORM_MAX_ROWS = 0x7fffffff - 63;
 struct NormArgs {
   const void *X, *R, *weight;
   int rows, d;

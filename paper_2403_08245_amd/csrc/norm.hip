@@ -1,6 +1,7 @@
 // The root-mean-square norm of the residual stream with the addition in front of it, its gradient, and its output in 8 bits.
 // Bound: HBM, each tensor read or written once; a row stays in registers between its sum and its output.
 #include "block.h"
+#include <algorithm>
 #include <type_traits>
 
 namespace {
@@ -331,14 +332,30 @@ template <typename T, typename F> void by_bwd_shape(int d, F f) {
   }
 }
 constexpr int BWD_BLOCKS = 512;
+constexpr int LAUNCH_ROWS = 1 << 21;       // a launch has fewer than 2^32 threads
 
-template <typename T> int launch_norm_as(hipStream_t s, const NormArgs &a) {
-  by_shape<T>(a.d, [&](auto v, auto tpr, auto nv) {
-    constexpr int TPR = decltype(tpr)::value, ROWS = TPR > 256 ? 1 : 256 / TPR;
-    hipLaunchKernelGGL((norm_kernel<T, decltype(v)::value, TPR, decltype(nv)::value>), dim3(ceil_div(a.rows, ROWS)), dim3(TPR > 256 ? TPR : 256), 0, s, a,
-                       pitch8(a.d));
-  });
-  SMOE_LAUNCH_CHECK();
+template <typename T> int launch_norm_as(hipStream_t s, const NormArgs &all) {
+  for (long long first = 0; first < all.rows; first += LAUNCH_ROWS) {
+    NormArgs a = all;
+    const size_t skip = (size_t)first * all.d;
+    const int pitch = pitch8(all.d);
+    a.rows = (int)std::min<long long>(all.rows - first, LAUNCH_ROWS);
+    a.X = (const T *)all.X + skip;
+    if (a.R) a.R = (const T *)all.R + skip;
+    if (a.S) a.S = (T *)all.S + skip;
+    if (a.Y) a.Y = (T *)all.Y + skip;
+    if (a.rstd) a.rstd += first;
+    if (a.Y8.values) {
+      a.Y8.values += (size_t)first * pitch;
+      a.Y8.exps += (size_t)first * (pitch / BLOCK8);
+    }
+    by_shape<T>(a.d, [&](auto v, auto tpr, auto nv) {
+      constexpr int TPR = decltype(tpr)::value, ROWS = TPR > 256 ? 1 : 256 / TPR;
+      hipLaunchKernelGGL((norm_kernel<T, decltype(v)::value, TPR, decltype(nv)::value>), dim3(ceil_div(a.rows, ROWS)), dim3(TPR > 256 ? TPR : 256), 0, s, a,
+                         pitch);
+    });
+    SMOE_LAUNCH_CHECK();
+  }
   return SMOE_OK;
 }
 template <typename T> int launch_norm_bwd_as(hipStream_t s, const NormBwdArgs &a) {

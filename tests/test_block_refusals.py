@@ -79,7 +79,7 @@ def test_no_context(call, name):
 
 GATE = [dict(norule=True), dict(T=-1), dict(E=0), dict(k=0), dict(k=9), dict(score=2), dict(score=-1), dict(groups=0), dict(groups=3), dict(kept=0), dict(kept=5), dict(best=0),
         dict(kept=1, k=3), dict(renorm=2), dict(scale=math.nan), dict(scale=math.inf), dict(x=None)]
-TOO_MUCH = [dict(best=3), dict(E=1032, groups=1, kept=1), dict(E=256, groups=128, kept=128, k=2), dict(E=128, k=65, groups=1, kept=1), dict(T=2 ** 30, k=2), dict(x=STEP + 4)]
+TOO_MUCH = [dict(best=3), dict(E=1032, groups=1, kept=1), dict(E=256, groups=128, kept=128, k=2), dict(E=128, k=65, groups=1, kept=1), dict(T=2 ** 30, k=2), dict(T=2 ** 26 - 63, k=2), dict(x=STEP + 4)]
 
 
 @pytest.mark.parametrize("name", ["gate", "gate_bwd"])
@@ -125,7 +125,7 @@ def test_weights(m, call):
 def test_norm(call):
     for bad in (dict(dtype=9), dict(rows=-1), dict(d=0), dict(eps=-1.0), dict(eps=math.nan), dict(eps=math.inf), dict(Y=None, Yv=None), dict(x=None), dict(w=None), dict(Ye=None)):
         assert call("norm", **bad) == INVALID, bad
-    for bad in (dict(d=32769), dict(x=STEP + 8), dict(S=STEP + 2), dict(rstd=STEP + 4)):
+    for bad in (dict(d=32769), dict(rows=2 ** 31 - 63), dict(x=STEP + 8), dict(S=STEP + 2), dict(rstd=STEP + 4)):
         assert call("norm", **bad) == UNSUPPORTED, bad
     at = call.at
     for out in ("S", "Y"):
@@ -162,7 +162,7 @@ def test_linear(call):
     for bad in (dict(d_out=60), dict(Xv=STEP + 8), dict(Yhat=STEP + 8), dict(Tk=2 ** 31 - 2, x_rows=2 ** 30 - 1, d_out=2 ** 20)):
         assert call("linear", **bad) == UNSUPPORTED, bad
     at = call.at
-    for a, b in (("Yhat", "Xv"), ("Yhat", "Xe"), ("Yhat", "Wv"), ("Yhat", "We"), ("Yhat", "g"), ("Y", "Xv"), ("Y", "g"), ("Y", "Yhat"), ("Y", "Wv")):
+    for a, b in (("Yhat", "Xv"), ("Yhat", "Xe"), ("Yhat", "Wv"), ("Yhat", "We"), ("Yhat", "g"), ("Y", "Xv"), ("Y", "g"), ("Y", "Yhat"), ("Y", "Wv"), ("Yhat", "o"), ("Y", "off")):
         assert call("linear", **{a: at[b]}) == INVALID, (a, b)
     assert call("linear", Tk=0, x_rows=0, Xv=None, Yhat=None) == OK
 
@@ -178,7 +178,7 @@ def test_mlp(m, call):
     for bad in (dict(ws=None), dict(ws=call.at["ws"] + 16), dict(wsb=need - 1)):
         assert call("mlp", **bad) == WORKSPACE, bad
     at = call.at
-    for a, b in (("Y", "Xv"), ("Y", "Xe"), ("Y", "Wv"), ("Y", "Ve"), ("Y", "g"), ("Y", "ws"), ("ws", "Xv"), ("ws", "Xe"), ("ws", "Vv"), ("ws", "We"), ("ws", "g")):
+    for a, b in (("Y", "Xv"), ("Y", "Xe"), ("Y", "Wv"), ("Y", "Ve"), ("Y", "g"), ("Y", "ws"), ("ws", "Xv"), ("ws", "Xe"), ("ws", "Vv"), ("ws", "We"), ("ws", "g"), ("ws", "o"), ("Y", "off")):
         assert call("mlp", **{a: at[b]}) == INVALID, (a, b)
     assert call("mlp", T=0, Tk=0, Xv=None, Y=None, ws=None) == OK
     size = m.lib.smoe_mlp8_fwd_workspace_bytes

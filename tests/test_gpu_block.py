@@ -487,8 +487,9 @@ def test_a_block_as_it_is_served(smoe, T):
     _near(m.Y, y, 2.0 ** -8 * np.abs(y) * 1.01 + 2 * NORM_UNITS * np.abs(y))
 
 
-def test_a_block_replays_from_a_graph_on_another_stream(smoe):
-    state, others = _block_state(smoe, 24, 60), [_block_state(smoe, 24, 60 + 10 * i) for i in range(3)]
+@pytest.mark.parametrize("T", [24, 1500])
+def test_a_block_replays_from_a_graph_on_another_stream(smoe, T):
+    state, others = _block_state(smoe, T, 60), [_block_state(smoe, T, 60 + 10 * i) for i in range(3)]
     names = ("X", "R")
 
     def step():
@@ -514,6 +515,37 @@ def test_a_block_replays_from_a_graph_on_another_stream(smoe):
         got = [t.clone() for t in captured]
         for a, b in zip(got, step()):
             assert torch.equal(a, b)
+
+
+def test_rows_past_32_bits(smoe):
+    """More elements than 2^31: the last rows are those of a call of their own."""
+    rows, d = 2 ** 19 + 37, 4104
+    X = torch.zeros(rows, d, dtype=torch.bfloat16, device="cuda")
+    last = _normal((50, d), 1).cuda()
+    X[-50:] = last
+    w = _normal((d,), 2).cuda()
+    n, few = smoe.add_norm_fwd(X, w, X, packed=True), smoe.add_norm_fwd(last, w, last, packed=True)
+    for a, b in ((n.S, few.S), (n.Y, few.Y), (n.rstd, few.rstd), (n.Y8.values, few.Y8.values), (n.Y8.exps, few.Y8.exps)):
+        assert torch.equal(a[-50:], b)
+    packed = smoe.rows8_pack(X)
+    assert torch.equal(packed.values[-50:], smoe.rows8_pack(last).values)
+    assert torch.equal(smoe.rows8_unpack(packed)[-50:], smoe.rows8_unpack(smoe.rows8_pack(last)))
+    dX, dw = smoe.add_norm_bwd(X, n.S, w, n.rstd, out=(X, torch.empty_like(w)))
+    want, dweight = smoe.add_norm_bwd(last, few.S, w, few.rstd)
+    assert torch.equal(dX[-50:], want) and torch.equal(dX[:3], torch.zeros_like(dX[:3]))
+    tol = 64 * EPS32 * (last.double().abs() * (few.S.double() * few.rstd[:, None].double()).abs()).sum(0)      # another order of the sums, and a rounding
+    assert ((dw.double() - dweight.double()).abs() <= 2 * HALF[torch.bfloat16] * dweight.double().abs() + tol).all()
+
+
+def test_more_rows_than_a_launch_has(smoe):
+    rows = 2 ** 21 + 101
+    X, w = torch.randn(rows, 8, device="cuda"), torch.ones(8, device="cuda")
+    n, last = smoe.add_norm_fwd(X, w, X, packed=True), smoe.add_norm_fwd(X[-128:].contiguous(), w, X[-128:].contiguous(), packed=True)
+    for a, b in ((n.S, last.S), (n.Y, last.Y), (n.rstd, last.rstd), (n.Y8.values, last.Y8.values), (n.Y8.exps, last.Y8.exps)):
+        assert torch.equal(a[-128:], b)
+    assert torch.equal(n.S, X + X)
+    packed = smoe.rows8_pack(X)
+    assert torch.equal(packed.values[-128:], smoe.rows8_pack(X[-128:].contiguous()).values)
 
 
 def test_identical_calls_give_identical_bits(smoe):
