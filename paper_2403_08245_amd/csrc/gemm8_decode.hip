@@ -82,7 +82,8 @@ __global__ void __launch_bounds__(64 * CW * KW, 2) s2s8_decode_kernel(S2S8Args a
       }
       return w;
     };
-    Weights w0 = load_w(0), w1 = load_w(min(1, mine - 1));
+    const int second = mine > 1 ? 1 : 0;               // a share may be of one step or none: then products of zeros
+    Weights w0 = load_w(0), w1 = load_w(second);
     const uint8_t *xv[F], *xe[F];                      // rows past the segment repeat its last row
 #pragma unroll
     for (int m = 0; m < F; ++m) {
@@ -99,7 +100,7 @@ __global__ void __launch_bounds__(64 * CW * KW, 2) s2s8_decode_kernel(S2S8Args a
       }
       return x;
     };
-    Rows<F> x0 = load_x(0), x1 = load_x(min(1, mine - 1));
+    Rows<F> x0 = load_x(0), x1 = load_x(second);
     f32x4 acc[F][4];
 #pragma unroll
     for (int m = 0; m < F; ++m)
@@ -244,7 +245,7 @@ template <int ACT, bool WIDE, int CW, int KW> int launch_as(hipStream_t s, const
   return SMOE_OK;
 }
 template <int ACT, bool WIDE> int launch(hipStream_t s, const S2S8Args &a) {
-  const long long experts = a.Tk < a.W.E ? a.Tk : a.W.E, units = ACT == SMOE_ACT_SWIGLU ? a.W.d_out / 64 : a.W.d_out / 64;
+  const long long experts = a.Tk < a.W.E ? a.Tk : a.W.E, units = a.W.d_out / 64;
   if (experts * units >= 8 * a.grid) return launch_as<ACT, WIDE, 4, 1>(s, a);
   if (experts * units >= 4 * a.grid) return launch_as<ACT, WIDE, 2, 2>(s, a);
   return launch_as<ACT, WIDE, 1, 4>(s, a);
