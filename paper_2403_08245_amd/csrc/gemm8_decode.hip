@@ -244,10 +244,20 @@ template <int ACT, bool WIDE, int CW, int KW> int launch_as(hipStream_t s, const
   SMOE_LAUNCH_CHECK();
   return SMOE_OK;
 }
+// How the wavefronts of a block divide the work: side by side, or along the contraction where there are too few columns to fill the chip.  One product, weights from
+// memory, us, 4 x 1 / 2 x 2 / 1 x 4: 64 tokens on 64 experts, k = 8, 512 -> 2048 13.6 / 15.7 / 18.9; 200 tokens on 8 experts, k = 2, 2816 -> 1024 22.6 / 14 / 10.3;
+// four tokens on 64 experts, k = 8, 512 -> 2048 8.7 / 8 / 10.7; 16 tokens on 8 experts, k = 2, 14336 -> 4096 94 / 75 / 73.5.
+// Groups of columns that lie an odd number of 32 KB apart get in one another's way when 16 of them are read in step, with up to 16 rows an expert: 64 tokens on 64
+// experts, k = 8, -> 8192: 2048 206 / 191 / 174, 1024 105 / 95 / 108, 4096 wide (-> 4096) 183 / 207 / 195, 1920 (-> 4096) 94.5 / 95.3 / 97.5.  (Wavefronts that begin
+// at different steps of the contraction gained 0 to 4 % there and cost others up to 40 %.)
 template <int ACT, bool WIDE> int launch(hipStream_t s, const S2S8Args &a) {
   const long long experts = a.Tk < a.W.E ? a.Tk : a.W.E, units = a.W.d_out / 64;
-  if (experts * units >= 8 * a.grid) return launch_as<ACT, WIDE, 4, 1>(s, a);
-  if (experts * units >= 4 * a.grid) return launch_as<ACT, WIDE, 2, 2>(s, a);
+  const int steps = ceil_div(a.W.d_in, ROW8);
+  const bool thin = a.Tk <= 16 * experts;
+  int shares = experts * units >= 8 * a.grid ? 1 : experts * units >= 4 * a.grid ? 2 : 4;
+  if (shares == 1 && thin) shares = steps % 32 == 16 ? 4 : steps % 16 == 8 ? 2 : 1;
+  if (shares == 1) return launch_as<ACT, WIDE, 4, 1>(s, a);
+  if (shares == 2) return launch_as<ACT, WIDE, 2, 2>(s, a);
   return launch_as<ACT, WIDE, 1, 4>(s, a);
 }
 

@@ -384,6 +384,30 @@ def test_linear_in_8_bits(smoe, T, d_in, d_out, E, k, form):
     _near(Y, want, half * np.abs(want) + (1 + half) * tol, form)
 
 
+# enough columns that wavefronts stand side by side (256, 1280), and the contractions at which they share it all the same (1024, 2048), but for more rows
+@pytest.mark.parametrize("T,d_in", [(20, 256), (20, 1280), (20, 1024), (20, 2048), (300, 1024), (7, 2050)])
+def test_wide_weights_of_few_rows(smoe, T, d_in):
+    E, k, d_out = 16, 2, 16392
+    _log(f"plinear8 wide {(T, d_in)}")
+    idx, _, r = _routed(smoe, T, E, k, 71)
+    X = _normal((T, d_in), 72)
+    W = torch.randn(E, d_in, d_out, generator=torch.Generator("cuda").manual_seed(73), device="cuda").mul_(0.05).bfloat16()
+    smoe.set_kernel_mode(1)
+    try:
+        Y = smoe.plinear8_fwd(smoe.rows8_pack(X.cuda()), smoe.weights8(W), r, k)[0]
+    finally:
+        smoe.set_kernel_mode(0)
+    columns = torch.cat([torch.arange(0, d_out, 797), torch.tensor([d_out - 1])])
+    kept = _f64(W[:, :, columns.cuda()])
+    w = [oracle.unpack8(*oracle.pack8(kept[e].T), d_in).T for e in range(E)]
+    x = oracle.unpack8(*oracle.pack8(_f64(X)), d_in)
+    slots = range(0, T * k, max(1, T * k // 40))
+    want = np.stack([x[s // k] @ w[idx[s // k, s % k]] for s in slots])
+    tol = np.stack([_slack(x[s // k], w[idx[s // k, s % k]]) for s in slots])
+    half = HALF[torch.bfloat16]
+    _near(Y[list(slots)][:, columns.cuda()], want, half * np.abs(want) + (1 + half) * tol, "wide")
+
+
 MLPS = [  # T, d_model, d_expert, E, k, act
     (1, 32, 32, 1, 1, "swiglu"), (4, 256, 64, 8, 2, "swiglu"), (9, 128, 100, 4, 2, "gelu"), (40, 200, 72, 2, 2, "swiglu"), (20, 256, 160, 16, 4, "gelu"), (130, 136, 40, 3, 1, "swiglu"),
     (3, 1000, 33, 2, 2, "swiglu"), (6, 128, 257, 3, 2, "gelu"),
