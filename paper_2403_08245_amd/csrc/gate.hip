@@ -1,5 +1,6 @@
-// The router's gate by scores and its gradient.  One wavefront per token; a lane holds VPL consecutive experts, so that a group of experts is a run of
-// lanes.  Bound: reading the logits (and writing their gradient), then the rounds of the selection.
+// The router's gate by scores and its gradient.  A lane holds VPL consecutive experts, so that a group of experts is a run of lanes; a token is 16 lanes (or
+// a wavefront: many experts, large k, and every token whose choice fp32 cannot tell).  Bound: the rounds of the selection, then reading the logits and writing
+// their gradient (32768 tokens of 256 experts in groups, k = 8: 22.3 us forward, where its logits take 6.7; 9.8 backward, 34 MB written, 3.6 TB/s).
 //
 // The choice is that of 64-bit scores: with a bias or sums of two, ranks of different experts come within 32-bit rounding of one another once in some
 // thousand tokens, and which one is taken would then hang on how the exponential was rounded.  Where the order of the scores is that of the
@@ -589,7 +590,9 @@ int launch_score_gate(hipStream_t s, const float *logits, const float *bias, int
   const dim3 block(256);
   const bool grouped = rule.kept_groups < rule.groups;
   const bool wide = bias || (grouped && rule.group_best > 1);
-  // four tokens a wavefront: where 16 lanes hold a row, and a group is a run of lanes
+  // Four tokens a wavefront: where 16 lanes hold a row, and a group is a run of lanes.  Four / one, us: 4 tokens of 256 experts 4.4 / 6.6, 16384 of 64 5.3 / 9.3, of
+  // 160 14.7 / 33.8, of 512 25.4 / 54.1, 32768 of 128 9.8 / 17, of 256 22.3 / 66.5; logits that are all equal, so that every token is taken
+  // again, 86 / 64.
   const int vpl = E <= 64 ? 4 : E <= 128 ? 8 : E <= 256 ? 16 : 32;
   if (E <= 512 && k <= 16 && (!grouped || E / rule.groups % vpl == 0)) {
     const dim3 grid(ceil_div(T, 16));
@@ -622,6 +625,7 @@ int launch_score_gate_bwd(hipStream_t s, const float *logits, const int32_t *idx
                           float *dlogits) {
   const dim3 block(256);
   const bool row = rule.score == SMOE_SCORE_SOFTMAX && !rule.renormalise;
+  // four tokens / one token a wavefront, us: 4 tokens of 256 experts 2.8 / 3.1, 16384 of 64 (softmax) 4.6 / 7.6, of 512 (sigmoid) 9 / 13.5, 32768 of 256 9.8 / 17.3
   if (k <= 16 && (!row || E <= 256)) {
     const dim3 grid(ceil_div(T, 16));
     if (!row) hipLaunchKernelGGL((score_gate_bwd_rows_kernel<1, false>), grid, block, 0, s, logits, idx, dgates, T, E, k, rule, dlogits);

@@ -1,5 +1,7 @@
 // The root-mean-square norm of the residual stream with the addition in front of it, its gradient, and its output in 8 bits.
-// Bound: HBM, each tensor read or written once; a row stays in registers between its sum and its output.
+// Bound: HBM, each tensor read or written once; a row stays in registers between its sum and its output.  Rows of 2048 in bf16, 8192 of them: forward 22.5 us
+// (134 MB, 6.0 TB/s), with 8 bits besides 27.5, 8 bits only 21, gradient 30 (4.5 TB/s); 8191 of 4096: 46, 57, 44, 51; 4000 of 5001, one element at a time
+// since rows start off the 16-byte lines: 66 (2.4 TB/s) and 85.
 #include "block.h"
 #include <algorithm>
 #include <type_traits>
