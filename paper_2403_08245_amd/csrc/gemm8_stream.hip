@@ -2,7 +2,7 @@
 // v_mfma_scale_f32_32x32x64_f8f6f4 with the weights as the first operand, so that a lane holds four consecutive columns of a row.
 // Bound: the matrix cores at twice the rate of bf16; an instruction reads as many bytes of operands in as many cycles, so the loop is the
 // one of the bf16 kernels (gemm_stream.hip) with stages of 128 elements instead of 64: the same 128 bytes a row.
-// 8192 x 8192 x 8192: 485 us, 2.27 PFLOP/s, 0.93 of the library's product of the same box; the matrix cores are busy for 0.79 of the cycles.  Of the rest 4 % are the
+// 8192 x 8192 x 8192: 485 us, 2.27 PFLOP/s, 0.93 of the library's product of the same box; the matrix cores are busy for 0.77 of the cycles.  Of the rest 4 % are the
 // rows' powers of two (gathered, four bytes a row and stage), 6 % misses of L2, by timing copies of the loop without the one or with rows that
 // stay there; with no loads in the loop at all it takes 413 us.
 //
