@@ -8,57 +8,59 @@
 
 namespace {
 
-// V elements of a row as they are loaded and stored
-template <typename T, int V> struct Pack {
-  float v[V];
-  __device__ __forceinline__ void load(const T *p) {
-    if constexpr (V == 1) {
-      v[0] = to_f32<T>(*p);
+// Eight elements of a row in memory.  WHOLE: rows are whole eights, on 16-byte lines; else a row starts on any element, and its last `n` may be fewer.
+template <typename T, bool WHOLE> struct Chunks {
+  static constexpr int PER = 16 / sizeof(T), N = 8 / PER;
+  typedef T vec __attribute__((ext_vector_type(PER)));
+  typedef T loose __attribute__((ext_vector_type(PER), aligned(sizeof(T))));
+  vec v[N];
+  __device__ __forceinline__ void load(const T *p, int n) {
+    if (WHOLE || n >= 8) {
+#pragma unroll
+      for (int q = 0; q < N; ++q) v[q] = WHOLE ? reinterpret_cast<const vec *>(p)[q] : *reinterpret_cast<const loose *>(p + q * PER);
     } else {
-      constexpr int PER = 16 / sizeof(T);
-      typedef T vec __attribute__((ext_vector_type(PER)));
 #pragma unroll
-      for (int q = 0; q < V / PER; ++q) {
-        const vec x = reinterpret_cast<const vec *>(p)[q];
-#pragma unroll
-        for (int i = 0; i < PER; ++i) v[q * PER + i] = to_f32<T>(x[i]);
-      }
+      for (int i = 0; i < 8; ++i) v[i / PER][i % PER] = i < n ? p[i] : from_f32<T>(0.f);
     }
   }
-  __device__ __forceinline__ void store(T *p) const {
-    if constexpr (V == 1) {
-      *p = from_f32<T>(v[0]);
-    } else {
-      constexpr int PER = 16 / sizeof(T);
-      typedef T vec __attribute__((ext_vector_type(PER)));
+  __device__ __forceinline__ void store(T *p, int n) const {
+    if (WHOLE || n >= 8) {
 #pragma unroll
-      for (int q = 0; q < V / PER; ++q) {
-        vec x;
-#pragma unroll
-        for (int i = 0; i < PER; ++i) x[i] = from_f32<T>(v[q * PER + i]);
-        reinterpret_cast<vec *>(p)[q] = x;
+      for (int q = 0; q < N; ++q) {
+        if (WHOLE) reinterpret_cast<vec *>(p)[q] = v[q];
+        else *reinterpret_cast<loose *>(p + q * PER) = v[q];
       }
+    } else {
+#pragma unroll
+      for (int i = 0; i < 7; ++i)
+        if (i < n) p[i] = v[i / PER][i % PER];
     }
   }
 };
-
-// the same, kept as they come
-template <typename T, int V> struct Raw {
-  static constexpr int PER = V == 1 ? 1 : 16 / sizeof(T);
-  typedef T vec __attribute__((ext_vector_type(PER)));
-  vec v[V / PER];
-  __device__ __forceinline__ void load(const T *p) {
+// Eight elements as they are worked on
+template <typename T, bool WHOLE> struct Pack {
+  float v[8];
+  __device__ __forceinline__ void load(const T *p, int n) {
+    Chunks<T, WHOLE> x;
+    x.load(p, n);
 #pragma unroll
-    for (int q = 0; q < V / PER; ++q) {
-      if constexpr (V == 1) v[q][0] = *p;
-      else v[q] = reinterpret_cast<const vec *>(p)[q];
-    }
+    for (int i = 0; i < 8; ++i) v[i] = to_f32<T>(x.v[i / x.PER][i % x.PER]);
   }
+  __device__ __forceinline__ void store(T *p, int n) const {
+    Chunks<T, WHOLE> x;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x.v[i / x.PER][i % x.PER] = from_f32<T>(v[i]);
+    x.store(p, n);
+  }
+};
+// the same, kept as they come
+template <typename T, bool WHOLE> struct Raw : Chunks<T, WHOLE> {
+  using C = Chunks<T, WHOLE>;
   __device__ __forceinline__ void clear() {
 #pragma unroll
-    for (int q = 0; q < V; ++q) v[q / PER][q % PER] = from_f32<T>(0.f);
+    for (int i = 0; i < 8; ++i) C::v[i / C::PER][i % C::PER] = from_f32<T>(0.f);
   }
-  __device__ __forceinline__ float get(int i) const { return to_f32<T>(v[i / PER][i % PER]); }
+  __device__ __forceinline__ float get(int i) const { return to_f32<T>(C::v[i / C::PER][i % C::PER]); }
 };
 
 // sum over the TPR threads of a row, in all of them; `slot`: LDS of the row's wavefronts
@@ -77,35 +79,31 @@ template <int TPR> __device__ __forceinline__ float row_sum(float v, float *slot
   return v;
 }
 
-// V elements of a block of 32 per lane, 32 / V lanes a block
-template <int V> __device__ __forceinline__ void store8(const float (&y)[V], uint8_t *values, uint8_t *exps, int col) {
+// eight elements of a block of 32 per lane
+__device__ __forceinline__ void store8(const float (&y)[8], uint8_t *values, uint8_t *exps, int col) {
   float amax = 0.f;
 #pragma unroll
-  for (int i = 0; i < V; ++i) amax = fmaxf(amax, finite_abs(y[i]));
-#pragma unroll
-  for (int d = 1; d < BLOCK8 / V; d <<= 1) amax = fmaxf(amax, __shfl_xor(amax, d, 64));
+  for (int i = 0; i < 8; ++i) amax = fmaxf(amax, finite_abs(y[i]));
+  amax = fmaxf(amax, __shfl_xor(amax, 1, 64));
+  amax = fmaxf(amax, __shfl_xor(amax, 2, 64));
   const unsigned int byte = e4m3_byte(amax);
-  if constexpr (V == 8) {
-    uint2 q;
-    q.x = e4m3_four(y[0], y[1], y[2], y[3], byte);
-    q.y = e4m3_four(y[4], y[5], y[6], y[7], byte);
-    *reinterpret_cast<uint2 *>(values + col) = q;
-  } else {
-    values[col] = (uint8_t)(e4m3_four(y[0], 0.f, 0.f, 0.f, byte) & 0xffu);
-  }
+  uint2 q;
+  q.x = e4m3_four(y[0], y[1], y[2], y[3], byte);
+  q.y = e4m3_four(y[4], y[5], y[6], y[7], byte);
+  *reinterpret_cast<uint2 *>(values + col) = q;
   if (col % BLOCK8 == 0) exps[col / BLOCK8] = (uint8_t)byte;
 }
 
-// TPR threads a row, NV packs of V elements each; rows wider than that are another instantiation's.
-template <typename T, int V, int TPR, int NV>
+// TPR threads a row, NV packs of eight elements each; rows wider than that are another instantiation's.
+template <typename T, bool WHOLE, int TPR, int NV>
 __global__ void __launch_bounds__(TPR > 256 ? TPR : 256) norm_kernel(NormArgs a, int pitch) {
-  constexpr int ROWS = TPR > 256 ? 1 : 256 / TPR;
+  constexpr int V = 8, ROWS = TPR > 256 ? 1 : 256 / TPR;
   __shared__ float s_sum[16];
   const int t = threadIdx.x % TPR;
   const long long row = (long long)blockIdx.x * ROWS + threadIdx.x / TPR;
   if (row >= a.rows) return;                           // with several rows a block each is one wavefront's
   const size_t at = (size_t)row * a.d;
-  Pack<T, V> x[NV], w[NV];
+  Pack<T, WHOLE> x[NV], w[NV];
   float sum = 0.f;
 #pragma unroll
   for (int i = 0; i < NV; ++i) {
@@ -113,11 +111,11 @@ __global__ void __launch_bounds__(TPR > 256 ? TPR : 256) norm_kernel(NormArgs a,
 #pragma unroll
     for (int q = 0; q < V; ++q) x[i].v[q] = w[i].v[q] = 0.f;
     if (c < a.d) {
-      x[i].load((const T *)a.X + at + c);
-      w[i].load((const T *)a.weight + c);
+      x[i].load((const T *)a.X + at + c, a.d - c);
+      w[i].load((const T *)a.weight + c, a.d - c);
       if (a.R) {
-        Pack<T, V> r;
-        r.load((const T *)a.R + at + c);
+        Pack<T, WHOLE> r;
+        r.load((const T *)a.R + at + c, a.d - c);
 #pragma unroll
         for (int q = 0; q < V; ++q) x[i].v[q] += r.v[q];
       }
@@ -144,36 +142,36 @@ __global__ void __launch_bounds__(TPR > 256 ? TPR : 256) norm_kernel(NormArgs a,
   for (int i = 0; i < NV; ++i) {
     const int c = (i * TPR + t) * V;
     if (c < a.d) {
-      if (a.S) x[i].store((T *)a.S + at + c);
+      if (a.S) x[i].store((T *)a.S + at + c, a.d - c);
 #pragma unroll
       for (int q = 0; q < V; ++q) x[i].v[q] = x[i].v[q] * rstd * w[i].v[q];
-      if (a.Y) x[i].store((T *)a.Y + at + c);
+      if (a.Y) x[i].store((T *)a.Y + at + c, a.d - c);
     }
-    if (a.Y8.values && c < pitch) store8<V>(x[i].v, a.Y8.values + (size_t)row * pitch, a.Y8.exps + (size_t)row * (pitch / BLOCK8), c);
+    if (a.Y8.values && c < pitch) store8(x[i].v, a.Y8.values + (size_t)row * pitch, a.Y8.exps + (size_t)row * (pitch / BLOCK8), c);
   }
 }
 
 // Gradient.  A block's rows (ROWS at a time, TPR threads each) lie gridDim.x * ROWS apart; the next ones are requested before the present ones' sum is
 // taken, so that HBM does not wait for it.  Up to 2048 elements a wavefront has a row to itself and no barrier stands in the loop (8192 rows of
 // 2048 in bf16, with the sum of the parts: 256 threads a row, nothing requested ahead, 45 us; so 30, 134 MB at 4.9 TB/s in the larger kernel).  A block leaves its sum of dweight.
-template <typename T, int V, int TPR, int NV>
+template <typename T, bool WHOLE, int TPR, int NV>
 __global__ void __launch_bounds__(TPR > 256 ? TPR : 256) norm_bwd_kernel(NormBwdArgs a) {
-  constexpr int ROWS = TPR > 256 ? 1 : 256 / TPR;
+  constexpr int V = 8, ROWS = TPR > 256 ? 1 : 256 / TPR;
   constexpr bool LEAN = TPR > 256;       // 128 registers a thread: neither the next row nor the weights are held
   __shared__ float s_sum[16];
   __shared__ float s_dw[ROWS > 1 ? NV * TPR * V : 1];
   const int t = threadIdx.x % TPR, mine = threadIdx.x / TPR;
-  Pack<T, V> w[NV];
+  Pack<T, WHOLE> w[NV];
   float dw[NV][V];
 #pragma unroll
   for (int i = 0; i < NV; ++i) {
     const int c = (i * TPR + t) * V;
 #pragma unroll
     for (int q = 0; q < V; ++q) dw[i][q] = w[i].v[q] = 0.f;
-    if (c < a.d && !LEAN) w[i].load((const T *)a.weight + c);
+    if (c < a.d && !LEAN) w[i].load((const T *)a.weight + c, a.d - c);
   }
   struct Row {
-    Raw<T, V> s[NV], dy[NV], ds[NV];
+    Raw<T, WHOLE> s[NV], dy[NV], ds[NV];
     float rstd;
   };
   auto request = [&](long long row) {
@@ -184,9 +182,9 @@ __global__ void __launch_bounds__(TPR > 256 ? TPR : 256) norm_bwd_kernel(NormBwd
     for (int i = 0; i < NV; ++i) {
       const int c = (i * TPR + t) * V;
       if (c < a.d) {
-        r.s[i].load((const T *)a.S + at + c);
-        r.dy[i].load((const T *)a.dY + at + c);
-        if (a.dS && !LEAN) r.ds[i].load((const T *)a.dS + at + c);
+        r.s[i].load((const T *)a.S + at + c, a.d - c);
+        r.dy[i].load((const T *)a.dY + at + c, a.d - c);
+        if (a.dS && !LEAN) r.ds[i].load((const T *)a.dS + at + c, a.d - c);
       } else {
         r.s[i].clear();
         r.dy[i].clear();
@@ -214,7 +212,7 @@ __global__ void __launch_bounds__(TPR > 256 ? TPR : 256) norm_bwd_kernel(NormBwd
 #pragma unroll
       for (int i = 0; i < NV; ++i) {
         const int c = (i * TPR + t) * V;
-        if (LEAN && c < a.d) w[i].load((const T *)a.weight + c);
+        if (LEAN && c < a.d) w[i].load((const T *)a.weight + c, a.d - c);
 #pragma unroll
         for (int q = 0; q < V; ++q) {
           g[i][q] *= w[i].v[q];
@@ -226,11 +224,11 @@ __global__ void __launch_bounds__(TPR > 256 ? TPR : 256) norm_bwd_kernel(NormBwd
       for (int i = 0; i < NV; ++i) {
         const int c = (i * TPR + t) * V;
         if (c < a.d) {
-          Pack<T, V> o;
-          if (LEAN && a.dS) now.ds[i].load((const T *)a.dS + (size_t)row * a.d + c);
+          Pack<T, WHOLE> o;
+          if (LEAN && a.dS) now.ds[i].load((const T *)a.dS + (size_t)row * a.d + c, a.d - c);
 #pragma unroll
           for (int q = 0; q < V; ++q) o.v[q] = now.rstd * (g[i][q] - u[i][q] * mean) + (a.dS ? now.ds[i].get(q) : 0.f);
-          o.store((T *)a.dX + (size_t)row * a.d + c);
+          o.store((T *)a.dX + (size_t)row * a.d + c, a.d - c);
         }
       }
       if constexpr (!LEAN) now = next;
@@ -264,7 +262,8 @@ __global__ void __launch_bounds__(TPR > 256 ? TPR : 256) norm_bwd_kernel(NormBwd
     const int c = (i * TPR + t) * V;
     if (c < a.d) {
 #pragma unroll
-      for (int q = 0; q < V; ++q) part[c + q] = dw[i][q];
+      for (int q = 0; q < V; ++q)
+        if (WHOLE || c + q < a.d) part[c + q] = dw[i][q];
     }
   }
 }
@@ -289,48 +288,31 @@ template <typename T> __global__ void __launch_bounds__(1024) norm_dweight_kerne
   if (threadIdx.x < 16 && c < d) dweight[c] = from_f32<T>(sum);
 }
 
-// The shape for rows of d elements: eight at a time where rows start on 16-byte lines, else one.
-template <typename T, typename F> void by_shape(int d, F f) {
-  using std::integral_constant;
-  auto go = [&](auto v, auto tpr, auto nv) { f(v, tpr, nv); };
-  if (d % 8 == 0) {
-    integral_constant<int, 8> v;
-    const int packs = ceil_div(pitch8(d), 8);
-    if (packs <= 64) go(v, integral_constant<int, 64>{}, integral_constant<int, 1>{});
-    else if (packs <= 128) go(v, integral_constant<int, 64>{}, integral_constant<int, 2>{});
-    else if (packs <= 256) go(v, integral_constant<int, 256>{}, integral_constant<int, 1>{});
-    else if (packs <= 512) go(v, integral_constant<int, 256>{}, integral_constant<int, 2>{});
-    else if (packs <= 1024) go(v, integral_constant<int, 256>{}, integral_constant<int, 4>{});
-    else if (packs <= 2048) go(v, integral_constant<int, 1024>{}, integral_constant<int, 2>{});
-    else go(v, integral_constant<int, 1024>{}, integral_constant<int, 4>{});
-  } else {
-    integral_constant<int, 1> v;
-    const int n = pitch8(d);
-    if (n <= 256) go(v, integral_constant<int, 64>{}, integral_constant<int, 4>{});
-    else if (n <= 1024) go(v, integral_constant<int, 256>{}, integral_constant<int, 4>{});
-    else if (n <= 4096) go(v, integral_constant<int, 256>{}, integral_constant<int, 16>{});
-    else if (n <= 8192) go(v, integral_constant<int, 1024>{}, integral_constant<int, 8>{});
-    else if (n <= 16384) go(v, integral_constant<int, 1024>{}, integral_constant<int, 16>{});
-    else go(v, integral_constant<int, 1024>{}, integral_constant<int, 32>{});
-  }
-}
-// Of the gradient, whose registers hold two rows and the sums: a wavefront a row up to 2048 elements (1024 in ones).
-template <typename T, typename F> void by_bwd_shape(int d, F f) {
+// The shape for rows of d elements.
+template <typename F> void by_shape(int d, F f) {
   using std::integral_constant;
   const int packs = ceil_div(pitch8(d), 8);
-  if (d % 8 == 0 && packs <= 256) {
-    integral_constant<int, 8> v;
-    integral_constant<int, 64> wave;
-    if (packs <= 64) f(v, wave, integral_constant<int, 1>{});
-    else if (packs <= 128) f(v, wave, integral_constant<int, 2>{});
-    else f(v, wave, integral_constant<int, 4>{});
-  } else if (d % 8 && d <= 1024) {
-    integral_constant<int, 1> v;
-    integral_constant<int, 64> wave;
-    if (d <= 256) f(v, wave, integral_constant<int, 4>{});
-    else f(v, wave, integral_constant<int, 16>{});
+  auto go = [&](auto tpr, auto nv) {
+    if (d % 8 == 0) f(std::true_type{}, tpr, nv);
+    else f(std::false_type{}, tpr, nv);
+  };
+  if (packs <= 64) go(integral_constant<int, 64>{}, integral_constant<int, 1>{});
+  else if (packs <= 128) go(integral_constant<int, 64>{}, integral_constant<int, 2>{});
+  else if (packs <= 256) go(integral_constant<int, 256>{}, integral_constant<int, 1>{});
+  else if (packs <= 512) go(integral_constant<int, 256>{}, integral_constant<int, 2>{});
+  else if (packs <= 1024) go(integral_constant<int, 256>{}, integral_constant<int, 4>{});
+  else if (packs <= 2048) go(integral_constant<int, 1024>{}, integral_constant<int, 2>{});
+  else go(integral_constant<int, 1024>{}, integral_constant<int, 4>{});
+}
+// Of the gradient, whose registers hold two rows and the sums: a wavefront a row up to 2048 elements.
+template <typename F> void by_bwd_shape(int d, F f) {
+  using std::integral_constant;
+  const int packs = ceil_div(pitch8(d), 8);
+  if (packs > 128 && packs <= 256) {
+    if (d % 8 == 0) f(std::true_type{}, integral_constant<int, 64>{}, integral_constant<int, 4>{});
+    else f(std::false_type{}, integral_constant<int, 64>{}, integral_constant<int, 4>{});
   } else {
-    by_shape<T>(d, f);
+    by_shape(d, f);
   }
 }
 constexpr int BWD_BLOCKS = 512;
@@ -351,9 +333,9 @@ template <typename T> int launch_norm_as(hipStream_t s, const NormArgs &all) {
       a.Y8.values += (size_t)first * pitch;
       a.Y8.exps += (size_t)first * (pitch / BLOCK8);
     }
-    by_shape<T>(a.d, [&](auto v, auto tpr, auto nv) {
+    by_shape(a.d, [&](auto whole, auto tpr, auto nv) {
       constexpr int TPR = decltype(tpr)::value, ROWS = TPR > 256 ? 1 : 256 / TPR;
-      hipLaunchKernelGGL((norm_kernel<T, decltype(v)::value, TPR, decltype(nv)::value>), dim3(ceil_div(a.rows, ROWS)), dim3(TPR > 256 ? TPR : 256), 0, s, a,
+      hipLaunchKernelGGL((norm_kernel<T, decltype(whole)::value, TPR, decltype(nv)::value>), dim3(ceil_div(a.rows, ROWS)), dim3(TPR > 256 ? TPR : 256), 0, s, a,
                          pitch);
     });
     SMOE_LAUNCH_CHECK();
@@ -363,9 +345,9 @@ template <typename T> int launch_norm_as(hipStream_t s, const NormArgs &all) {
 template <typename T> int launch_norm_bwd_as(hipStream_t s, const NormBwdArgs &a) {
   const int parts = norm_bwd_parts(SMOE_BF16, a.rows, a.d);
   if (a.rows > 0) {
-    by_bwd_shape<T>(a.d, [&](auto v, auto tpr, auto nv) {
+    by_bwd_shape(a.d, [&](auto whole, auto tpr, auto nv) {
       constexpr int TPR = decltype(tpr)::value;
-      hipLaunchKernelGGL((norm_bwd_kernel<T, decltype(v)::value, TPR, decltype(nv)::value>), dim3(parts), dim3(TPR > 256 ? TPR : 256), 0, s, a);
+      hipLaunchKernelGGL((norm_bwd_kernel<T, decltype(whole)::value, TPR, decltype(nv)::value>), dim3(parts), dim3(TPR > 256 ? TPR : 256), 0, s, a);
     });
     SMOE_LAUNCH_CHECK();
   }
@@ -379,7 +361,7 @@ template <typename T> int launch_norm_bwd_as(hipStream_t s, const NormBwdArgs &a
 int launch_norm(hipStream_t s, smoe_dtype dt, const NormArgs &a) { return dt == SMOE_BF16 ? launch_norm_as<bf16_t>(s, a) : launch_norm_as<float>(s, a); }
 int norm_bwd_parts(smoe_dtype, int rows, int d) {
   int per = 1;                   // rows a block has at a time
-  by_bwd_shape<float>(d, [&](auto, auto tpr, auto) { per = decltype(tpr)::value > 256 ? 1 : 256 / decltype(tpr)::value; });
+  by_bwd_shape(d, [&](auto, auto tpr, auto) { per = decltype(tpr)::value > 256 ? 1 : 256 / decltype(tpr)::value; });
   const int blocks = ceil_div(rows, per);
   return blocks < BWD_BLOCKS ? blocks : BWD_BLOCKS;
 }
