@@ -1,7 +1,7 @@
 // The root-mean-square norm of the residual stream with the addition in front of it, its gradient, and its output in 8 bits.
 // Bound: HBM, each tensor read or written once; a row stays in registers between its sum and its output.  Rows of 2048 in bf16, 8192 of them: forward 22.5 us
-// (134 MB, 6.0 TB/s), with 8 bits besides 27.5, 8 bits only 21, gradient 30 (4.5 TB/s); 8191 of 4096: 46, 57, 44, 51; 4000 of 5001, one element at a time
-// since rows start off the 16-byte lines: 66 (2.4 TB/s) and 85.
+// (134 MB, 6.0 TB/s), with 8 bits besides 27.5, 8 bits only 21, gradient 30 (4.5 TB/s); 8191 of 4096: 46, 57, 44, 51; 4000 of 5001, whose rows start off the
+// 16-byte lines: 42 (3.8 TB/s), 46, 40, 74 (loads of single elements: 66, 80, 69, 85).
 #include "block.h"
 #include <algorithm>
 #include <type_traits>
@@ -157,7 +157,7 @@ __global__ void __launch_bounds__(TPR > 256 ? TPR : 256) norm_kernel(NormArgs a,
 template <typename T, bool WHOLE, int TPR, int NV>
 __global__ void __launch_bounds__(TPR > 256 ? TPR : 256) norm_bwd_kernel(NormBwdArgs a) {
   constexpr int V = 8, ROWS = TPR > 256 ? 1 : 256 / TPR;
-  constexpr bool LEAN = TPR > 256;       // 128 registers a thread: neither the next row nor the weights are held
+  constexpr bool LEAN = TPR > 512;       // 128 registers a thread: neither the next row nor the weights are held
   __shared__ float s_sum[16];
   __shared__ float s_dw[ROWS > 1 ? NV * TPR * V : 1];
   const int t = threadIdx.x % TPR, mine = threadIdx.x / TPR;
@@ -288,32 +288,38 @@ template <typename T> __global__ void __launch_bounds__(1024) norm_dweight_kerne
   if (threadIdx.x < 16 && c < d) dweight[c] = from_f32<T>(sum);
 }
 
-// The shape for rows of d elements.
-template <typename F> void by_shape(int d, F f) {
-  using std::integral_constant;
-  const int packs = ceil_div(pitch8(d), 8);
-  auto go = [&](auto tpr, auto nv) {
-    if (d % 8 == 0) f(std::true_type{}, tpr, nv);
-    else f(std::false_type{}, tpr, nv);
-  };
-  if (packs <= 64) go(integral_constant<int, 64>{}, integral_constant<int, 1>{});
-  else if (packs <= 128) go(integral_constant<int, 64>{}, integral_constant<int, 2>{});
-  else if (packs <= 256) go(integral_constant<int, 256>{}, integral_constant<int, 1>{});
-  else if (packs <= 512) go(integral_constant<int, 256>{}, integral_constant<int, 2>{});
-  else if (packs <= 1024) go(integral_constant<int, 256>{}, integral_constant<int, 4>{});
-  else if (packs <= 2048) go(integral_constant<int, 1024>{}, integral_constant<int, 2>{});
-  else go(integral_constant<int, 1024>{}, integral_constant<int, 4>{});
-}
-// Of the gradient, whose registers hold two rows and the sums: a wavefront a row up to 2048 elements.
-template <typename F> void by_bwd_shape(int d, F f) {
-  using std::integral_constant;
-  const int packs = ceil_div(pitch8(d), 8);
-  if (packs > 128 && packs <= 256) {
-    if (d % 8 == 0) f(std::true_type{}, integral_constant<int, 64>{}, integral_constant<int, 4>{});
-    else f(std::false_type{}, integral_constant<int, 64>{}, integral_constant<int, 4>{});
-  } else {
-    by_shape(d, f);
+// The shape for rows of d elements: threads a row, packs a thread.
+template <typename F> struct Shapes {
+  int d;
+  F f;
+  template <int TPR, int NV> void go() const {
+    if (d % 8 == 0) f(std::true_type{}, std::integral_constant<int, TPR>{}, std::integral_constant<int, NV>{});
+    else f(std::false_type{}, std::integral_constant<int, TPR>{}, std::integral_constant<int, NV>{});
   }
+};
+template <typename F> void by_shape(int d, F f) {
+  const int packs = ceil_div(pitch8(d), 8);
+  const Shapes<F> s{d, f};
+  if (packs <= 64) s.template go<64, 1>();
+  else if (packs <= 128) s.template go<64, 2>();
+  else if (packs <= 256) s.template go<256, 1>();
+  else if (packs <= 512) s.template go<256, 2>();
+  else if (packs <= 1024) s.template go<256, 4>();
+  else if (packs <= 2048) s.template go<1024, 2>();
+  else s.template go<1024, 4>();
+}
+// Of the gradient, whose registers hold two rows and the sums: a wavefront a row up to 2048 elements, two packs a thread from there on (4096 rows of 8192 in bf16, 256
+// threads of four packs, one block a compute unit: 70 us; 512 of two 65).
+template <typename F> void by_bwd_shape(int d, F f) {
+  const int packs = ceil_div(pitch8(d), 8);
+  const Shapes<F> s{d, f};
+  if (packs <= 64) s.template go<64, 1>();
+  else if (packs <= 128) s.template go<64, 2>();
+  else if (packs <= 256) s.template go<64, 4>();
+  else if (packs <= 512) s.template go<256, 2>();
+  else if (packs <= 1024) s.template go<512, 2>();
+  else if (packs <= 2048) s.template go<1024, 2>();
+  else s.template go<1024, 4>();
 }
 constexpr int BWD_BLOCKS = 512;
 constexpr int LAUNCH_ROWS = 1 << 21;       // a launch has fewer than 2^32 threads
