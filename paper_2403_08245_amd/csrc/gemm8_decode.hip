@@ -1,12 +1,16 @@
 // The products in 8 bits for a few rows per expert: a stream of the used experts' weights past a handful of rows.  Bound: HBM.
 //
-// A wavefront owns 64 columns (four groups of 16) of a tile of up to 32 rows of one expert: v_mfma_scale_f32_16x16x128_f8f6f4 with the weights as the first operand,
-// so that a lane ends up with four consecutive columns of one row.  Weights are laid out as the instruction takes them (smoe_weights8): a
-// step of 128 of the contraction of a group is 2 KB, two loads of 16 bytes a lane, straight to registers; no LDS, no barrier in the loop.
-// Wavefronts of a block stand side by side (CW) or share the contraction (KW) and add their sums through LDS in a fixed order.
+// A wavefront owns 64 columns (four groups of 16) of a tile of up to 32 rows of one expert, with the weights as the first operand, so that a lane ends
+// up with four consecutive columns of one row.  Weights are laid out for it (smoe_weights8): a step of 128 of the contraction of a group is 2 KB, two
+// loads of 16 bytes a lane, straight to registers; no LDS, no barrier in the loop.  Wavefronts of a block stand side by side (CW) or share the
+// contraction (KW) and add their sums through LDS in a fixed order.
 //
-// Operands: lane (r, q) = (lane % 16, lane / 16) holds elements 16 q .. 16 q + 15 and 64 + 16 q .. of row or column r, and the power of two of
-// its elements 32 q .. 32 q + 31.
+// Bare products: v_mfma_scale_f32_16x16x128_f8f6f4, lane (r, q) = (lane % 16, lane / 16) with elements 16 q .. 16 q + 15 and 64 + 16 q .. of row or column r, and
+// the power of two of its elements 32 q .. 32 q + 31.  It adds its 128 products to about 2^-12 of the largest, far under the rounding of what is stored.
+// Hidden rows, which are packed to codes of four bits, would feel that: 1.6e-3 (GELU) to 2.5e-3 (SwiGLU) of the codes came out on the other side of a border, a
+// step of up to an eighth of a value each.  There the codes are widened to bf16, which holds them with their power of two exactly, and multiplied by
+// v_mfma_f32_16x16x32_bf16: four times the matrix time, of which there is enough beside the weights' stream, and sums good to fp32 (under 1e-4 of the codes).
+// Which eight of a lane's elements an instruction takes does not matter, as long as rows and columns give the same.
 #include "block.h"
 #include "mfma_common.h"
 #include <type_traits>
@@ -41,6 +45,27 @@ template <int F> struct Rows {                // one step of the tile's fragment
   unsigned int exps[F];
 };
 __device__ __forceinline__ i32x8 joined(i32x4 lo, i32x4 hi) { return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7); }
+
+// A lane's 32 elements of a step as the values they stand for; `exps`: the bytes of the step's four blocks of 32, the lane's are q / 2 and 2 + q / 2.
+struct Wide {
+  bf16x8 v[4];
+};
+__device__ __forceinline__ Wide widened(i32x8 codes, unsigned int exps, int q) {
+  typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+  const unsigned int mine = exps >> (8 * (q >> 1));
+  const float scale[2] = {__uint_as_float((mine & 0xffu) << 23), __uint_as_float((mine << 7) & 0x7f800000u)};
+  Wide w;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const bf16x2 lo = __builtin_bit_cast(bf16x2, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(codes[i], scale[i >> 2], false));
+    const bf16x2 hi = __builtin_bit_cast(bf16x2, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(codes[i], scale[i >> 2], true));
+    w.v[i >> 1][4 * (i & 1)] = lo[0];
+    w.v[i >> 1][4 * (i & 1) + 1] = lo[1];
+    w.v[i >> 1][4 * (i & 1) + 2] = hi[0];
+    w.v[i >> 1][4 * (i & 1) + 3] = hi[1];
+  }
+  return w;
+}
 
 // ACT: none (out: bf16, or fp32 with WIDE), GELU or SwiGLU (out: packed hidden rows; a tile's columns are then 32 gates and their 32 ups)
 template <int ACT, bool WIDE, int CW, int KW, bool ONCE>
@@ -107,12 +132,26 @@ __global__ void __launch_bounds__(64 * CW * KW, 2) s2s8_decode_kernel(S2S8Args a
 #pragma unroll
       for (int j = 0; j < 4; ++j) acc[m][j] = f32x4{0.f, 0.f, 0.f, 0.f};
     auto multiply = [&](const Weights &w, const Rows<F> &x) {
+      if constexpr (ACT == SMOE_ACT_NONE) {
 #pragma unroll
-      for (int j = 0; j < 4; ++j)
+        for (int j = 0; j < 4; ++j)
 #pragma unroll
-        for (int m = 0; m < F; ++m)
-          acc[m][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(w.v[j], x.v[m], acc[m][j], 0, 0, 0,
-                                                                       (int)(w.exps[j] >> (8 * q)), 0, (int)(x.exps[m] >> (8 * q)));
+          for (int m = 0; m < F; ++m)
+            acc[m][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(w.v[j], x.v[m], acc[m][j], 0, 0, 0,
+                                                                         (int)(w.exps[j] >> (8 * q)), 0, (int)(x.exps[m] >> (8 * q)));
+        return;
+      }
+      Wide xs[F];
+#pragma unroll
+      for (int m = 0; m < F; ++m) xs[m] = widened(x.v[m], x.exps[m], q);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const Wide ws = widened(w.v[j], w.exps[j], q);
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+          for (int m = 0; m < F; ++m) acc[m][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ws.v[i], xs[m].v[i], acc[m][j], 0, 0, 0);
+      }
     };
     // the last steps stand by themselves, so that nothing is requested past the end
     int s = 0;
