@@ -103,7 +103,7 @@ int smoe_plinear8_fwd(smoe_ctx *ctx, void *stream, const smoe_rows8 *X, int x_ro
  * a border between two codes may take either.  The kernels for few rows make that product from bf16 in fp32 (under 1e-4 of the codes differ from the definition's,
  * and Y is as near to it as its rounding allows); those for many rows by the 8-bit instructions (2e-3 of the codes, and Y's error in the root mean square is 1.2 to
  * 1.7 times its rounding's, with most of it in the few tokens whose largest hidden values are concerned).  The second product's rows are summed from fp32 or fp16 with
- * a power of two for 128 columns (bf16 for more than 8192 routed rows on the kernels for few rows).  d_model a multiple of 8, d_expert any. */
+ * a power of two for 64 or 128 columns.  d_model a multiple of 8, d_expert any. */
 size_t smoe_mlp8_fwd_workspace_bytes(smoe_act act, int T, int k, int d_model, int d_expert);
 int smoe_mlp8_fwd(smoe_ctx *ctx, void *stream, smoe_act act, const smoe_rows8 *X, int T, int d_model, int d_expert, const smoe_weights8 *W1,
                   const smoe_weights8 *W2, const smoe_routing *r, int k, const float *gates, void *Y, void *ws, size_t ws_bytes);

@@ -38,7 +38,8 @@ static inline int groups8(int d_out, int halves) { return halves * 2 * ceil_div(
 int launch_rows8_pack(hipStream_t s, smoe_dtype dt, const void *X, int rows, int d, const smoe_rows8 &out);
 int launch_rows8_unpack(hipStream_t s, smoe_dtype dt, const smoe_rows8 &in, int rows, int d, void *X);
 // Y[t] = sum_j g[t k + j] Yhat[t k + j] of rows as S2S8Args has them with C_exps, rounded to bf16 once
-int launch_combine_f16(hipStream_t s, const void *Yhat, const uint8_t *exps, const float *g, void *Y, int T, int k, int d);
+// (exp_cols: the columns that share a power of two, 64 or 128)
+int launch_combine_f16(hipStream_t s, const void *Yhat, const uint8_t *exps, int exp_cols, const float *g, void *Y, int T, int k, int d);
 int launch_weights8_pack(hipStream_t s, smoe_dtype dt, const void *W, const smoe_weights8 &out);
 
 // ---- products (gemm8_decode.hip, gemm8_stream.hip)
@@ -49,7 +50,8 @@ struct S2S8Args {
   RowMap a_map, c_map;
   const int32_t *offsets;
   int Tk;
-  // [*, d_out] bf16; few rows, with `wide`: fp32; many rows, with C_exps [Tk, ceil(d_out / 128)]: fp16 times 2^(exponent - 141), one for 128 columns of a row
+  // [*, d_out] bf16; few rows, with `wide`: fp32; with C_exps [Tk, ceil(d_out / n)]: fp16 times 2^(exponent - 141), one for n columns of a row, n = 64 for few
+  // rows and 128 for many
   void *C = nullptr;
   bool wide = false;
   uint8_t *C_exps = nullptr;

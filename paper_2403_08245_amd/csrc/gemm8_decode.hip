@@ -23,6 +23,7 @@ constexpr int DM = 32;
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef int i32x4 __attribute__((ext_vector_type(4)));
 typedef int i32x8 __attribute__((ext_vector_type(8)));
+typedef _Float16 f16x4 __attribute__((ext_vector_type(4)));
 typedef __amdgpu_buffer_rsrc_t window_t;
 
 // 16-byte and 4-byte loads of a window: the lane's offset in a register, the rest of the address in a scalar one.  ONCE: kept by no cache.
@@ -67,8 +68,10 @@ __device__ __forceinline__ Wide widened(i32x8 codes, unsigned int exps, int q) {
   return w;
 }
 
-// ACT: none (out: bf16, or fp32 with WIDE), GELU or SwiGLU (out: packed hidden rows; a tile's columns are then 32 gates and their 32 ups)
-template <int ACT, bool WIDE, int CW, int KW, bool ONCE>
+enum { ROWS_BF16, ROWS_F32, ROWS_F16 };       // ROWS_F16: with a power of two for 64 columns
+
+// ACT: none (out: rows as OUT says), GELU or SwiGLU (out: packed hidden rows; a tile's columns are then 32 gates and their 32 ups)
+template <int ACT, int OUT, int CW, int KW, bool ONCE>
 __global__ void __launch_bounds__(64 * CW * KW, 2) s2s8_decode_kernel(S2S8Args a, int n_chunks, int groups, int steps, int pitch, int h_pitch) {
   __shared__ float s_part[KW > 1 ? KW - 1 : 1][CW][32][64];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
@@ -207,12 +210,31 @@ __global__ void __launch_bounds__(64 * CW * KW, 2) s2s8_decode_kernel(S2S8Args a
       const int i = row0 + m * 16 + r;
       if constexpr (ACT == SMOE_ACT_NONE) {
         const size_t dst = i < row_end ? (size_t)map_row(a.c_map, i) : 0;
+        float scale = 1.0f;
+        if constexpr (OUT == ROWS_F16) {
+          // The largest finite value of the row's 64 columns goes into [2^14, 2^15): exponents as in gemm8_stream.hip
+          float most = 0.f;
+#pragma unroll
+          for (int j = 0; j < 4; ++j)
+#pragma unroll
+            for (int c = 0; c < 4; ++c) most = fmaxf(most, finite_abs(acc[m][j][c]));
+          most = fmaxf(most, __shfl_xor(most, 16, 64));
+          most = fmaxf(most, __shfl_xor(most, 32, 64));
+          const unsigned int e = max(__float_as_uint(most) >> 23, 15u);
+          scale = __uint_as_float((268u - e) << 23);
+          if (q == 0 && i < row_end && tile * 64 < a.W.d_out) a.C_exps[dst * ((a.W.d_out + 63) / 64) + tile] = (uint8_t)e;
+        }
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
           const int col = group(j) * 16 + 4 * q;
           if (i >= row_end || col >= a.W.d_out) continue;
-          if constexpr (WIDE) {
+          if constexpr (OUT == ROWS_F32) {
             *reinterpret_cast<f32x4 *>((float *)a.C + dst * a.W.d_out + col) = acc[m][j];
+          } else if constexpr (OUT == ROWS_F16) {
+            f16x4 v;
+#pragma unroll
+            for (int c = 0; c < 4; ++c) v[c] = (_Float16)(acc[m][j][c] * scale);
+            *reinterpret_cast<f16x4 *>((_Float16 *)a.C + dst * a.W.d_out + col) = v;
           } else {
             bf16x4 v;
 #pragma unroll
@@ -267,7 +289,7 @@ __global__ void __launch_bounds__(64 * CW * KW, 2) s2s8_decode_kernel(S2S8Args a
   }
 }
 
-template <int ACT, bool WIDE, int CW, int KW> int launch_as(hipStream_t s, const S2S8Args &a) {
+template <int ACT, int OUT, int CW, int KW> int launch_as(hipStream_t s, const S2S8Args &a) {
   const int groups = groups8(a.W.d_out, a.W.halves), steps = ceil_div(a.W.d_in, ROW8), h_pitch = pitch8(a.W.d_out / a.W.halves);
   const int units = ACT == SMOE_ACT_SWIGLU ? h_pitch / 32 : ACT ? h_pitch / 64 : ceil_div(groups, 4);     // of a wavefront each
   const int n_chunks = ceil_div(units, CW);
@@ -277,9 +299,9 @@ template <int ACT, bool WIDE, int CW, int KW> int launch_as(hipStream_t s, const
   // past: 64 tokens on 64 experts, 2048 -> 2 x 512 -> 2048 (208 MB each) 46.3 / 44.7; 32 tokens on 16 experts, 4096 -> 2 x 1024 -> 4096 (208 MB) 48 / 45.3; 64
   // tokens on 8 experts, 1024 -> 2 x 2816 -> 1024 (71 MB) 26 / 30.
   if (a.call_weights > LAST_LEVEL_CACHE / 2)
-    hipLaunchKernelGGL((s2s8_decode_kernel<ACT, WIDE, CW, KW, true>), grid, block, 0, s, a, n_chunks, groups, steps, pitch8(a.W.d_in), h_pitch);
+    hipLaunchKernelGGL((s2s8_decode_kernel<ACT, OUT, CW, KW, true>), grid, block, 0, s, a, n_chunks, groups, steps, pitch8(a.W.d_in), h_pitch);
   else
-    hipLaunchKernelGGL((s2s8_decode_kernel<ACT, WIDE, CW, KW, false>), grid, block, 0, s, a, n_chunks, groups, steps, pitch8(a.W.d_in), h_pitch);
+    hipLaunchKernelGGL((s2s8_decode_kernel<ACT, OUT, CW, KW, false>), grid, block, 0, s, a, n_chunks, groups, steps, pitch8(a.W.d_in), h_pitch);
   SMOE_LAUNCH_CHECK();
   return SMOE_OK;
 }
@@ -289,21 +311,22 @@ template <int ACT, bool WIDE, int CW, int KW> int launch_as(hipStream_t s, const
 // Groups of columns that lie an odd number of 32 KB apart get in one another's way when 16 of them are read in step, with up to 16 rows an expert: 64 tokens on 64
 // experts, k = 8, -> 8192: 2048 206 / 191 / 174, 1024 105 / 95 / 108, 4096 wide (-> 4096) 183 / 207 / 195, 1920 (-> 4096) 94.5 / 95.3 / 97.5.  (Wavefronts that begin
 // at different steps of the contraction gained 0 to 4 % there and cost others up to 40 %.)
-template <int ACT, bool WIDE> int launch(hipStream_t s, const S2S8Args &a) {
+template <int ACT, int OUT> int launch(hipStream_t s, const S2S8Args &a) {
   const long long experts = a.Tk < a.W.E ? a.Tk : a.W.E, units = a.W.d_out / 64;
   const int steps = ceil_div(a.W.d_in, ROW8);
   const bool thin = a.Tk <= 16 * experts;
   int shares = experts * units >= 8 * a.grid ? 1 : experts * units >= 4 * a.grid ? 2 : 4;
   if (shares == 1 && thin) shares = steps % 32 == 16 ? 4 : steps % 16 == 8 ? 2 : 1;
-  if (shares == 1) return launch_as<ACT, WIDE, 4, 1>(s, a);
-  if (shares == 2) return launch_as<ACT, WIDE, 2, 2>(s, a);
-  return launch_as<ACT, WIDE, 1, 4>(s, a);
+  if (shares == 1) return launch_as<ACT, OUT, 4, 1>(s, a);
+  if (shares == 2) return launch_as<ACT, OUT, 2, 2>(s, a);
+  return launch_as<ACT, OUT, 1, 4>(s, a);
 }
 
 }  // namespace
 
 int launch_s2s8_decode(hipStream_t s, const S2S8Args &a) {
-  if (a.act == SMOE_ACT_SWIGLU) return launch<SMOE_ACT_SWIGLU, false>(s, a);
-  if (a.act == SMOE_ACT_GELU) return launch<SMOE_ACT_GELU, false>(s, a);
-  return a.wide ? launch<SMOE_ACT_NONE, true>(s, a) : launch<SMOE_ACT_NONE, false>(s, a);
+  if (a.act == SMOE_ACT_SWIGLU) return launch<SMOE_ACT_SWIGLU, ROWS_BF16>(s, a);
+  if (a.act == SMOE_ACT_GELU) return launch<SMOE_ACT_GELU, ROWS_BF16>(s, a);
+  if (a.wide) return launch<SMOE_ACT_NONE, ROWS_F32>(s, a);
+  return a.C_exps ? launch<SMOE_ACT_NONE, ROWS_F16>(s, a) : launch<SMOE_ACT_NONE, ROWS_BF16>(s, a);
 }

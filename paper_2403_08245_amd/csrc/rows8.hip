@@ -78,7 +78,7 @@ __global__ void __launch_bounds__(256) rows8_unpack_kernel(smoe_rows8 in, long l
 // The weighted sum of k slots' rows, eight columns a thread; up to K rows in flight, read past the caches (each once).
 template <int K>
 __global__ void __launch_bounds__(256) combine_f16_kernel(const uint4 *__restrict__ Yhat, const uint8_t *__restrict__ exps, const float *__restrict__ g, bf16_t *__restrict__ Y,
-                                                          long long chunks, int k, int per_row, int exps_row) {
+                                                          long long chunks, int k, int per_row, int exps_row, int exp_chunks) {
   typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
   typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
   typedef bf16_t bf16x8 __attribute__((ext_vector_type(8)));
@@ -86,7 +86,7 @@ __global__ void __launch_bounds__(256) combine_f16_kernel(const uint4 *__restric
     const long long t = i / per_row;
     const int c = (int)(i - t * per_row);
     const u32x4 *src = reinterpret_cast<const u32x4 *>(Yhat) + t * k * per_row + c;
-    const uint8_t *e = exps + t * k * exps_row + c / 16;
+    const uint8_t *e = exps + t * k * exps_row + c / exp_chunks;
     const float *w = g + t * k;
     float acc[8];
 #pragma unroll
@@ -178,11 +178,11 @@ int launch_rows8_unpack(hipStream_t s, smoe_dtype dt, const smoe_rows8 &in, int 
   SMOE_LAUNCH_CHECK();
   return SMOE_OK;
 }
-int launch_combine_f16(hipStream_t s, const void *Yhat, const uint8_t *exps, const float *g, void *Y, int T, int k, int d) {
+int launch_combine_f16(hipStream_t s, const void *Yhat, const uint8_t *exps, int exp_cols, const float *g, void *Y, int T, int k, int d) {
   const int per_row = d / 8;
   const long long chunks = (long long)T * per_row;
   const dim3 grid(row_blocks(chunks)), block(256);
-  auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, block, 0, s, (const uint4 *)Yhat, exps, g, (bf16_t *)Y, chunks, k, per_row, ceil_div(d, 128)); };
+  auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, block, 0, s, (const uint4 *)Yhat, exps, g, (bf16_t *)Y, chunks, k, per_row, ceil_div(d, exp_cols), exp_cols / 8); };
   if (k == 1) go(combine_f16_kernel<1>);
   else if (k == 2) go(combine_f16_kernel<2>);
   else if (k <= 4) go(combine_f16_kernel<4>);

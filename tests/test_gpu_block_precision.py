@@ -107,3 +107,39 @@ def test_every_row_of_both_kernels(smoe, mode, T, d_model, d_expert, E, k, act):
         Y[m] = _f64(smoe.mlp8_fwd(rows, *packed, r, k, g, code))
     _close_by_rows(Y[mode], Y[FEW], "Y")
     assert _rms(Y[mode] - Y[FEW]) / _rms(Y[FEW]) <= WHOLE[mode] + WHOLE[FEW]
+
+
+def test_many_routed_rows_on_the_kernels_for_few(smoe):
+    """More routed rows than the layer sums from fp32 (8192): no rounding to bf16 between the second product and the sum.  Values of one sign and logarithm spread evenly are off by
+    2^-7 / sqrt(12) sqrt(0.375 / ln 2) = 1.66e-3 after one rounding to bf16, 2.35e-3 after two; fp16 rows add 2.1e-4, hidden codes 0.8e-3."""
+    T, d_model, d_expert, E, k = 4200, 264, 96, 6, 2
+    _log("rms of many rows on the kernels for few")
+    idx, gates, r, code, X, W1, W2, packed = _mlp_case(smoe, T, d_model, d_expert, E, k, "swiglu", seed=121)
+    smoe.set_kernel_mode(FEW)
+    Y = smoe.mlp8_fwd(smoe.rows8_pack(X.cuda()), *packed, r, k, torch.from_numpy(gates).cuda(), code)
+    sample = np.arange(0, T, 13)
+    x = oracle.unpack8(*oracle.pack8(_f64(X[sample])), d_model)
+    want, _ = oracle.mlp8(x, _stored(smoe, W1), _stored(smoe, W2), idx[sample], gates[sample].astype(np.float64), code)
+    got = _f64(Y[torch.from_numpy(sample).cuda()])
+    _close_by_rows(got, want, "Y")
+    assert _rms(got - want) / _rms(want) <= 1.9e-3
+
+
+@pytest.mark.parametrize("d_model", [256, 72])
+def test_many_rows_of_all_sizes_on_the_kernels_for_few(smoe, d_model):
+    """Rows from 2^-60 to 2^30, as many as are summed from fp16 with a power of two for 64 columns; a row of NaN, and one of products past fp32."""
+    T, E, k = 4200, 3, 2
+    idx, gates, r, code, X, W1, W2, packed = _mlp_case(smoe, T, d_model, 160, E, k, "swiglu", seed=131)
+    X = (X.float() * 2.0 ** torch.linspace(-60, 30, T).round()[:, None]).to(torch.bfloat16)
+    X[77, 3] = float("nan")
+    X[1234] = 1e30
+    smoe.set_kernel_mode(FEW)
+    Y = smoe.mlp8_fwd(smoe.rows8_pack(X.cuda()), *packed, r, k, torch.from_numpy(gates).cuda(), code)
+    sample = np.array([t for t in range(0, T, 21) if t not in (77, 1234)])
+    x = oracle.unpack8(*oracle.pack8(_f64(X[sample])), d_model)
+    with np.errstate(over="ignore"):
+        want, _ = oracle.mlp8(x, _stored(smoe, W1), _stored(smoe, W2), idx[sample], gates[sample].astype(np.float64), code)
+    got = _f64(Y[torch.from_numpy(sample).cuda()])
+    off, size = _pieces(got - want), _pieces(want)
+    assert (off <= ONE * size + 1e-37).all()                # under 1e-37 fp32 has fewer bits
+    assert torch.isnan(Y[77]).all() and torch.isfinite(Y[[76, 78, 1233, 1235]]).all()
