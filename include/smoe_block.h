@@ -22,7 +22,8 @@ extern "C" {
  *      where it has fewer), and the kept_groups largest stay, ties to the lower group.
  *   3. The k largest ranks of the experts in them are kept, ties to the lower expert id, slots by descending rank.
  *   4. gates[t,j] = scale * s[e_j], divided by the sum of the k kept scores with `renormalise`.
- * The choice is made as 64-bit scores make it; gates are fp32.  A masked expert, whose logit is NaN or -inf, has score 0 and comes behind
+ * Ranks that are scores alone (no bias, and groups that count by one expert or all stay) are compared as the exact scores are, which is as the logits are;
+ * others, and sums of two, as 64-bit numbers, in which scores may be equal whose logits are not (sigmoids of logits over 37 are 1).  Gates are fp32.  A masked expert, whose logit is NaN or -inf, has score 0 and comes behind
  * every other of the kept groups, whatever its bias; so does one whose rank is NaN or -inf.  Such experts count nothing towards their
  * group, and a group of nothing else comes last.  Logits of +inf share the softmax equally, as do the logits of a row that are all masked; kept scores that
  * are all 0 share `scale` equally under `renormalise`.  Every slot of every token is written. */

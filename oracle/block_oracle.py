@@ -46,8 +46,8 @@ def score_gate(logits, k, score="softmax", bias=None, groups=1, kept_groups=1, g
         with np.errstate(invalid="ignore"):
             rank = s + (0.0 if bias is None else np.asarray(bias, dtype=np.float64))
         rank[np.isnan(rank) | (x == -np.inf)] = -np.inf
-        if bias is None and group_best == 1:
-            rank = x                                            # the same order, where scores are too close to 1 or 0 to show it
+        if bias is None and (group_best == 1 or kept_groups == groups):
+            rank = x                                            # exact scores compared: 64 bits do not hold those next to 1 or 0 apart
         worth = []
         for g in range(groups):
             live = sorted((r for r in rank[g * per:(g + 1) * per] if r > -np.inf), reverse=True)[:group_best]

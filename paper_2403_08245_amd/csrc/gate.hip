@@ -2,9 +2,9 @@
 // a wavefront: many experts, large k, and every token whose choice fp32 cannot tell).  Bound: the rounds of the selection, then reading the logits and writing
 // their gradient (32768 tokens of 256 experts in groups, k = 8: 22.3 us forward, where its logits take 6.7; 9.8 backward, 34 MB written, 3.6 TB/s).
 //
-// The choice is that of 64-bit scores: with a bias or sums of two, ranks of different experts come within 32-bit rounding of one another once in some
-// thousand tokens, and which one is taken would then hang on how the exponential was rounded.  Where the order of the scores is that of the
-// logits (no bias, groups that count by their best), the logits themselves are compared.
+// The choice is that of 64-bit ranks: with a bias or sums of two, ranks of different experts come within 32-bit rounding of one another once in some
+// thousand tokens, and which one is taken would then hang on how the exponential was rounded.  Where ranks are scores alone (no bias, and groups that count by
+// their best or all stay) the logits themselves are compared, which is the order of the exact scores.
 #include "block.h"
 #include <limits.h>
 #include <type_traits>
