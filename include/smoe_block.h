@@ -81,6 +81,8 @@ int smoe_weights8_pack(smoe_ctx *ctx, void *stream, smoe_dtype dtype, const void
  *   X, R [rows, d], weight [d] of one dtype (F32 or BF16; R NULL: s = x).  Sums are fp32, and y is made from the unrounded s.
  *   S [rows, d] (out, nullable): s rounded once, the stream that goes on.  Y [rows, d] and Y8 (out, either may be NULL, not both): y in the
  *   dtype, and in 8 bits (packed from the unrounded y).  rstd [rows] fp32 (out, nullable): kept for the backward pass.
+ * Squares that leave fp32's range at either end are no loss: y is that of the formula for every finite s and every eps, 0 included (rows of zeros are then 0 / 0); an rstd past
+ * fp32's range, of rows under 2^-127, is kept as infinity, and the backward pass of such rows is not finite.
  * S and Y may be X or R themselves; any other overlap of an output with an input or output is SMOE_ERR_INVALID_ARG.  1 <= d <= 32768, else
  * SMOE_ERR_UNSUPPORTED; eps >= 0. */
 int smoe_add_norm_fwd(smoe_ctx *ctx, void *stream, smoe_dtype dtype, const void *X, const void *R, const void *weight, int rows, int d, float eps,

@@ -124,27 +124,30 @@ __global__ void __launch_bounds__(TPR > 256 ? TPR : 256) norm_kernel(NormArgs a,
     for (int q = 0; q < V; ++q) sum = fmaf(x[i].v[q], x[i].v[q], sum);
   }
   sum = row_sum<TPR>(sum, s_sum);
-  float rstd = 1.0f / sqrtf(sum / (float)a.d + a.eps);
-  if (!(sum < INFINITY)) {                             // squares past fp32's range: the same of values 2^-70 as large
+  float rstd = 1.0f / sqrtf(sum / (float)a.d + a.eps), by = 1.0f;      // y = s by rstd weight
+  // Squares past fp32's range, or so far under 1 that they lose bits or vanish, with an eps that does not hide that: the same of values `by` times as large.
+  const bool large = !(sum < INFINITY);
+  if (large || (sum < (float)a.d * 0x1p-100f && a.eps < 0x1p-80f)) {
+    by = large ? 0x1p-70f : 0x1p100f;
     sum = 0.f;
 #pragma unroll
     for (int i = 0; i < NV; ++i)
 #pragma unroll
       for (int q = 0; q < V; ++q) {
-        const float y = x[i].v[q] * 0x1p-70f;
+        const float y = x[i].v[q] * by;
         sum = fmaf(y, y, sum);
       }
     sum = row_sum<TPR>(sum, s_sum);
-    rstd = 0x1p-70f / sqrtf(sum / (float)a.d);
+    rstd = 1.0f / sqrtf(sum / (float)a.d + a.eps * by * by);
   }
-  if (a.rstd && t == 0) a.rstd[row] = rstd;
+  if (a.rstd && t == 0) a.rstd[row] = by * rstd;
 #pragma unroll
   for (int i = 0; i < NV; ++i) {
     const int c = (i * TPR + t) * V;
     if (c < a.d) {
       if (a.S) x[i].store((T *)a.S + at + c, a.d - c);
 #pragma unroll
-      for (int q = 0; q < V; ++q) x[i].v[q] = x[i].v[q] * rstd * w[i].v[q];
+      for (int q = 0; q < V; ++q) x[i].v[q] = x[i].v[q] * by * rstd * w[i].v[q];
       if (a.Y) x[i].store((T *)a.Y + at + c, a.d - c);
     }
     if (a.Y8.values && c < pitch) store8(x[i].v, a.Y8.values + (size_t)row * pitch, a.Y8.exps + (size_t)row * (pitch / BLOCK8), c);
