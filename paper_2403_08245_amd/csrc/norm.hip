@@ -127,7 +127,7 @@ __global__ void __launch_bounds__(TPR > 256 ? TPR : 256) norm_kernel(NormArgs a,
   float rstd = 1.0f / sqrtf(sum / (float)a.d + a.eps), by = 1.0f;      // y = s by rstd weight
   // Squares past fp32's range, or so far under 1 that they lose bits or vanish, with an eps that does not hide that: the same of values `by` times as large.
   const bool large = !(sum < INFINITY);
-  if (large || (sum < (float)a.d * 0x1p-100f && a.eps < 0x1p-80f)) {
+  if (__builtin_expect(large || (sum < (float)a.d * 0x1p-100f && a.eps < 0x1p-80f), 0)) {
     by = large ? 0x1p-70f : 0x1p100f;
     sum = 0.f;
 #pragma unroll
@@ -149,6 +149,10 @@ __global__ void __launch_bounds__(TPR > 256 ? TPR : 256) norm_kernel(NormArgs a,
 #pragma unroll
       for (int q = 0; q < V; ++q) x[i].v[q] = x[i].v[q] * by * rstd * w[i].v[q];
       if (a.Y) x[i].store((T *)a.Y + at + c, a.d - c);
+      if (!WHOLE && c + V > a.d) {                     // 0 by an rstd of NaN or infinity is no zero
+#pragma unroll
+        for (int q = 0; q < V; ++q) x[i].v[q] = c + q < a.d ? x[i].v[q] : 0.f;
+      }
     }
     if (a.Y8.values && c < pitch) store8(x[i].v, a.Y8.values + (size_t)row * pitch, a.Y8.exps + (size_t)row * (pitch / BLOCK8), c);
   }
