@@ -96,8 +96,8 @@ __device__ __forceinline__ void store8(const float (&y)[8], uint8_t *values, uin
 
 // TPR threads a row, NV packs of eight elements each; rows wider than that are another instantiation's.
 template <typename T, bool WHOLE, int TPR, int NV>
-__global__ void __launch_bounds__(TPR > 256 ? TPR : 256) norm_kernel(NormArgs a, int pitch) {
-  constexpr int V = 8, ROWS = TPR > 256 ? 1 : 256 / TPR;
+__global__ void __launch_bounds__(TPR > 64 ? TPR : 256) norm_kernel(NormArgs a, int pitch) {
+  constexpr int V = 8, ROWS = TPR > 64 ? 1 : 256 / TPR;
   __shared__ float s_sum[16];
   const int t = threadIdx.x % TPR;
   const long long row = (long long)blockIdx.x * ROWS + threadIdx.x / TPR;
@@ -304,10 +304,13 @@ template <typename F> struct Shapes {
     else f(std::false_type{}, std::integral_constant<int, TPR>{}, std::integral_constant<int, NV>{});
   }
 };
-template <typename F> void by_shape(int d, F f) {
+// Two wavefronts a row in fp32, whose packs are two loads each, where in bf16 one holds a row's two packs.  Rows of x and r in us, one / two: fp32, 1999 of 999 9.4 / 9.1 (x
+// alone 6.1 / 5.7), 200 of 700 4.2 / 3.5, 8192 of 1024 24.4 / 23; bf16, 16384 of 777 21.1 / 23.2, 2000 of 1024 4.8 / 4.8.
+template <typename T, typename F> void by_shape(int d, F f) {
   const int packs = ceil_div(pitch8(d), 8);
   const Shapes<F> s{d, f};
   if (packs <= 64) s.template go<64, 1>();
+  else if (packs <= 128 && sizeof(T) == 4) s.template go<128, 1>();
   else if (packs <= 128) s.template go<64, 2>();
   else if (packs <= 256) s.template go<256, 1>();
   else if (packs <= 512) s.template go<256, 2>();
@@ -346,9 +349,9 @@ template <typename T> int launch_norm_as(hipStream_t s, const NormArgs &all) {
       a.Y8.values += (size_t)first * pitch;
       a.Y8.exps += (size_t)first * (pitch / BLOCK8);
     }
-    by_shape(a.d, [&](auto whole, auto tpr, auto nv) {
-      constexpr int TPR = decltype(tpr)::value, ROWS = TPR > 256 ? 1 : 256 / TPR;
-      hipLaunchKernelGGL((norm_kernel<T, decltype(whole)::value, TPR, decltype(nv)::value>), dim3(ceil_div(a.rows, ROWS)), dim3(TPR > 256 ? TPR : 256), 0, s, a,
+    by_shape<T>(a.d, [&](auto whole, auto tpr, auto nv) {
+      constexpr int TPR = decltype(tpr)::value, ROWS = TPR > 64 ? 1 : 256 / TPR;
+      hipLaunchKernelGGL((norm_kernel<T, decltype(whole)::value, TPR, decltype(nv)::value>), dim3(ceil_div(a.rows, ROWS)), dim3(TPR > 64 ? TPR : 256), 0, s, a,
                          pitch);
     });
     SMOE_LAUNCH_CHECK();
