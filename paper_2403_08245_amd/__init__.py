@@ -788,7 +788,15 @@ def momha_decode(X, W_K, W_V, W_Q, W_O, r: Routing, k: int, gates, cache: KVCach
 
 
 # ---- the block around the experts (include/smoe_block.h) ------------------------------------------------------------------
+def _held(*numbers: int):
+    """Numbers that come from the caller as they are: none that 32 bits would cut down to another."""
+    for n in numbers:
+        if not -INT_MAX <= n <= INT_MAX:
+            raise ValueError(f"{n} does not fit 32 bits")
+
+
 SCORES = {"softmax": 0, "sigmoid": 1}
+FLOAT_MAX = (2 - 2.0 ** -23) * 2.0 ** 127
 
 
 class GateRule(_Fixed):
@@ -797,6 +805,9 @@ class GateRule(_Fixed):
     def __init__(self, score: str, groups: int, kept_groups: int, group_best: int, renormalise: bool, scale: float):
         if score not in SCORES:
             raise ValueError(f"score {score!r}")
+        _held(groups, kept_groups, group_best)
+        if not abs(scale) <= FLOAT_MAX:
+            raise ValueError(f"scale {scale} is not a finite number of 32 bits")
         self.__dict__.update(score=score, groups=groups, kept_groups=kept_groups, group_best=group_best, renormalise=renormalise, scale=scale,
                              _c=ctypes.byref(smoe_gate_rule(SCORES[score], groups, kept_groups, group_best, int(renormalise), scale)))
 
@@ -910,6 +921,7 @@ class Weights8(_Fixed):
     def __init__(self, values: torch.Tensor, exps: torch.Tensor, E: int, d_in: int, d_out: int, halves: int):
         for t in (values, exps):
             _chk(t, torch.uint8)
+        _held(E, d_in, d_out, halves)
         nb = lib.smoe_weights8_bytes(E, d_in, d_out, halves)
         if not nb or values.numel() != nb or exps.numel() * 32 != nb or exps.device != values.device:
             raise ValueError("weights in 8 bits must be values of smoe_weights8_bytes and a 32nd as many exps, on one device")
@@ -924,6 +936,7 @@ def weights8(W: torch.Tensor, halves: int = 1) -> Weights8:
     if W.dim() != 3 or max(W.shape) > INT_MAX:
         raise ValueError("weights must be [E, d_in, d_out]")
     E, d_in, d_out = W.shape
+    _held(halves)
     nb = lib.smoe_weights8_bytes(E, d_in, d_out, halves)
     if not nb:
         raise ValueError(f"no layout for {E} experts of {d_in} x {d_out} in {halves} halves")
@@ -1028,6 +1041,7 @@ def plinear8_fwd(X: Rows8, W: Weights8, r: Routing, k: int, gates=None, grouped_
     dev = _device(X.values)
     _rows_on(dev, X)
     _experts8(dev, r, W)
+    _held(k)
     if X.d != W.d_in:
         raise ValueError("rows and weights differ in d_in")
     Y, gk = None, 0
@@ -1050,6 +1064,7 @@ def mlp8_fwd(X: Rows8, W1: Weights8, W2: Weights8, r: Routing, k: int, gates, ac
     dev = _device(X.values)
     _rows_on(dev, X)
     _experts8(dev, r, W1, W2)
+    _held(k, act)
     _here(dev, torch.float32, gates)
     T, d_model, d_expert = X.rows, X.d, W2.d_in
     if W1.d_in != d_model or W2.d_out != d_model or W1.d_out != hidden_width(act, d_expert) or W1.halves != hidden_width(act, 1) or W2.halves != 1:
