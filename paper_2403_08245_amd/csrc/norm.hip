@@ -275,24 +275,25 @@ __global__ void __launch_bounds__(TPR > 256 ? TPR : 256) norm_bwd_kernel(NormBwd
   }
 }
 
-// dweight = the sum of the parts: 16 columns a block, each in 64 shares that are added in a fixed order
+// dweight = the sum of the parts: 16 columns a block, each in 64 shares that are added in a fixed order.  In 64 bits: up to 512 parts of either sign, whose sum is often smaller than
+// they are (1999 rows of 999 in fp32: error against 64 bits 1.24e-7 in 32 bits, 0.77e-7 so, 0.61e-7 a sum in 64 bits throughout)
 template <typename T> __global__ void __launch_bounds__(1024) norm_dweight_kernel(const float *__restrict__ part, int parts, int d, T *__restrict__ dweight) {
-  __shared__ float s_part[64][16];
+  __shared__ double s_part[64][16];
   const int c = blockIdx.x * 16 + (threadIdx.x & 15), share = threadIdx.x >> 4;
-  float sum = 0.f;
+  double sum = 0.0;
   if (c < d) {
 #pragma unroll 8
-    for (int p = share; p < parts; p += 64) sum += part[(size_t)p * d + c];
+    for (int p = share; p < parts; p += 64) sum += (double)part[(size_t)p * d + c];
   }
   s_part[share][threadIdx.x & 15] = sum;
   __syncthreads();
   if (threadIdx.x >= 64) return;
-  sum = 0.f;
+  sum = 0.0;
 #pragma unroll
   for (int q = 0; q < 16; ++q) sum += s_part[(threadIdx.x >> 4) * 16 + q][threadIdx.x & 15];
   sum += __shfl_xor(sum, 16, 64);
   sum += __shfl_xor(sum, 32, 64);
-  if (threadIdx.x < 16 && c < d) dweight[c] = from_f32<T>(sum);
+  if (threadIdx.x < 16 && c < d) dweight[c] = from_f32<T>((float)sum);
 }
 
 // The shape for rows of d elements: threads a row, packs a thread.

@@ -47,3 +47,17 @@ def test_zero_rows_without_eps(smoe):
     n = smoe.add_norm_fwd(x, w, eps=0.0)
     assert torch.isnan(n.Y).all() and torch.isinf(n.rstd).all()
     assert (smoe.add_norm_fwd(x, w, eps=1e-45).Y == 0).all()
+
+
+@pytest.mark.parametrize("rows,d", [(1999, 999), (5000, 264), (700, 2048)])
+def test_weight_gradient_in_fp32_in_the_root_mean_square(smoe, rows, d):
+    """Roundings of 2^-24 / sqrt(3) = 3.4e-8 at most in the root mean square: the result's, u's, rstd's twice, and those of the sums of a thread's 2 to 16 rows, of which the last are as
+    large as the sum: sqrt(3.4^2 + 3.4^2 + 2 * 3.4^2 + 2 * 3.4^2) = 8.3e-8.  The sum over the blocks is in 64 bits."""
+    X, w, dY = _normal((rows, d), 1, torch.float32), 1 + 0.1 * _normal((d,), 2, torch.float32), _normal((rows, d), 3, torch.float32)
+    n = smoe.add_norm_fwd(X.cuda(), w.cuda())
+    dw = smoe.add_norm_bwd(dY.cuda(), n.S, w.cuda(), n.rstd)[1]
+    x = _f64(X)
+    want = (_f64(dY) * x / np.sqrt((x * x).mean(-1, keepdims=True) + float(np.float32(1e-6)))).sum(0)
+    off = np.sqrt(np.mean((_f64(dw) - want) ** 2) / np.mean(want ** 2))
+    _log(f"dweight {(rows, d)} {off:.2e}")
+    assert off <= 1e-7
