@@ -243,9 +243,16 @@ int smoe_plinear8_fwd(smoe_ctx *ctx, void *stream, const smoe_rows8 *X, int x_ro
   a.Tk = Tk;
   a.C = Yhat;
   a.call_weights = stored;
+  // Sums of rows rounded to bf16 would err by 2.35e-3, so what rounding took from them is kept beside them, where the sums will be (1.7e-3).  That has room for eight rows, in places of 64 columns.
+  const bool rest = gates && gates_k <= REST_SLOTS && d_out % 64 == 0 && (long long)Tk * gates_k < 0x100000000LL;
+  if (rest) {
+    a.rest = (uint8_t *)Y;
+    a.sum_k = gates_k;
+  }
   rc = product8(ctx, s, a);
-  if (rc == SMOE_OK && gates) rc = launch_combine(s, SMOE_BF16, Yhat, gates, Y, Tk / gates_k, gates_k, d_out);
-  return rc;
+  if (rc != SMOE_OK || !gates) return rc;
+  const int T = Tk / gates_k;
+  return rest ? launch_combine_rest(s, Yhat, gates, Y, T, gates_k, d_out) : launch_combine(s, SMOE_BF16, Yhat, gates, Y, T, gates_k, d_out);
 }
 
 size_t smoe_mlp8_fwd_workspace_bytes(smoe_act act, int T, int k, int d_model, int d_expert) {

@@ -40,6 +40,9 @@ int launch_rows8_unpack(hipStream_t s, smoe_dtype dt, const smoe_rows8 &in, int 
 // Y[t] = sum_j g[t k + j] Yhat[t k + j] of rows as S2S8Args has them with C_exps, rounded to bf16 once
 // (exp_cols: the columns that share a power of two, 64 or 128)
 int launch_combine_f16(hipStream_t s, const void *Yhat, const uint8_t *exps, int exp_cols, const float *g, void *Y, int T, int k, int d);
+// The same of rows in bf16 and what rounding took from them (S2S8Args::rest), which lies in Y and makes way for the sums
+constexpr int REST_SLOTS = 8;
+int launch_combine_rest(hipStream_t s, const void *Yhat, const float *g, void *Y, int T, int k, int d);
 int launch_weights8_pack(hipStream_t s, smoe_dtype dt, const void *W, const smoe_weights8 &out);
 
 // ---- products (gemm8_decode.hip, gemm8_stream.hip)
@@ -55,6 +58,11 @@ struct S2S8Args {
   void *C = nullptr;
   bool wide = false;
   uint8_t *C_exps = nullptr;
+  // C in bf16 for sums of up to REST_SLOTS rows each, d_out a multiple of 64: what rounding took from a row goes where the sums will be, in two bits an element.
+  // The place of 64 columns' sums, 128 bytes, has 16 for each row i % sum_k: words [32 columns][odd or even four of them], byte b, bits 2 g and 2 g + 1 for
+  // column 8 g + 4 odd + b.  NULL: not kept.
+  uint8_t *rest = nullptr;
+  int sum_k = 1;
   smoe_rows8 H{nullptr, nullptr};  // in C's place: expert-sorted
   int act = SMOE_ACT_NONE;
   size_t call_weights = 0;         // bytes of all the weights that the call may read: past the last-level cache they are read past it
@@ -83,6 +91,17 @@ __device__ __forceinline__ float e4m3_scaled(float x, unsigned int byte) {
   float y = x * __uint_as_float((254u - byte) << 23);
   if (byte == 247u) y = fabsf(y) > 240.f ? copysignf(240.f, y) : y;      // e = 120: the code above 240 would stand for 2^128
   return fabsf(x) < INFINITY ? y : NAN;
+}
+// Where x lies between the halves of steps around the bf16 number nearest to it, in quarters of a step: 0 .. 3, in bits 14 and 15
+__device__ __forceinline__ unsigned int bf16_rest_at_14(float x) {
+  const unsigned int u = __float_as_uint(x);
+  return u + 0x7fffu + ((u >> 16) & 1u);
+}
+__device__ __forceinline__ unsigned int bf16_rest(float x) { return (bf16_rest_at_14(x) >> 14) & 3u; }
+// The number back, in the middle of its quarter, from the upper half of its bits; zeros, infinities and NaN, and those under 2^-126, as they are
+__device__ __forceinline__ float bf16_with_rest(unsigned int upper, unsigned int rest) {
+  const bool plain = ((upper + 0x800000u) & 0x7f000000u) == 0u;      // exponents 0 and 255
+  return __uint_as_float(plain ? upper : upper + (rest << 14) - 0x6000u);
 }
 __device__ __forceinline__ unsigned int e4m3_four(float a, float b, float c, float d, unsigned int byte) {
   const int lo = __builtin_amdgcn_cvt_pk_fp8_f32(e4m3_scaled(a, byte), e4m3_scaled(b, byte), 0, false);

@@ -242,6 +242,21 @@ __global__ void __launch_bounds__(64 * CW * KW, 2) s2s8_decode_kernel(S2S8Args a
             *reinterpret_cast<bf16x4 *>((bf16_t *)a.C + dst * a.W.d_out + col) = v;
           }
         }
+        if (OUT == ROWS_BF16 && a.rest) {
+          const size_t t = (unsigned int)dst / (unsigned int)a.sum_k;
+          unsigned int *to = reinterpret_cast<unsigned int *>(a.rest + t * a.W.d_out * 2 + (size_t)tile * 128 + (dst - t * a.sum_k) * 16);
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            unsigned int word = 0;
+#pragma unroll
+            for (int j = 2 * h; j < 2 * h + 2; ++j)
+#pragma unroll
+              for (int c = 0; c < 4; ++c) word |= bf16_rest(acc[m][j][c]) << (8 * c + 4 * (j & 1));
+            word <<= 2 * (q >> 1);
+            word |= __shfl_xor(word, 32, 64);
+            if (i < row_end && q < 2 && tile * 64 < a.W.d_out) to[2 * h + q] = word;
+          }
+        }
       } else {
         // two groups are a block of 32 hidden units, spread over the four lanes of a row
         constexpr int BLOCKS = ACT == SMOE_ACT_SWIGLU ? 1 : 2;

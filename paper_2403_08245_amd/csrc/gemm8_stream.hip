@@ -40,9 +40,9 @@ using Big8 = Shape8<4>;
 using Half8 = Shape8<2>;
 using Half8Once = Shape8<2, true>;
 
-enum { OUT_BF16, OUT_F16, OUT_SWIGLU, OUT_GELU };
+enum { OUT_BF16, OUT_F16, OUT_SWIGLU, OUT_GELU, OUT_BF16_REST };
 // store instructions that a wavefront issues per tile
-template <int FM, int OUT> constexpr int Stores8 = FM * (OUT == OUT_BF16 ? 8 : OUT == OUT_F16 ? 9 : OUT == OUT_SWIGLU ? 3 : 5);
+template <int FM, int OUT> constexpr int Stores8 = FM * (OUT == OUT_BF16 ? 8 : OUT == OUT_BF16_REST ? 10 : OUT == OUT_F16 ? 9 : OUT == OUT_SWIGLU ? 3 : 5);
 
 // first[e] = M-tiles of the experts before e, by every wavefront for itself (all write the same); returns first[E]
 template <int TM> __device__ __forceinline__ int number_tiles8(const int32_t *offsets, int E, int *first, int lane) {
@@ -266,6 +266,46 @@ __device__ __forceinline__ void store_wave_tile_f16(const f32x16 (&acc)[FM][FR],
   issue_row_store(pend);
 }
 
+// The rows in bf16 of a weighted sum, and what rounding took from them (S2S8Args::rest): of 64 columns a lane has every other four, and with its neighbour's in
+// the other half of the wavefront the 16 bytes of its row.
+template <int FM, typename DestFn, typename RestFn>
+__device__ __forceinline__ void store_wave_tile_rest(const f32x16 (&acc)[FM][FR], char *patch, DestFn dest, RestFn put_rest, int lane) {
+  acc_settle();
+  RowStore<decltype(dest(0, 0))> pend;
+#pragma unroll
+  for (int fm = 0; fm < FM; ++fm)
+#pragma unroll
+    for (int half = 0; half < 2; ++half) {
+      unsigned int word[2];
+      pipe_block(pend, patch, lane, [&] {
+#pragma unroll
+        for (int f2 = 0; f2 < 2; ++f2) {
+          unsigned int bits = 0;
+#pragma unroll
+          for (int g = 0; g < 4; ++g) {
+            bf16x4 v;
+            unsigned int t[4];
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+              const float x = acc_read(acc[fm][half * 2 + f2][g * 4 + q]);
+              v[q] = (bf16_t)x;
+              t[q] = bf16_rest_at_14(x);
+            }
+            // bits 14 and 15 of each, four to a word, in front of those of the g before
+            const unsigned int lo = __builtin_amdgcn_perm(t[1], t[0], 0x0c0c0501u), hi = __builtin_amdgcn_perm(t[3], t[2], 0x05010c0cu);
+            bits = ((lo | hi) & 0xc0c0c0c0u) | ((bits >> 2) & 0x3f3f3f3fu);
+            patch_put(patch, lane, f2, g, v);
+          }
+          word[f2] = bits;
+        }
+      }, dest(fm, half));
+      const unsigned int other[2] = {(unsigned int)__shfl_xor((int)word[0], 32, 64), (unsigned int)__shfl_xor((int)word[1], 32, 64)};
+      put_rest(fm, half, i32x4{(int)word[0], (int)other[0], (int)word[1], (int)other[1]});
+    }
+  sched_fence();
+  issue_row_store(pend);
+}
+
 // Sixteen values of a row's block of 32 (its other lane has the rest): their codes, four to a word, and the block's byte.
 __device__ __forceinline__ unsigned int pack_block(float (&h)[16], unsigned int (&code)[4]) {
   float amax = 0.f;
@@ -294,7 +334,7 @@ __device__ __forceinline__ unsigned int pack_block(float (&h)[16], unsigned int 
 
 // EVEN: an even number of stages, so that every tile starts in slot 0 and slots are constants.
 template <typename S, int OUT, bool SCATTER, bool EVEN>
-__global__ void __launch_bounds__(NTHREADS, 1) s2s8_stream_kernel(S2S8Args a, int tiles_n, int group_m, uint32_t magic_a) {
+__global__ void __launch_bounds__(NTHREADS, 1) s2s8_stream_kernel(S2S8Args a, int tiles_n, int group_m, uint32_t magic_a, uint32_t magic_sum) {
   constexpr bool HIDDEN = OUT == OUT_SWIGLU || OUT == OUT_GELU;
   constexpr int STORES = Stores8<S::FM, OUT>;
   extern __shared__ __attribute__((aligned(1024))) char smem[];
@@ -509,6 +549,14 @@ __global__ void __launch_bounds__(NTHREADS, 1) s2s8_stream_kernel(S2S8Args a, in
           const uint32_t off = lane < 32 && r < left && wcol < N ? (uint32_t)idx[r] * (uint32_t)per_row + (uint32_t)(wcol / 128) : ~0u;
           __builtin_amdgcn_raw_buffer_store_b8((char)e, win_e, (int)off, 0, 0);
         }, lane);
+      } else if constexpr (OUT == OUT_BF16_REST) {
+        const window_t win_r = make_window(p->rest, (uint32_t)(p->Tk / p->sum_k) * (uint32_t)N * 2);
+        store_wave_tile_rest(acc, patch, dest, [&](int fm, int block, i32x4 rest) {
+          const int r = fm * 32 + (lane & 31), col = wcol + block * 64;
+          const uint32_t row = (uint32_t)idx[r], t = magic_sum ? __umulhi(row, magic_sum) : row;
+          const uint32_t off = lane < 32 && r < left && col < N ? (t * (uint32_t)N + (uint32_t)col) * 2 + (row - t * (uint32_t)p->sum_k) * 16 : ~0u;
+          __builtin_amdgcn_raw_buffer_store_b128(rest, win_r, (int)off, 0, 0);
+        }, lane);
       } else {
         store_wave_tile(acc, patch, dest, lane);
       }
@@ -576,8 +624,8 @@ template <typename S, int OUT, bool SCATTER> int launch_as(hipStream_t s, const 
   const int tiles_n = OUT == OUT_SWIGLU ? ceil_div(hidden, TB / 2) : OUT == OUT_GELU ? ceil_div(hidden, TB) : ceil_div(a.W.d_out, TB);
   const uint32_t magic = a.a_map.o ? division_magic(a.a_map.fan) : 0u;
   const dim3 grid(a.grid), block(NTHREADS);
-  if (steps % 2 == 0 || steps == 1) hipLaunchKernelGGL((s2s8_stream_kernel<S, OUT, SCATTER, true>), grid, block, S::LDS_BYTES, s, a, tiles_n, a.group_m, magic);
-  else hipLaunchKernelGGL((s2s8_stream_kernel<S, OUT, SCATTER, false>), grid, block, S::LDS_BYTES, s, a, tiles_n, a.group_m, magic);
+  if (steps % 2 == 0 || steps == 1) hipLaunchKernelGGL((s2s8_stream_kernel<S, OUT, SCATTER, true>), grid, block, S::LDS_BYTES, s, a, tiles_n, a.group_m, magic, division_magic(a.sum_k));
+  else hipLaunchKernelGGL((s2s8_stream_kernel<S, OUT, SCATTER, false>), grid, block, S::LDS_BYTES, s, a, tiles_n, a.group_m, magic, division_magic(a.sum_k));
   SMOE_LAUNCH_CHECK();
   return SMOE_OK;
 }
@@ -585,6 +633,7 @@ template <typename S> int launch(hipStream_t s, const S2S8Args &a) {
   if (a.act == SMOE_ACT_SWIGLU) return launch_as<S, OUT_SWIGLU, false>(s, a);
   if (a.act == SMOE_ACT_GELU) return launch_as<S, OUT_GELU, false>(s, a);
   if (a.C_exps) return launch_as<S, OUT_F16, true>(s, a);
+  if (a.rest) return launch_as<S, OUT_BF16_REST, true>(s, a);
   return a.c_map.o ? launch_as<S, OUT_BF16, true>(s, a) : launch_as<S, OUT_BF16, false>(s, a);
 }
 template <typename S, int OUT, bool SCATTER> int init_as() {
@@ -595,6 +644,7 @@ template <typename S> int init() {
   int rc = init_as<S, OUT_SWIGLU, false>();
   if (rc == SMOE_OK) rc = init_as<S, OUT_GELU, false>();
   if (rc == SMOE_OK) rc = init_as<S, OUT_F16, true>();
+  if (rc == SMOE_OK) rc = init_as<S, OUT_BF16_REST, true>();
   if (rc == SMOE_OK) rc = init_as<S, OUT_BF16, true>();
   if (rc == SMOE_OK) rc = init_as<S, OUT_BF16, false>();
   return rc;
@@ -612,7 +662,7 @@ int init_stream8_kernels() {
 // 32-bit offsets into the rows, an expert's weights and a scattered output; the fan-out's division.
 bool s2s8_stream_supported(const S2S8Args &a) {
   if (a.Tk < 1 || a.W.E > MAX_E8 || a.grid < 8) return false;
-  if (a.wide || (a.C_exps && !a.c_map.o)) return false;
+  if (a.wide || ((a.C_exps || a.rest) && !a.c_map.o)) return false;
   const unsigned long long pitch = pitch8(a.W.d_in), rows = a.a_map.o ? a.Tk / a.a_map.fan : 256;
   if (rows * pitch > 0x7fff0000ULL || (unsigned long long)groups8(a.W.d_out, a.W.halves) * 16 * pitch + 32 * pitch * 16 > 0x7fff0000ULL) return false;
   if (!a.H.values && a.c_map.o && (unsigned long long)a.Tk * a.W.d_out * 2 > 0xfffffff0ULL) return false;

@@ -115,6 +115,48 @@ __global__ void __launch_bounds__(256) combine_f16_kernel(const uint4 *__restric
   }
 }
 
+// The weighted sum of up to K slots' rows in bf16, to within an eighth of their last place, with what rounding took from them, which lies where the sums go: the eight
+// threads of 64 columns, which are one wavefront's, read it in front of writing those.
+template <int K>
+__global__ void __launch_bounds__(256) combine_rest_kernel(const uint4 *__restrict__ Yhat, const float *__restrict__ g, uint4 *Y, long long chunks, int k, int per_row) {
+  typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
+  typedef bf16_t bf16x8 __attribute__((ext_vector_type(8)));
+  for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < chunks; i += (long long)gridDim.x * 256) {
+    const long long t = i / per_row;                                 // per_row: whole eights
+    const int c = (int)(i - t * per_row), at = c & 7;
+    const u32x4 *src = reinterpret_cast<const u32x4 *>(Yhat) + t * k * per_row + c;
+    const uint2 *rest = reinterpret_cast<const uint2 *>(Y + (i - at)) + at / 4;
+    u32x4 row[K];
+    uint2 bits[K];
+    float w[K];
+#pragma unroll
+    for (int j = 0; j < K; ++j)
+      if (j < k) {
+        row[j] = __builtin_nontemporal_load(src + (long long)j * per_row);
+        bits[j] = rest[2 * j];
+        w[j] = g[t * k + j];
+      }
+    float acc[8];
+#pragma unroll
+    for (int q = 0; q < 8; ++q) acc[q] = 0.f;
+#pragma unroll
+    for (int j = 0; j < K; ++j)
+      if (j < k) {
+        const unsigned int first = bits[j].x >> (2 * (at & 3)), second = bits[j].y >> (2 * (at & 3));
+#pragma unroll
+        for (int q = 0; q < 8; ++q) {
+          const unsigned int upper = q & 1 ? row[j][q / 2] & 0xffff0000u : row[j][q / 2] << 16;
+          acc[q] = fmaf(w[j], bf16_with_rest(upper, ((q < 4 ? first : second) >> (8 * (q & 3))) & 3u), acc[q]);
+        }
+      }
+    bf16x8 o;
+#pragma unroll
+    for (int q = 0; q < 8; ++q) o[q] = (bf16_t)acc[q];
+    __builtin_amdgcn_wave_barrier();
+    Y[i] = __builtin_bit_cast(uint4, o);
+  }
+}
+
 // A block packs one step of 128 of the contraction of 64 columns: rows of W into LDS, a thread takes 32 elements of a column.
 template <typename T>
 __global__ void __launch_bounds__(256) weights8_pack_kernel(const T *__restrict__ W, smoe_weights8 out, int groups, int steps) {
@@ -187,6 +229,18 @@ int launch_combine_f16(hipStream_t s, const void *Yhat, const uint8_t *exps, int
   else if (k == 2) go(combine_f16_kernel<2>);
   else if (k <= 4) go(combine_f16_kernel<4>);
   else go(combine_f16_kernel<8>);
+  SMOE_LAUNCH_CHECK();
+  return SMOE_OK;
+}
+int launch_combine_rest(hipStream_t s, const void *Yhat, const float *g, void *Y, int T, int k, int d) {
+  const int per_row = d / 8;
+  const long long chunks = (long long)T * per_row;
+  const dim3 grid(row_blocks(chunks)), block(256);
+  auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, block, 0, s, (const uint4 *)Yhat, g, (uint4 *)Y, chunks, k, per_row); };
+  if (k == 1) go(combine_rest_kernel<1>);
+  else if (k == 2) go(combine_rest_kernel<2>);
+  else if (k <= 4) go(combine_rest_kernel<4>);
+  else go(combine_rest_kernel<REST_SLOTS>);
   SMOE_LAUNCH_CHECK();
   return SMOE_OK;
 }
