@@ -323,9 +323,13 @@ template <int ACT, int OUT, int CW, int KW> int launch_as(hipStream_t s, const S
 // How the wavefronts of a block divide the work: side by side, or along the contraction where there are too few columns to fill the chip.  One product, weights from
 // memory, us, 4 x 1 / 2 x 2 / 1 x 4: 64 tokens on 64 experts, k = 8, 512 -> 2048 13.6 / 15.7 / 18.9; 200 tokens on 8 experts, k = 2, 2816 -> 1024 22.6 / 14 / 10.3;
 // four tokens on 64 experts, k = 8, 512 -> 2048 8.7 / 8 / 10.7; 16 tokens on 8 experts, k = 2, 14336 -> 4096 94 / 75 / 73.5.
-// Groups of columns that lie an odd number of 32 KB apart get in one another's way when 16 of them are read in step, with up to 16 rows an expert: 64 tokens on 64
-// experts, k = 8, -> 8192: 2048 206 / 191 / 174, 1024 105 / 95 / 108, 4096 wide (-> 4096) 183 / 207 / 195, 1920 (-> 4096) 94.5 / 95.3 / 97.5.  (Wavefronts that begin
-// at different steps of the contraction gained 0 to 4 % there and cost others up to 40 %.)
+// Groups of columns that lie an odd number of 32 KB apart (16 steps of the contraction, 48, ..) get in one another's way when 16 of them are read in step, with up to 16
+// rows an expert, and so do some at odd numbers of 16 KB: 1 / 2 / 4 shares, T tokens on E experts, us:
+//   2048 -> 8192 (64 on 64, k = 8) 203 / 188 / 173, -> 6144 157 / 150 / 136, -> 4096 108 / 105 / 94, -> 16384 (32 on 16, k = 2) 112 / 103 / 91, -> 8192 (64 on 32, k = 4) 109 / 105 / 95
+//   1024 -> 8192 (64 on 64) 107 / 99 / 114, -> 4096 59 / 53 / 60, -> 16384 (32 on 16) 57 / 50 / 56, -> 20480 (32 on 8) 41 / 35 / 39, -> 8192 (64 on 32) 59 / 52 / 59
+//   further odd numbers: 5120 -> 8192 (32 on 16) 121 / 115 / 117, 6144 -> 8192 136 / 136 / 137, 10240 -> 8192 231 / 234 / 226
+//   others: 4096 -> 8192 96 / 111 / 103, 2560 -> 8192 62.6 / 62.5 / 62.7, 1536 -> 4096 (64 on 64) 77 / 78 / 81
+// (Wavefronts that begin at different steps of the contraction gained 0 to 4 % and cost others up to 40 %.)
 template <int ACT, int OUT> int launch(hipStream_t s, const S2S8Args &a) {
   const long long experts = a.Tk < a.W.E ? a.Tk : a.W.E, units = a.W.d_out / 64;
   const int steps = ceil_div(a.W.d_in, ROW8);
