@@ -143,3 +143,17 @@ def test_many_rows_of_all_sizes_on_the_kernels_for_few(smoe, d_model):
     off, size = _pieces(got - want), _pieces(want)
     assert (off <= ONE * size + 1e-37).all()                # under 1e-37 fp32 has fewer bits
     assert torch.isnan(Y[77]).all() and torch.isfinite(Y[[76, 78, 1233, 1235]]).all()
+
+
+def test_small_rows_on_the_kernels_for_few(smoe):
+    """Rows down to 2^-112, whose codes stand for numbers next to the least that bf16 and fp32 hold in full."""
+    T, d, E, k = 60, 256, 3, 1
+    idx, gates, r, code, X, W1, W2, packed = _mlp_case(smoe, T, d, 160, E, k, "gelu", seed=201)
+    X = (X.float() * 2.0 ** torch.linspace(-112, -40, T).round()[:, None]).to(torch.bfloat16)
+    smoe.set_kernel_mode(FEW)
+    Y = _f64(smoe.mlp8_fwd(smoe.rows8_pack(X.cuda()), *packed, r, k, torch.from_numpy(gates).cuda(), code))
+    x = oracle.unpack8(*oracle.pack8(_f64(X)), d)
+    want, _ = oracle.mlp8(x, _stored(smoe, W1), _stored(smoe, W2), idx, gates.astype(np.float64), code)
+    off, size = _pieces(Y - want), _pieces(want)
+    assert (off <= ONE * size + 1e-37).all()
+    assert _rms(Y[20:] / np.abs(want[20:]).max(1, keepdims=True) - want[20:] / np.abs(want[20:]).max(1, keepdims=True)) <= 1e-3      # rounding alone: 1.66e-3 of a value, a third of the largest
