@@ -311,8 +311,8 @@ template <int ACT, int OUT, int CW, int KW> int launch_as(hipStream_t s, const S
   const long long blocks = ((long long)a.Tk / DM + a.W.E) * n_chunks;                       // >= sum_e ceil(n_e / DM)
   const dim3 grid((unsigned)blocks), block(64 * CW * KW);
   // Weights over half of the last-level cache are not there any more when the layer's turn comes again: read past it.  Three layers in turn, us, through /
-  // past: 64 tokens on 64 experts, 2048 -> 2 x 512 -> 2048 (208 MB each) 46.3 / 44.7; 32 tokens on 16 experts, 4096 -> 2 x 1024 -> 4096 (208 MB) 48 / 45.3; 64
-  // tokens on 8 experts, 1024 -> 2 x 2816 -> 1024 (71 MB) 26 / 30.
+  // past: 64 tokens on 64 experts, 2048 -> 2 x 512 -> 2048 (208 MB each) 47.8 / 45; 32 tokens on 16 experts, 4096 -> 2 x 1024 -> 4096 (208 MB) 45.5 / 42.8; 64
+  // tokens on 8 experts, 1024 -> 2 x 2816 -> 1024 (71 MB) 27 / 30.
   if (a.call_weights > LAST_LEVEL_CACHE / 2)
     hipLaunchKernelGGL((s2s8_decode_kernel<ACT, OUT, CW, KW, true>), grid, block, 0, s, a, n_chunks, groups, steps, pitch8(a.W.d_in), h_pitch);
   else

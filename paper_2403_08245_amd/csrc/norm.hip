@@ -1,7 +1,7 @@
 // The root-mean-square norm of the residual stream with the addition in front of it, its gradient, and its output in 8 bits.
 // Bound: HBM, each tensor read or written once; a row stays in registers between its sum and its output.  Rows of 2048 in bf16, 8192 of them: forward 22.5 us
 // (134 MB, 6.0 TB/s), with 8 bits besides 27.5, 8 bits only 21, gradient 30 (4.5 TB/s); 8191 of 4096: 46, 57, 44, 51; 4000 of 5001, whose rows start off the
-// 16-byte lines: 42 (3.8 TB/s), 46, 40, 74 (loads of single elements: 66, 80, 69, 85).
+// 16-byte lines: 43 (3.7 TB/s), 46, 41, 75 (loads of single elements: 66, 80, 69, 85).
 #include "block.h"
 #include <algorithm>
 #include <type_traits>

@@ -1,5 +1,5 @@
-// Rows in 8 bits: packing and unpacking them, and packing weights into the layout of the products.  Bound: HBM (8191 rows of 4096 to bf16 17 us, 102 MB,
-// 6.0 TB/s).
+// Rows in 8 bits: packing and unpacking them, and packing weights into the layout of the products.  Bound: HBM (8191 rows of 4096 from bf16 23 us, 102 MB,
+// 4.4 TB/s, from fp32 31; to bf16 17, 5.9 TB/s).
 #include "block.h"
 
 namespace {
