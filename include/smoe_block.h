@@ -98,7 +98,7 @@ int smoe_add_norm_bwd(smoe_ctx *ctx, void *stream, smoe_dtype dtype, const void 
  * smoe_plinear_fwd on rows and weights in 8 bits, bf16 out: X [x_rows, d_in] and W (halves = 1) as packed, the other arguments as there;
  * d_out a multiple of 8.  No workspace.  Products are summed in fp32 over the contraction; the matrix instructions add each 64 or 128 of
  * them with an error of about 2^-12 of the largest (1.5e-5 of the sum for normal values), under the output's rounding.  With gates, Y is the sum
- * of the rows of Yhat as they were to within 2^-11 before their rounding to bf16, for gates_k up to 8 and d_out of whole 64s; else of the rounded ones.  Kernel modes 1 and 2 of
+ * of the rows of Yhat as they were to within 2^-10 before their rounding to bf16, for gates_k up to 8 and d_out of whole 64s; else of the rounded ones.  Kernel modes 1 and 2 of
  * smoe_set_kernel_mode force the kernels for few rows, 3 and 4 the 128 x 256 / 256 x 256 tiles. */
 int smoe_plinear8_fwd(smoe_ctx *ctx, void *stream, const smoe_rows8 *X, int x_rows, int d_in, const smoe_weights8 *W, int d_out, const smoe_routing *r,
                       int k, const float *gates, int gates_k, int grouped_in, int grouped_out, void *Yhat, void *Y);
