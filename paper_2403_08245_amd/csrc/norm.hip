@@ -124,9 +124,10 @@ __global__ void __launch_bounds__(TPR > 64 ? TPR : 256) norm_kernel(NormArgs a, 
     for (int q = 0; q < V; ++q) sum = fmaf(x[i].v[q], x[i].v[q], sum);
   }
   sum = row_sum<TPR>(sum, s_sum);
-  float rstd = 1.0f / sqrtf(sum / (float)a.d + a.eps), by = 1.0f;      // y = s by rstd weight
+  const float square = sum / (float)a.d + a.eps;
+  float rstd = 1.0f / sqrtf(square), by = 1.0f;        // y = s by rstd weight
   // Squares past fp32's range, or so far under 1 that they lose bits or vanish, with an eps that does not hide that: the same of values `by` times as large.
-  const bool large = !(sum < INFINITY);
+  const bool large = !(square < INFINITY);
   if (__builtin_expect(large || (sum < (float)a.d * 0x1p-100f && a.eps < 0x1p-80f), 0)) {
     by = large ? 0x1p-70f : 0x1p100f;
     sum = 0.f;

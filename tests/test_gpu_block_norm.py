@@ -61,3 +61,14 @@ def test_weight_gradient_in_fp32_in_the_root_mean_square(smoe, rows, d):
     off = np.sqrt(np.mean((_f64(dw) - want) ** 2) / np.mean(want ** 2))
     _log(f"dweight {(rows, d)} {off:.2e}")
     assert off <= 1e-7
+
+
+@pytest.mark.parametrize("d", [1, 2, 500])
+def test_mean_square_and_eps_past_fp32_together(smoe, d):
+    """Each of them within fp32's range (500 elements: the sum of the squares is not), their sum past it."""
+    for dtype in (torch.bfloat16, torch.float32):
+        x, w = (torch.linspace(1.0, 1.25, 4 * d).view(4, d) * 2.0 ** 63).to(dtype), torch.ones(d, dtype=dtype)
+        n = smoe.add_norm_fwd(x.cuda(), w.cuda(), eps=3e38)
+        _, y, rstd = oracle.add_norm(_f64(x), None, np.ones(d), float(np.float32(3e38)))
+        _near(n.Y, y, (HALF[dtype] + 1.01 * NORM_UNITS + 2.0 ** -23) * np.abs(y), "Y")
+        _near(n.rstd, rstd, NORM_UNITS * rstd, "rstd")
